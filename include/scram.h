@@ -25,7 +25,11 @@
  * 4.2.1) restricts both steps to keys at or before the query in raster order.
  *
  * scram_sparse_attend_backward gives the gradients of step 2 with respect to
- * Q, K and V with the maps held fixed.
+ * Q, K and V with the maps held fixed.  scram_differential_attend takes the
+ * difference of two softmax maps over the same keys instead.
+ *
+ * Around them, for the layer that uses them: scram_layer_norm (the rows of Q
+ * and K, or of the output) and scram_rotary (positions on the grid).
  *
  * scram_snis_attend replaces the window of step 2 by the self-normalised
  * importance-sampling estimator of Section 4.2 (Monte Carlo estimators,
@@ -358,6 +362,139 @@ int scram_snis_attend(const void* Q, const void* K, const void* V, int dtype, co
  */
 int scram_pad_channels(int count, const void* const* src, void* const* dst, const int64_t* rows, const int* widths,
                        int width, int elem_bytes, int unpad, hipStream_t stream);
+
+/*
+ * Differential attention around the matches: the difference of two softmax
+ * maps over the key set of scram_sparse_attend.  A row of Q and K holds the
+ * channels of two maps, the first half and the last; with a1_ij = scale *
+ * q1_i . k1_j, a2_ij likewise and W_i the union of query i's windows,
+ *   out_i = sum_{j in W_i} (softmax_j(a1_ij) - lam[s] * softmax_j(a2_ij)) v_j
+ * for the queries of slice s (a zero row if W_i is empty).  The softmaxes are
+ * fp32 and online; the difference is taken of their normalised fp32 sums of
+ * values and rounded once.  A key that is not in W_i does not reach query i,
+ * whatever its rows hold.
+ *
+ * Arguments: as scram_sparse_attend, plus
+ *   lam       fp32 [S] weight of the second map, on the device
+ *   scale     softmax temperature of both maps, 1/sqrt(d/2) by custom; finite
+ *   flags     0 or SCRAM_CAUSAL
+ *   first, origin
+ *             with SCRAM_CAUSAL the queries of a slice stand for the run
+ *             r, r + 1, ..., r + Hq*Wq - 1 of its keys in raster order, and
+ *             query r + i sees the keys up to r + i: r = first (0 where the
+ *             grids are the same), or, with origin (int32 [S] on the device),
+ *             a position for each slice, clamped into the key grid; first is
+ *             then 0.  Needs Wq == Wk or Hq == 1, and first + Hq*Wq <= Hk*Wk.
+ *             0 and NULL without SCRAM_CAUSAL.
+ *   events    nullable array of 2 caller-created HIP events stamped with the
+ *             start and the end
+ * Returns a status code.
+ */
+int scram_differential_attend(const void* Q, const void* K, const void* V, int dtype, const int32_t* argmax, int kappa,
+                              const float* lam, int S, int Hq, int Wq, int Hk, int Wk, int d, int dv, int window,
+                              float scale, uint32_t flags, int first, const int32_t* origin, void* out,
+                              hipEvent_t* events, hipStream_t stream);
+
+/*
+ * Gradients of scram_differential_attend with the maps held fixed.  With p1,
+ * p2 the two softmaxes, dp_ij = dO_i . v_j and D1_i = sum_j p1_ij dp_ij, D2_i
+ * likewise:
+ *   dQ1_i = scale * sum_j p1_ij (dp_ij - D1_i) k1_j
+ *   dQ2_i = - lam[s] * scale * sum_j p2_ij (dp_ij - D2_i) k2_j
+ *   dK1_j, dK2_j: the same sums over the queries i, of q1_i, q2_i
+ *   dV_j  = sum_i (p1_ij - lam[s] p2_ij) dO_i
+ *   dlam[s] = - sum_i D2_i
+ * in fp32, recomputed from Q, K, V.  A query with an empty set contributes
+ * nothing.  dQ and dlam are deterministic; dK and dV sum a key's queries in
+ * the order that the inverse map was filled in, as in
+ * scram_sparse_attend_backward, and may differ in the last bits between calls.
+ *
+ * Arguments: as scram_differential_attend, plus
+ *   dO        [S, Hq, Wq, dv] in `dtype`
+ *   dQ, dK, dV, dlam
+ *             fp32 [S, Hq, Wq, d], [S, Hk, Wk, d], [S, Hk, Wk, dv], [S] (written)
+ *   workspace device scratch of at least
+ *             scram_differential_attend_backward_workspace_bytes(...) bytes,
+ *             256-byte aligned; contents undefined on return
+ * Also requires S*Hq*Wq*kappa < 2^31 and S*Hk*Wk < 2^31.  No output or the
+ * workspace may overlap an input or another output.  Returns a status code.
+ */
+size_t scram_differential_attend_backward_workspace_bytes(int S, int Hq, int Wq, int Hk, int Wk, int d, int dtype,
+                                                          int kappa);
+
+int scram_differential_attend_backward(const void* Q, const void* K, const void* V, int dtype, const int32_t* argmax,
+                                       int kappa, const float* lam, int S, int Hq, int Wq, int Hk, int Wk, int d,
+                                       int dv, int window, float scale, uint32_t flags, int first,
+                                       const int32_t* origin, const void* dO, float* dQ, float* dK, float* dV,
+                                       float* dlam, void* workspace, size_t workspace_bytes, hipEvent_t* events,
+                                       hipStream_t stream);
+
+/* flags of scram_rotary, and the most channel pairs it turns */
+enum { SCRAM_ROTARY_INTERLEAVED = 1u, SCRAM_ROTARY_INVERSE = 2u };
+enum { SCRAM_ROTARY_MAX_PAIRS = 128 };
+
+/*
+ * Rotary positions on a grid with the axes time, height and width: `count` (1
+ * to 4) tensors of one grid in one launch.  Tensor i is [slices[i], T, H, W,
+ * d] (T = 1: the [S, H, W, d] of the other entry points), its rows split into
+ * `groups` equal groups of channels that are turned alike (2 for the rows of
+ * scram_differential_attend).  In a group the first sections[0] channel pairs
+ * turn with the time, the next sections[1] with the height, the next
+ * sections[2] with the width, the channels after them not at all: pair k
+ * (a, b) of a pixel at position x along its axis becomes
+ *   (a cos t - b sin t, a sin t + b cos t),  t = x * freqs[k].
+ * Pair k is channels (k, k + P) of the group, P = sum of the sections, or with
+ * SCRAM_ROTARY_INTERLEAVED (2k, 2k + 1).  SCRAM_ROTARY_INVERSE turns by -t:
+ * the gradient.  The angle is reduced by whole turns in 64-bit fixed point
+ * (frequencies rounded to 2^-53 of their value), so positions over the whole
+ * int32 range keep their accuracy; sums are fp32, rounded once.
+ *
+ * Arguments:
+ *   src, dst  tensors, aligned to their elements (dst[i] == src[i]: in place)
+ *   d         channels of a row, 2 .. 65536, a multiple of groups
+ *   sections  pairs of time, height, width; 1 to SCRAM_ROTARY_MAX_PAIRS in
+ *             all, 2 P <= d / groups
+ *   freqs     host array of P finite radians per step
+ *   first     host array of 3: position of the grid's first pixel (used when
+ *             origin is NULL)
+ *   origin    nullable int32 [origin_rows, 3] on the device: the same, one row
+ *             for all slices, or one per slice (origin_rows == slices[i])
+ * T*H*W * groups * (d / groups - P) < 2^31.  Returns a status code.
+ */
+int scram_rotary(int count, const void* const* src, void* const* dst, const int* slices, int dtype, int T, int H, int W,
+                 int d, int groups, const int* sections, const double* freqs, const int* first, const int32_t* origin,
+                 int origin_rows, uint32_t flags, hipStream_t stream);
+
+/*
+ * Layer norm of `rows` rows of `channels` (1 .. 16384) channels:
+ *   mu = mean x, r = (mean (x - mu)^2 + eps)^-1/2, y = (x - mu) r weight + bias
+ * in fp32, y rounded to `dtype`.
+ *
+ * Arguments:
+ *   X, Y      [rows, channels] in `dtype` (Y == X: in place)
+ *   weight, bias  nullable [channels] in `weight_dtype`, which is dtype or
+ *             SCRAM_F32 (NULL: ones, zeros)
+ *   eps       >= 0, finite
+ *   mean, rstd  nullable (both) fp32 [rows]: mu and r, for the gradient
+ * Outputs overlap nothing else.  Returns a status code.
+ */
+int scram_layer_norm(const void* X, int dtype, const void* weight, const void* bias, int weight_dtype, int64_t rows,
+                     int channels, float eps, void* Y, float* mean, float* rstd, hipStream_t stream);
+
+/*
+ * Gradients of scram_layer_norm.  With xh = (x - mean) rstd and g = dY weight:
+ *   dX = rstd (g - mean(g) - xh mean(g xh)),  dweight = sum_rows dY xh,  dbias = sum_rows dY
+ * dY and dX are in `grad_dtype`, which is dtype or SCRAM_F32 (dX == dY: in
+ * place); dweight and dbias fp32 [channels], summed in a fixed order.
+ * workspace: scram_layer_norm_backward_workspace_bytes(rows, channels) bytes,
+ * 256-byte aligned.  Outputs overlap nothing else.  Returns a status code.
+ */
+size_t scram_layer_norm_backward_workspace_bytes(int64_t rows, int channels);
+
+int scram_layer_norm_backward(const void* dY, int grad_dtype, const void* X, int dtype, const float* mean,
+                              const float* rstd, const void* weight, int weight_dtype, int64_t rows, int channels,
+                              void* dX, float* dweight, float* dbias, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* scram_status_string(int status);

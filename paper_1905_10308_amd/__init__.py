@@ -25,3 +25,15 @@ from .binding import (  # noqa: F401
     sparse_attend_backward_workspace_bytes,
     status_string,
 )
+from .differential import (  # noqa: F401
+    differential_attend,
+    differential_attend_backward,
+    differential_attend_backward_workspace_bytes,
+)
+from .rows import (  # noqa: F401
+    layer_norm,
+    layer_norm_backward,
+    layer_norm_backward_workspace_bytes,
+    rotary,
+    rotary_backward,
+)

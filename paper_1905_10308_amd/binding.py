@@ -84,6 +84,22 @@ def load(path: str) -> ctypes.CDLL:
     L.scram_snis_attend.restype = I
     L.scram_pad_channels.argtypes = [I, P, P, P, P, I, I, I, P]
     L.scram_pad_channels.restype = I
+    F, I64, D = ctypes.c_float, ctypes.c_int64, ctypes.c_double
+    L.scram_differential_attend.argtypes = [P, P, P, I, P, I, P, I, I, I, I, I, I, I, I, F, U32, I, P, P, P, P]
+    L.scram_differential_attend.restype = I
+    L.scram_differential_attend_backward.argtypes = [P, P, P, I, P, I, P, I, I, I, I, I, I, I, I, F, U32, I, P, P, P, P, P, P,
+                                                     P, SZ, P, P]
+    L.scram_differential_attend_backward.restype = I
+    L.scram_differential_attend_backward_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I]
+    L.scram_differential_attend_backward_workspace_bytes.restype = SZ
+    L.scram_rotary.argtypes = [I, P, P, P, I, I, I, I, I, I, P, ctypes.POINTER(D), P, P, I, U32, P]
+    L.scram_rotary.restype = I
+    L.scram_layer_norm.argtypes = [P, I, P, P, I, I64, I, F, P, P, P, P]
+    L.scram_layer_norm.restype = I
+    L.scram_layer_norm_backward.argtypes = [P, I, P, I, P, P, P, I, I64, I, P, P, P, P, SZ, P]
+    L.scram_layer_norm_backward.restype = I
+    L.scram_layer_norm_backward_workspace_bytes.argtypes = [I64, I]
+    L.scram_layer_norm_backward_workspace_bytes.restype = SZ
     L.scram_status_string.argtypes = [I]
     L.scram_status_string.restype = ctypes.c_char_p
     L.scram_abi_version.argtypes = []
@@ -520,9 +536,39 @@ def _paddable(*tensors) -> bool:
                for t in tensors) and q.dtype in (torch.float32, torch.bfloat16)
 
 
+def _placed(Q, K, norm, positions, groups):
+    """Q and K normalised and turned by their grid positions, where asked for."""
+    from .rows import layer_norm, rotary
+
+    if norm is not None:
+        wq, bq, wk, bk = norm
+        parts = lambda t: t.view(*t.shape[:-1], groups, t.shape[-1] // groups)  # noqa: E731
+        Q, K = layer_norm(parts(Q), wq, bq).view(Q.shape), layer_norm(parts(K), wk, bk).view(K.shape)
+    if positions is not None:
+        if Q.shape[1:] == K.shape[1:]:
+            Q, K = rotary(Q, K, groups=groups, **positions)
+        else:
+            Q, K = rotary(Q, groups=groups, **positions), rotary(K, groups=groups, **positions)
+    return Q, K
+
+
 def forward(Q, K, V, iters: int, seed: int, window: int, scale: float | None = None, *, kappa: int = 1,
-            sep: int = 1, causal: bool = False):
-    """The whole path: kappa argmax maps, then the sparse attention output over their windows."""
+            sep: int = 1, causal: bool = False, lam=None, norm=None, positions=None):
+    """The whole path: kappa argmax maps, then the sparse attention output over their windows.
+
+    With ``lam`` (fp32 ``[S]``) the rows of Q and K hold two maps and the output is that of
+    :func:`differential_attend` (maps by the whole rows' scores, the sum of the two maps').  ``norm``
+    (``(weight_q, bias_q, weight_k, bias_k)``, any of them None) first normalises the rows of Q and K
+    (:func:`layer_norm`; with ``lam`` each half by itself), and ``positions`` (keyword arguments of
+    :func:`rotary`) then turns them by their grid positions.
+    """
+    if norm is not None or positions is not None:
+        Q, K = _placed(Q, K, norm, positions, 1 if lam is None else 2)
+    if lam is not None:
+        from .differential import differential_attend
+
+        J = patchmatch_kappa(Q, K, kappa, iters, seed, sep=sep, causal=causal)
+        return differential_attend(Q, K, V, J, lam, window, scale, causal=causal), J
     d, dv = Q.shape[-1], V.shape[-1]
     w = _native_width(max(d, dv))
     if d == dv < w and K.shape[-1] == d and _paddable(Q, K, V):  # once for every call below

@@ -55,6 +55,34 @@ int check_type(int dtype, int d)
     return SCRAM_OK;
 }
 
+// Arguments that the differential attend and its gradients share, but for pointers.
+int check_differential(int dtype, const scram::Grid& g, int kappa, int dv, int window, float scale, uint32_t flags, int first,
+                       const int32_t* origin)
+{
+    int rc = check_grid(g.S, g.Hq, g.Wq, g.Hk, g.Wk);
+    if (rc) return rc;
+    if (window < 1 || window % 2 == 0 || window > 32767) return SCRAM_ERR_SHAPE;
+    if (kappa < 1 || kappa > SCRAM_MAX_KAPPA) return SCRAM_ERR_SHAPE;
+    if (!isfinite(scale)) return SCRAM_ERR_SHAPE;
+    if ((rc = check_type(dtype, g.d))) return rc;
+    if (dv != g.d) return SCRAM_ERR_UNSUPPORTED;
+    if (flags & ~uint32_t(SCRAM_CAUSAL)) return SCRAM_ERR_UNSUPPORTED;
+    const int64_t nq = int64_t(g.Hq) * g.Wq, nk = int64_t(g.Hk) * g.Wk;
+    if (!(flags & SCRAM_CAUSAL)) return first != 0 || origin ? SCRAM_ERR_SHAPE : SCRAM_OK;
+    // the queries are a run of the keys' raster: whole rows, or a part of it as one row
+    if (g.Hq != 1 && g.Wq != g.Wk) return SCRAM_ERR_SHAPE;
+    if (first < 0 || (origin && first != 0) || first + nq > nk) return SCRAM_ERR_SHAPE;
+    return SCRAM_OK;
+}
+
+int check_norm(int64_t rows, int channels, int dtype, int weight_dtype)
+{
+    if (rows < 1 || rows >= (int64_t(1) << 40) || channels < 1 || channels > scram::kNormMaxChannels) return SCRAM_ERR_SHAPE;
+    if (dtype != SCRAM_F32 && dtype != SCRAM_BF16) return SCRAM_ERR_UNSUPPORTED;
+    if (weight_dtype != dtype && weight_dtype != SCRAM_F32) return SCRAM_ERR_UNSUPPORTED;
+    return SCRAM_OK;
+}
+
 }  // namespace
 
 namespace scram {
@@ -339,6 +367,200 @@ int scram_pad_channels(int count, const void* const* src, void* const* dst, cons
     }
     const hipError_t e = scram::launch_pad(t, count, width, elem_bytes, unpad != 0, stream);
     return e == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+int scram_differential_attend(const void* Q, const void* K, const void* V, int dtype, const int32_t* argmax, int kappa,
+                              const float* lam, int S, int Hq, int Wq, int Hk, int Wk, int d, int dv, int window, float scale,
+                              uint32_t flags, int first, const int32_t* origin, void* out, hipEvent_t* events,
+                              hipStream_t stream)
+{
+    if (!Q || !K || !V || !argmax || !lam || !out) return SCRAM_ERR_NULL;
+    const scram::Grid grid{S, Hq, Wq, Hk, Wk, d};
+    int rc = check_differential(dtype, grid, kappa, dv, window, scale, flags, first, origin);
+    if (rc) return rc;
+    if (scram::diff_attend_max_blocks(dtype, grid) > kMaxBlocks) return SCRAM_ERR_SHAPE;
+    if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(argmax, 4) || !aligned(lam, 4) ||
+        !aligned(origin, 4))
+        return SCRAM_ERR_ALIGN;
+    const size_t n = size_t(S) * Hq * Wq, nk = size_t(S) * Hk * Wk, eb = elem_bytes(dtype);
+    const Range rO = range(out, n * dv * eb);
+    for (const Range& other : {range(Q, n * d * eb), range(K, nk * d * eb), range(V, nk * dv * eb),
+                               range(argmax, 4 * n * size_t(kappa)), range(lam, 4 * size_t(S)),
+                               range(origin, origin ? 4 * size_t(S) : 0)}) {
+        if (overlap(rO, other)) return SCRAM_ERR_ALIAS;
+    }
+    const scram::DiffCall call{Q, K, V, argmax, kappa, lam, grid, window, scale, (flags & SCRAM_CAUSAL) != 0, first, origin};
+    const hipError_t e = scram::launch_diff_attend(dtype, call, out, stream, events ? events[0] : nullptr,
+                                                   events ? events[1] : nullptr);
+    return e == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+size_t scram_differential_attend_backward_workspace_bytes(int S, int Hq, int Wq, int Hk, int Wk, int d, int dtype, int kappa)
+{
+    if (check_grid(S, Hq, Wq, Hk, Wk) || kappa < 1 || kappa > SCRAM_MAX_KAPPA || check_type(dtype, d)) return 0;
+    return scram::diff_backward_workspace_bytes(scram::Grid{S, Hq, Wq, Hk, Wk, d}, kappa);
+}
+
+int scram_differential_attend_backward(const void* Q, const void* K, const void* V, int dtype, const int32_t* argmax,
+                                       int kappa, const float* lam, int S, int Hq, int Wq, int Hk, int Wk, int d, int dv,
+                                       int window, float scale, uint32_t flags, int first, const int32_t* origin,
+                                       const void* dO, float* dQ, float* dK, float* dV, float* dlam, void* workspace,
+                                       size_t workspace_bytes, hipEvent_t* events, hipStream_t stream)
+{
+    if (!Q || !K || !V || !argmax || !lam || !dO || !dQ || !dK || !dV || !dlam) return SCRAM_ERR_NULL;
+    const scram::Grid grid{S, Hq, Wq, Hk, Wk, d};
+    int rc = check_differential(dtype, grid, kappa, dv, window, scale, flags, first, origin);
+    if (rc) return rc;
+    // the inverse map codes (match, query) pairs as e * n + i in an int32, and keys are numbered across slices
+    if (int64_t(S) * Hq * Wq * kappa >= kMaxCount || int64_t(S) * Hk * Wk >= kMaxCount) return SCRAM_ERR_SHAPE;
+    if (scram::diff_backward_max_blocks(grid) > kMaxBlocks) return SCRAM_ERR_SHAPE;
+    if (!workspace) return SCRAM_ERR_WORKSPACE;
+    if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(dO, 16) || !aligned(argmax, 4) || !aligned(lam, 4) ||
+        !aligned(origin, 4) || !aligned(dQ, 16) || !aligned(dK, 16) || !aligned(dV, 16) || !aligned(dlam, 4) ||
+        !aligned(workspace, 256))
+        return SCRAM_ERR_ALIGN;
+    const size_t need = scram::diff_backward_workspace_bytes(grid, kappa);
+    if (workspace_bytes < need) return SCRAM_ERR_WORKSPACE;
+    const size_t n = size_t(S) * Hq * Wq, nk = size_t(S) * Hk * Wk, eb = elem_bytes(dtype);
+    const Range outs[] = {range(dQ, 4 * n * d), range(dK, 4 * nk * d), range(dV, 4 * nk * dv), range(dlam, 4 * size_t(S)),
+                          range(workspace, need)};
+    for (const Range& o : outs) {
+        for (const Range& other : {range(Q, n * d * eb), range(K, nk * d * eb), range(V, nk * dv * eb),
+                                   range(argmax, 4 * n * size_t(kappa)), range(dO, n * dv * eb), range(lam, 4 * size_t(S)),
+                                   range(origin, origin ? 4 * size_t(S) : 0)}) {
+            if (overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+        for (const Range& other : outs) {
+            if (&o != &other && overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+    }
+    const scram::DiffCall call{Q, K, V, argmax, kappa, lam, grid, window, scale, (flags & SCRAM_CAUSAL) != 0, first, origin};
+    const hipError_t e = scram::launch_diff_backward(dtype, call, dO, dQ, dK, dV, dlam, workspace, stream,
+                                                     events ? events[0] : nullptr, events ? events[1] : nullptr);
+    return e == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+int scram_rotary(int count, const void* const* src, void* const* dst, const int* slices, int dtype, int T, int H, int W, int d,
+                 int groups, const int* sections, const double* freqs, const int* first, const int32_t* origin, int origin_rows,
+                 uint32_t flags, hipStream_t stream)
+{
+    if (!src || !dst || !slices || !sections || !freqs) return SCRAM_ERR_NULL;
+    if (origin ? origin_rows < 1 : !first) return SCRAM_ERR_NULL;
+    if (count < 1 || count > 4) return SCRAM_ERR_SHAPE;
+    if (dtype != SCRAM_F32 && dtype != SCRAM_BF16) return SCRAM_ERR_UNSUPPORTED;
+    if (flags & ~uint32_t(SCRAM_ROTARY_INTERLEAVED | SCRAM_ROTARY_INVERSE)) return SCRAM_ERR_UNSUPPORTED;
+    if (T < 1 || H < 1 || W < 1 || T > kMaxSide || H > kMaxSide || W > kMaxSide) return SCRAM_ERR_SHAPE;
+    if (int64_t(H) * W >= kMaxCount || int64_t(T) * (int64_t(H) * W) >= kMaxCount) return SCRAM_ERR_SHAPE;
+    if (groups < 1 || d < 2 || d > 65536 || d % groups) return SCRAM_ERR_SHAPE;
+    int64_t pairs = 0;
+    for (int a = 0; a < 3; ++a) {
+        if (sections[a] < 0) return SCRAM_ERR_SHAPE;
+        pairs += sections[a];
+    }
+    if (pairs < 1 || pairs > SCRAM_ROTARY_MAX_PAIRS || 2 * pairs > d / groups) return SCRAM_ERR_SHAPE;
+    for (int64_t k = 0; k < pairs; ++k)
+        if (!isfinite(freqs[k])) return SCRAM_ERR_SHAPE;
+    scram::RotaryCall c{};
+    const size_t eb = elem_bytes(dtype), plane = size_t(T) * H * W * d * eb;
+    c.count = count;
+    for (int i = 0; i < count; ++i) {
+        if (!src[i] || !dst[i]) return SCRAM_ERR_NULL;
+        if (slices[i] < 1 || (origin && origin_rows > 1 && slices[i] != origin_rows)) return SCRAM_ERR_SHAPE;
+        if (!aligned(src[i], eb) || !aligned(dst[i], eb)) return SCRAM_ERR_ALIGN;
+        c.src[i] = src[i];
+        c.dst[i] = dst[i];
+        c.slices[i] = slices[i];
+    }
+    if (!aligned(origin, 4)) return SCRAM_ERR_ALIGN;
+    for (int i = 0; i < count; ++i) {
+        const Range o = range(dst[i], plane * slices[i]);
+        if (overlap(o, range(origin, origin ? 12 * size_t(origin_rows) : 0))) return SCRAM_ERR_ALIAS;
+        for (int j = 0; j < count; ++j) {
+            // a tensor may be turned in place, and overlaps nothing otherwise
+            if (!(i == j && src[j] == dst[i]) && overlap(o, range(src[j], plane * slices[j]))) return SCRAM_ERR_ALIAS;
+            if (i != j && overlap(o, range(dst[j], plane * slices[j]))) return SCRAM_ERR_ALIAS;
+        }
+    }
+    c.T = T;
+    c.H = H;
+    c.W = W;
+    c.d = d;
+    c.groups = groups;
+    for (int a = 0; a < 3; ++a) {
+        c.pairs[a] = sections[a];
+        c.first[a] = origin ? 0 : first[a];
+    }
+    c.freq = freqs;
+    c.origin = origin;
+    c.origin_rows = origin_rows;
+    c.interleaved = (flags & SCRAM_ROTARY_INTERLEAVED) != 0;
+    c.inverse = (flags & SCRAM_ROTARY_INVERSE) != 0;
+    if (scram::rotary_items(dtype, c) >= uint64_t(kMaxCount)) return SCRAM_ERR_SHAPE;
+    return scram::launch_rotary(dtype, c, stream) == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+int scram_layer_norm(const void* X, int dtype, const void* weight, const void* bias, int weight_dtype, int64_t rows, int channels,
+                     float eps, void* Y, float* mean, float* rstd, hipStream_t stream)
+{
+    if (!X || !Y || !mean != !rstd) return SCRAM_ERR_NULL;
+    int rc = check_norm(rows, channels, dtype, weight_dtype);
+    if (rc) return rc;
+    if (!(eps >= 0.f) || !isfinite(eps)) return SCRAM_ERR_SHAPE;
+    const size_t eb = elem_bytes(dtype), wb = elem_bytes(weight_dtype);
+    if (!aligned(X, eb) || !aligned(Y, eb) || !aligned(weight, wb) || !aligned(bias, wb) || !aligned(mean, 4) || !aligned(rstd, 4))
+        return SCRAM_ERR_ALIGN;
+    const size_t n = size_t(rows) * channels, stat = mean ? 4 * size_t(rows) : 0;
+    const Range outs[] = {range(Y, n * eb), range(mean, stat), range(rstd, stat)};
+    for (const Range& o : outs) {
+        // Y may be X: a row is read before it is written
+        if (overlap(o, range(X, n * eb)) && !(&o == &outs[0] && Y == X)) return SCRAM_ERR_ALIAS;
+        if (overlap(o, range(weight, weight ? wb * channels : 0)) || overlap(o, range(bias, bias ? wb * channels : 0)))
+            return SCRAM_ERR_ALIAS;
+        for (const Range& other : outs) {
+            if (&o != &other && overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+    }
+    const scram::NormCall c{rows, channels, dtype, dtype, weight_dtype, X, weight, bias, nullptr, eps};
+    return scram::launch_norm(c, Y, mean, rstd, stream) == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+size_t scram_layer_norm_backward_workspace_bytes(int64_t rows, int channels)
+{
+    if (check_norm(rows, channels, SCRAM_F32, SCRAM_F32)) return 0;
+    return scram::norm_backward_workspace_bytes(rows, channels);
+}
+
+int scram_layer_norm_backward(const void* dY, int grad_dtype, const void* X, int dtype, const float* mean, const float* rstd,
+                              const void* weight, int weight_dtype, int64_t rows, int channels, void* dX, float* dweight,
+                              float* dbias, void* workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    if (!dY || !X || !mean || !rstd || !dX || !dweight || !dbias) return SCRAM_ERR_NULL;
+    int rc = check_norm(rows, channels, dtype, weight_dtype);
+    if (rc) return rc;
+    if (grad_dtype != dtype && grad_dtype != SCRAM_F32) return SCRAM_ERR_UNSUPPORTED;
+    if (!workspace) return SCRAM_ERR_WORKSPACE;
+    const size_t eb = elem_bytes(dtype), gb = elem_bytes(grad_dtype), wb = elem_bytes(weight_dtype);
+    if (!aligned(X, eb) || !aligned(dY, gb) || !aligned(dX, gb) || !aligned(weight, wb) || !aligned(mean, 4) || !aligned(rstd, 4) ||
+        !aligned(dweight, 4) || !aligned(dbias, 4) || !aligned(workspace, 256))
+        return SCRAM_ERR_ALIGN;
+    const size_t need = scram::norm_backward_workspace_bytes(rows, channels);
+    if (workspace_bytes < need) return SCRAM_ERR_WORKSPACE;
+    const size_t n = size_t(rows) * channels;
+    const Range outs[] = {range(dX, n * gb), range(dweight, 4 * size_t(channels)), range(dbias, 4 * size_t(channels)),
+                          range(workspace, need)};
+    for (const Range& o : outs) {
+        // dX may be dY: a row is read before it is written
+        if (overlap(o, range(dY, n * gb)) && !(&o == &outs[0] && dX == dY)) return SCRAM_ERR_ALIAS;
+        for (const Range& other : {range(X, n * eb), range(mean, 4 * size_t(rows)), range(rstd, 4 * size_t(rows)),
+                                   range(weight, weight ? wb * channels : 0)}) {
+            if (overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+        for (const Range& other : outs) {
+            if (&o != &other && overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+    }
+    const scram::NormCall c{rows, channels, dtype, grad_dtype, weight_dtype, X, weight, nullptr, dY, 0.f};
+    return scram::launch_norm_backward(c, mean, rstd, dX, dweight, dbias, workspace, stream) == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
 }
 
 const char* scram_status_string(int status)

@@ -1,5 +1,6 @@
 // Backward of the sparse window attention with the maps held fixed.
 
+#include "scram_inverse.h"
 #include "scram_tile.h"
 
 #include <algorithm>
@@ -29,162 +30,6 @@ namespace {
 // range as contiguous rows.  No float atomics: every gradient row has one
 // writer.
 // ---------------------------------------------------------------------------
-constexpr int kScanItems = 8;                          // counts per thread in the scan
-constexpr int kScanTile = kBlock * kScanItems;         // counts per scan block
-
-struct BwdParams {
-    const void* Q;
-    const void* K;
-    const void* V;
-    const int32_t* J;      // [kappa, n]
-    const void* dO;
-    float* dQ;
-    float* dK;
-    float* dV;
-    float* lse2;           // [n] max + log2(normaliser), base-2 scores
-    float* Dq;             // [n] D_i
-    const int32_t* offsets;  // [S * nkeys + 1] start of each key's entries
-    const int32_t* entries;  // [kappa * n] e * n + i, grouped by match key
-    int32_t* counts;         // [S * nkeys] entries per match key (zeroed before the query kernel)
-    int32_t* slots;          // [kappa * n] each entry's slot among its key's entries
-    int32_t* heavy;          // [S * nkeys] keys left to bwd_heavy_kernel (fp32 strips: to bwd_strip_team_f32_kernel)
-    int32_t* n_heavy;        // their count
-    int heavy_entries;       // fp32 strips: most entries of a strip that one wave sums
-    void* qs;                // [kappa * n, D] q_i of each entry, in entry order
-    void* gs;                // [kappa * n, D] dO_i of each entry, in entry order
-    float2* st;              // [kappa * n] (log2 normaliser, D_i) of each entry
-    uint32_t n;
-    uint32_t keys_total;   // S * nkeys
-    Tiling tq, tk;         // blocks -> tiles of the query grid (query kernel), the key grid (key kernel)
-    int Hq, Wq, Hk, Wk;
-    uint32_t nkeys;
-    Div div_plane, div_wk, div_n, div_keys;
-    int b;
-    float scale;
-    float scale_log2e;
-    int kappa;
-    int causal;
-    int rc;                // cluster radius of the matrix-core query kernel
-};
-
-// a[0 .. count) = 0 and, when given, *word = 0
-__global__ __launch_bounds__(kBlock) void zero_i32_kernel(int32_t* a, size_t count, int32_t* word)
-{
-    for (size_t i = static_cast<size_t>(blockIdx.x) * kBlock + threadIdx.x; i < count;
-         i += static_cast<size_t>(gridDim.x) * kBlock)
-        a[i] = 0;
-    if (word != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *word = 0;
-}
-
-// Exclusive scan of in[0 .. count) by one block, count <= kScanTile, into
-// out (which may be in, in global or shared memory); returns the total to
-// thread kBlock - 1.  wave_tot: kBlock / 64 ints of shared memory.
-__device__ int32_t block_exclusive_scan(const int32_t* in, int32_t* out, size_t count, int32_t* wave_tot)
-{
-    const size_t base = static_cast<size_t>(threadIdx.x) * kScanItems;
-    int32_t v[kScanItems];
-    int32_t run = 0;
-#pragma unroll
-    for (int i = 0; i < kScanItems; ++i) {
-        v[i] = base + i < count ? in[base + i] : 0;
-        const int32_t x = v[i];
-        v[i] = run;  // exclusive within the thread
-        run += x;
-    }
-    // exclusive prefix of the thread totals: within the wave, then across waves
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int32_t incl = run;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-        const int32_t y = __shfl_up(incl, k, 64);
-        if (lane >= k) incl += y;
-    }
-    if (lane == 63) wave_tot[wave] = incl;
-    __syncthreads();
-    int32_t before = incl - run;
-    for (int w = 0; w < wave; ++w) before += wave_tot[w];
-#pragma unroll
-    for (int i = 0; i < kScanItems; ++i)
-        if (base + i < count) out[base + i] = before + v[i];
-    return before + run;
-}
-
-// Exclusive scan, step 1: each block scans a tile of kScanTile counts into
-// out (tile-local prefixes; out may be in) and writes the tile's total to
-// sums[tile].
-__global__ __launch_bounds__(kBlock) void scan_tiles_kernel(const int32_t* in, int32_t* out, int32_t* sums,
-                                                            size_t count)
-{
-    __shared__ int32_t wave_tot[kBlock / 64];
-    const size_t base = static_cast<size_t>(blockIdx.x) * kScanTile;
-    const int32_t tot = block_exclusive_scan(in + base, out + base, count - base < kScanTile ? count - base : kScanTile,
-                                             wave_tot);
-    if (threadIdx.x == kBlock - 1) sums[blockIdx.x] = tot;
-}
-
-// Exclusive scan, step 2 (one block): sums[0..tiles) in place, total in sums[tiles].
-__global__ __launch_bounds__(kBlock) void scan_sums_kernel(int32_t* sums, uint32_t tiles)
-{
-    __shared__ int32_t wave_tot[kBlock / 64];
-    __shared__ int32_t carry_s;
-    if (threadIdx.x == 0) carry_s = 0;
-    __syncthreads();
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (uint32_t c0 = 0; c0 < tiles; c0 += kBlock) {
-        const uint32_t i = c0 + threadIdx.x;
-        const int32_t x = i < tiles ? sums[i] : 0;
-        int32_t incl = x;
-#pragma unroll
-        for (int k = 1; k < 64; k <<= 1) {
-            const int32_t y = __shfl_up(incl, k, 64);
-            if (lane >= k) incl += y;
-        }
-        if (lane == 63) wave_tot[wave] = incl;
-        __syncthreads();
-        int32_t before = carry_s + incl - x;
-        for (int w = 0; w < wave; ++w) before += wave_tot[w];
-        if (i < tiles) sums[i] = before;
-        __syncthreads();  // every thread has read carry_s and wave_tot
-        if (threadIdx.x == kBlock - 1) carry_s = before + x;
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) sums[tiles] = carry_s;
-}
-
-// The inverse map from the scan: key k's entries start at
-// offsets[k] = local[k] + pre[k / kScanTile] (local: tile-local exclusive
-// prefixes of the counts, pre: exclusive prefixes of the tile totals, the
-// grand total in pre[tiles]), and entry x goes to its key's start plus the
-// slot the count recorded for it.  OWN_SCAN (tiles <= kScanTile): sums holds
-// the raw tile totals and every block scans them into shared memory itself;
-// otherwise scan_sums_kernel has turned sums into pre.
-template <bool OWN_SCAN>
-__global__ __launch_bounds__(kBlock) void bwd_fill_kernel(BwdParams p, const int32_t* local, const int32_t* sums,
-                                                          uint32_t tiles, int32_t* offsets, int32_t* entries)
-{
-    __shared__ int32_t s_pre[OWN_SCAN ? kScanTile + 1 : 1];
-    __shared__ int32_t wave_tot[kBlock / 64];
-    const int32_t* pre = sums;
-    if constexpr (OWN_SCAN) {
-        const int32_t tot = block_exclusive_scan(sums, s_pre, tiles, wave_tot);
-        if (threadIdx.x == kBlock - 1) s_pre[tiles] = tot;
-        __syncthreads();
-        pre = s_pre;
-    }
-    const size_t stride = static_cast<size_t>(gridDim.x) * kBlock;
-    const size_t first = static_cast<size_t>(blockIdx.x) * kBlock + threadIdx.x;
-    const size_t total = static_cast<size_t>(p.kappa) * p.n;
-    for (size_t x = first; x < total; x += stride) {
-        const uint32_t g = static_cast<uint32_t>(x % p.n);
-        uint32_t s, rem;
-        divmod(g, p.div_plane, s, rem);
-        const size_t key = static_cast<size_t>(s) * p.nkeys + clamp_index(p.J[x], p.nkeys);
-        entries[local[key] + pre[key / kScanTile] + p.slots[x]] = static_cast<int32_t>(x);
-    }
-    for (size_t k = first; k < p.keys_total; k += stride) offsets[k] = local[k] + pre[k / kScanTile];
-    if (first == 0) offsets[p.keys_total] = pre[tiles];
-}
-
 // W > 0: window side W (odd), visited one window row at a time with its W
 // key and W value rows loaded together (as the forward's window kernel);
 // W = 0: any side, kNb keys at a time in row order.
@@ -450,47 +295,10 @@ __device__ __forceinline__ void key_batch(const BwdParams& p, const int (&x)[kNb
 #define SCRAM_BWD_HEAVY_ENTRIES 64
 #endif
 constexpr int kHeavyEntries = SCRAM_BWD_HEAVY_ENTRIES;
-constexpr int kMaxRows = 8;
 // Lane groups that share one heavy key (half a wave at four lanes per group).
 #ifndef SCRAM_BWD_TEAM
 #define SCRAM_BWD_TEAM 8
-#endif  // neighbourhoods of up to this many rows are walked as one flat list
-
-// The entry ranges of the neighbourhood rows r0..r1 of key j: row i covers
-// entries [lo[i], lo[i] + pre[i+1] - pre[i]); pre[] is the running count.
-struct Neighbourhood {
-    int lo[kMaxRows];
-    int pre[kMaxRows + 1];
-    int total;
-};
-
-__device__ __forceinline__ Neighbourhood load_neighbourhood(const int32_t* off, int Wk, int r0, int r1, int c0, int c1)
-{
-    Neighbourhood nb;
-    nb.pre[0] = 0;
-#pragma unroll
-    for (int i = 0; i < kMaxRows; ++i) {
-        int lo = 0, len = 0;
-        if (r0 + i <= r1) {
-            lo = off[(r0 + i) * Wk + c0];
-            len = off[(r0 + i) * Wk + c1 + 1] - lo;
-        }
-        nb.lo[i] = lo;
-        nb.pre[i + 1] = nb.pre[i] + len;
-    }
-    nb.total = nb.pre[kMaxRows];
-    return nb;
-}
-
-// Entry slot of flat position v (0 <= v < total): the last row with pre <= v.
-__device__ __forceinline__ int flat_slot(const Neighbourhood& nb, int v)
-{
-    int x = nb.lo[0] + v;
-#pragma unroll
-    for (int i = 1; i < kMaxRows; ++i)
-        if (v >= nb.pre[i]) x = nb.lo[i] + (v - nb.pre[i]);
-    return x;
-}
+#endif
 
 // Accumulate the entries of key j's neighbourhood taken by member `member`
 // of a team of `team` lane groups (positions member, member + team, ...).
@@ -549,23 +357,6 @@ __device__ __forceinline__ void store_key_grads(const BwdParams& p, uint32_t kg,
             ov[i] = make_float4(dv[e0], dv[e0 + 1], dv[e0 + 2], dv[e0 + 3]);
         }
     }
-}
-
-struct KeyPos {
-    uint32_t s, j, ju, jv;
-    int r0, r1, c0, c1;
-};
-
-__device__ __forceinline__ KeyPos key_pos(const BwdParams& p, uint32_t kg)
-{
-    KeyPos k;
-    divmod(kg, p.div_keys, k.s, k.j);
-    divmod(k.j, p.div_wk, k.ju, k.jv);
-    k.r0 = max(static_cast<int>(k.ju) - p.b, 0);
-    k.r1 = min(static_cast<int>(k.ju) + p.b, p.Hk - 1);
-    k.c0 = max(static_cast<int>(k.jv) - p.b, 0);
-    k.c1 = min(static_cast<int>(k.jv) + p.b, p.Wk - 1);
-    return k;
 }
 
 // One lane group per key j: sum over the entries (i, e) whose match e lies
@@ -2157,33 +1948,14 @@ hipError_t launch_attend_backward(int dtype, const void* Q, const void* K, const
     p.offsets = offsets;
     p.entries = entries;
 
-    auto grid_for = [](size_t items) {
-        const size_t b = (items + kBlock - 1) / kBlock;
-        return static_cast<uint32_t>(b < 1 ? 1 : (b > 4096 ? 4096 : b));
-    };
     hipEvent_t e0 = events ? events[0] : nullptr, e1 = events ? events[1] : nullptr;
     hipEvent_t q0 = events ? events[2] : nullptr;
-    const size_t entries_total = static_cast<size_t>(p.n) * kappa;
     hipError_t e;
     // inverse map: a counting sort of the (query, match) entries by match key.
     // The counts (and the heavy-key counter) start at zero; the query kernel
     // counts; the scan and the fill follow it.
-    if ((e = launch(zero_i32_kernel, grid_for(N), stream, q0, nullptr, counts, N, p.n_heavy)) != hipSuccess) return e;
-    auto inverse = [&]() -> hipError_t {
-        hipError_t r;
-        if ((r = launch(scan_tiles_kernel, tiles, stream, e0, nullptr, static_cast<const int32_t*>(counts), counts,
-                        sums, N)) != hipSuccess)
-            return r;
-        const uint32_t fill_blocks = grid_for(entries_total > N ? entries_total : N + 1);
-        if (tiles <= static_cast<uint32_t>(kScanTile))
-            return launch(bwd_fill_kernel<true>, fill_blocks, stream, nullptr, e1, p,
-                          static_cast<const int32_t*>(counts), static_cast<const int32_t*>(sums), tiles, offsets,
-                          entries);
-        if ((r = launch(scan_sums_kernel, 1u, stream, nullptr, nullptr, sums, tiles)) != hipSuccess) return r;
-        return launch(bwd_fill_kernel<false>, fill_blocks, stream, nullptr, e1, p,
-                      static_cast<const int32_t*>(counts), static_cast<const int32_t*>(sums), tiles, offsets,
-                      entries);
-    };
+    if ((e = launch(zero_i32_kernel, stride_blocks(N), stream, q0, nullptr, counts, N, p.n_heavy)) != hipSuccess) return e;
+    auto inverse = [&]() { return run_inverse(p, counts, offsets, sums, entries, stream, e0, e1); };
     // gradients
     return dispatch(dtype, g.d, [&](auto ty, auto d) {
         return run_backward<decltype(ty), decltype(d)::value>(p, stream, events, inverse);

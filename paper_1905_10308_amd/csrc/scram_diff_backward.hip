@@ -1,0 +1,423 @@
+// Gradients of the differential attention over the match windows (maps held
+// fixed).  With dp_ij = dO_i.v_j and D1_i = sum_j p1_ij dp_ij, D2_i likewise:
+//   dQ1_i =       scale sum_j p1_ij (dp_ij - D1_i) k1_j
+//   dQ2_i = - lam scale sum_j p2_ij (dp_ij - D2_i) k2_j
+//   dK1_j =       scale sum_i p1_ij (dp_ij - D1_i) q1_i,  dK2_j likewise with - lam
+//   dV_j  = sum_i (p1_ij - lam p2_ij) dO_i
+//   dlam  = - sum_i D2_i over the slice's queries
+// The query side walks each query's key set once, as the attend's gradients
+// do; the key side gathers over the queries whose windows hold the key,
+// through the inverse of the maps (scram_inverse.h).  No float atomics: every
+// gradient row has one writer.
+
+#include "scram_diff.h"
+#include "scram_inverse.h"
+
+#include <algorithm>
+
+namespace scram {
+namespace {
+
+// Sum of x over the block's threads (kBlock), in a fixed order, on thread 0.
+__device__ double block_sum(double x)
+{
+    __shared__ double s_wave[kBlock / 64];
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
+    if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = x;
+    __syncthreads();
+    double t = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < kBlock / 64; ++w) t += s_wave[w];
+    return t;
+}
+
+// A lane group per query.  As in the attend's gradients the keys enter as
+// k_j - k_ref, k_ref the key at the first match: the weights of a set sum to
+// one, so dQ = scale (A - D B) / l for any fixed k_ref, and A - D B does not
+// cancel where neighbouring keys are alike.
+template <typename T, int D, int G, int MK>
+__global__ __launch_bounds__(kBlock) void diff_query_kernel(DiffParams p)
+{
+    constexpr bool MULTI = MK > 0;
+    using RW = Row<T, D, G>;
+    static_assert(RW::kCh == 2, "two chunks per lane: one of each half");
+    constexpr int H = RW::kEpc;  // channels per lane of each half
+    constexpr int kNb = 2;
+    const int lane = threadIdx.x & (G - 1);
+    const uint32_t blk = xcd_remap(blockIdx.x, gridDim.x);
+    uint32_t g;
+    const bool valid = tile_item<RW::kQpb>(p.tq, blk, threadIdx.x / G, g);
+    float D2 = 0.f;
+    if (valid) {
+        uint32_t s, rem;
+        divmod(g, p.div_plane, s, rem);
+        // the inverse map's count: one entry per match of this query, and its slot among that match key's
+        if (lane == 0) {
+            for (int e = 0; e < (MULTI ? p.kappa : 1); ++e) {
+                const size_t x = static_cast<size_t>(e) * p.n + g;
+                p.slots[x] = atomicAdd(p.counts + static_cast<size_t>(s) * p.nkeys + clamp_index(p.J[x], p.nkeys), 1);
+            }
+        }
+        const size_t slice = static_cast<size_t>(s) * p.nkeys * D;
+        const T* Ks = static_cast<const T*>(p.K) + slice;
+        const T* Vs = static_cast<const T*>(p.V) + slice;
+        uint4 q[2], go[2];
+        load_row<T, D, G>(static_cast<const T*>(p.Q), g, lane, q);
+        load_row<T, D, G>(static_cast<const T*>(p.dO), g, lane, go);
+        WindowSet<(MK > 0 ? MK : 1)> ws;
+        if constexpr (MULTI) {
+            ws = make_window_set<MK>(p, g, rem);
+            ws.local = causal_limit(p, s, rem);
+        }
+        float kref[2 * H];
+        {
+            uint4 kr0[2];
+            load_row<T, D, G>(Ks, clamp_index(p.J[g], p.nkeys), lane, kr0);
+            unpack_row<T, 2>(kr0, kref);
+        }
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, dn[2] = {0.f, 0.f};
+        float A[2][H], B[2][H];
+#pragma unroll
+        for (int i = 0; i < H; ++i) A[0][i] = A[1][i] = B[0][i] = B[1][i] = 0.f;
+        for (int e = 0; e < (MULTI ? p.kappa : 1); ++e) {
+            uint32_t u, v;
+            if constexpr (MULTI)
+                ws.centre(e, u, v);
+            else
+                divmod(static_cast<uint32_t>(clamp_index(p.J[g], p.nkeys)), p.div_wk, u, v);
+            walk_window<T, D, G, kNb, MK>(p, Ks, Vs, ws, e, u, v, 0, 1, lane, [&](const auto& ok, const auto& kr, const auto& vr) {
+                float sc[2][kNb], dp[kNb];
+#pragma unroll
+                for (int j = 0; j < kNb; ++j) dp[j] = row_score<T, D, G>(go, vr[j]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float mb = m[h];
+#pragma unroll
+                    for (int j = 0; j < kNb; ++j) {
+                        sc[h][j] = half_score<T, G>(q[h], kr[j][h]) * p.scale_log2e;
+                        mb = ok[j] ? fmaxf(mb, sc[h][j]) : mb;
+                    }
+                    if (mb > m[h] + kRescaleSlack) {
+                        const float alpha = __builtin_amdgcn_exp2f(m[h] - mb);
+                        l[h] *= alpha;
+                        dn[h] *= alpha;
+#pragma unroll
+                        for (int i = 0; i < H; ++i) A[h][i] *= alpha, B[h][i] *= alpha;
+                        m[h] = mb;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kNb; ++j) {
+                    if (!ok[j]) continue;
+                    float kf[2 * H];
+                    unpack_row<T, 2>(kr[j], kf);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float pj = __builtin_amdgcn_exp2f(sc[h][j] - (m[h] == -INFINITY ? 0.f : m[h]));
+                        const float pd = pj * dp[j];
+                        l[h] += pj;
+                        dn[h] += pd;
+#pragma unroll
+                        for (int i = 0; i < H; ++i) {
+                            const float kd = kf[h * H + i] - kref[h * H + i];
+                            A[h][i] = fmaf(pd, kd, A[h][i]);
+                            B[h][i] = fmaf(pj, kd, B[h][i]);
+                        }
+                    }
+                }
+            });
+        }
+        float Dh[2], lse[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float inv = l[h] != 0.f ? 1.f / l[h] : 0.f;
+            Dh[h] = dn[h] * inv;
+            lse[h] = l[h] != 0.f ? m[h] + log2f(l[h]) : INFINITY;  // +inf: every weight is 0
+            const float f = (h == 0 ? p.scale : -p.lam[s] * p.scale) * inv;
+            float4* o = reinterpret_cast<float4*>(p.dQ + static_cast<size_t>(g) * D + (h * G + lane) * H);
+#pragma unroll
+            for (int i = 0; i < H / 4; ++i)
+                o[i] = make_float4((A[h][4 * i] - Dh[h] * B[h][4 * i]) * f, (A[h][4 * i + 1] - Dh[h] * B[h][4 * i + 1]) * f,
+                                   (A[h][4 * i + 2] - Dh[h] * B[h][4 * i + 2]) * f, (A[h][4 * i + 3] - Dh[h] * B[h][4 * i + 3]) * f);
+        }
+        if (lane == 0) {
+            p.stats[g] = make_float4(lse[0], Dh[0], lse[1], Dh[1]);
+            D2 = Dh[1];
+        }
+    }
+    const double part = block_sum(D2);
+    if (threadIdx.x == 0) p.lam_part[blk] = part;
+}
+
+// dlam of a slice: minus the sum of its query blocks' parts.  One block per slice.
+__global__ __launch_bounds__(kBlock) void diff_lam_kernel(const double* part, uint32_t blocks, float* dlam)
+{
+    const double* const mine = part + static_cast<size_t>(blockIdx.x) * blocks;
+    double x = 0.0;
+    for (uint32_t i = threadIdx.x; i < blocks; i += kBlock) x += mine[i];
+    x = block_sum(x);
+    if (threadIdx.x == 0) dlam[blockIdx.x] = static_cast<float>(-x);
+}
+
+// Contributions of kNb entries (slots x[t], valid where ok[t]) to dK_j, dV_j
+// (unscaled dK) for key j at (ju, jv): each query once -- through its first
+// window holding j -- and, with the causal mask, only if j is not after it.
+template <typename T, int D, int G, bool MULTI, int kNb>
+__device__ __forceinline__ void diff_key_batch(const DiffParams& p, const int (&x)[kNb], const bool (&valid)[kNb], float lam,
+                                               const KeyPos& k, int lane, const uint4 (&kj)[2], const uint4 (&vj)[2], float* dk,
+                                               float* dv)
+{
+    constexpr int H = Row<T, D, G>::kEpc;
+    uint4 qr[kNb][2], gr[kNb][2];
+    float4 st[kNb];
+    uint32_t e[kNb], g[kNb];
+#pragma unroll
+    for (int t = 0; t < kNb; ++t) divmod(static_cast<uint32_t>(p.entries[x[t]]), p.div_n, e[t], g[t]);
+#pragma unroll
+    for (int t = 0; t < kNb; ++t) {
+        st[t] = p.stats[g[t]];
+        load_row<T, D, G>(static_cast<const T*>(p.Q), g[t], lane, qr[t]);
+        load_row<T, D, G>(static_cast<const T*>(p.dO), g[t], lane, gr[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < kNb; ++t) {
+        bool ok = valid[t];
+        if constexpr (MULTI) {
+            for (int f = 0; f < static_cast<int>(e[t]) && ok; ++f) {
+                uint32_t fu, fv;
+                divmod(static_cast<uint32_t>(clamp_index(p.J[static_cast<size_t>(f) * p.n + g[t]], p.nkeys)), p.div_wk, fu, fv);
+                ok = abs(static_cast<int>(fu) - static_cast<int>(k.ju)) > p.b || abs(static_cast<int>(fv) - static_cast<int>(k.jv)) > p.b;
+            }
+            if (ok && p.causal) {
+                uint32_t gs, rem;
+                divmod(g[t], p.div_plane, gs, rem);
+                ok = k.j <= causal_limit(p, gs, rem);
+            }
+        }
+        if (!ok) continue;
+        const float dp = row_score<T, D, G>(gr[t], vj);
+        const float p1 = __builtin_amdgcn_exp2f(half_score<T, G>(qr[t][0], kj[0]) * p.scale_log2e - st[t].x);
+        const float p2 = lam * __builtin_amdgcn_exp2f(half_score<T, G>(qr[t][1], kj[1]) * p.scale_log2e - st[t].z);
+        const float ds[2] = {p1 * (dp - st[t].y), -p2 * (dp - st[t].w)};
+        const float w = p1 - p2;
+        float qf[2 * H], gf[2 * H];
+        unpack_row<T, 2>(qr[t], qf);
+        unpack_row<T, 2>(gr[t], gf);
+#pragma unroll
+        for (int i = 0; i < 2 * H; ++i) {
+            dk[i] = fmaf(ds[i / H], qf[i], dk[i]);
+            dv[i] = fmaf(w, gf[i], dv[i]);
+        }
+    }
+}
+
+// The entries of key k's neighbourhood taken by member `member` of a team of
+// `team` lane groups.
+template <typename T, int D, int G, bool MULTI>
+__device__ __forceinline__ void diff_key_sums(const DiffParams& p, const KeyPos& k, int member, int team, int lane,
+                                              const uint4 (&kj)[2], const uint4 (&vj)[2], float* dk, float* dv)
+{
+    constexpr int kNb = 2;
+    const int32_t* off = p.offsets + static_cast<size_t>(k.s) * p.nkeys;
+    const float lam = p.lam[k.s];
+    if (k.r1 - k.r0 + 1 <= kMaxRows) {
+        const Neighbourhood nb = load_neighbourhood(off, p.Wk, k.r0, k.r1, k.c0, k.c1);
+        for (int v0 = member; v0 < nb.total; v0 += kNb * team) {
+            int x[kNb];
+            bool valid[kNb];
+#pragma unroll
+            for (int t = 0; t < kNb; ++t) {
+                valid[t] = v0 + t * team < nb.total;
+                x[t] = flat_slot(nb, min(v0 + t * team, nb.total - 1));
+            }
+            diff_key_batch<T, D, G, MULTI, kNb>(p, x, valid, lam, k, lane, kj, vj, dk, dv);
+        }
+    } else {
+        for (int r = k.r0; r <= k.r1; ++r) {
+            const int lo = off[r * p.Wk + k.c0], hi = off[r * p.Wk + k.c1 + 1];
+            for (int x0 = lo + member; x0 < hi; x0 += kNb * team) {
+                int x[kNb];
+                bool valid[kNb];
+#pragma unroll
+                for (int t = 0; t < kNb; ++t) {
+                    valid[t] = x0 + t * team < hi;
+                    x[t] = min(x0 + t * team, hi - 1);
+                }
+                diff_key_batch<T, D, G, MULTI, kNb>(p, x, valid, lam, k, lane, kj, vj, dk, dv);
+            }
+        }
+    }
+}
+
+// dK_j (times scale) and dV_j from the lane's channels.
+template <typename T, int D, int G>
+__device__ __forceinline__ void diff_store_key(const DiffParams& p, uint32_t kg, int lane, const float* dk, const float* dv)
+{
+    constexpr int H = Row<T, D, G>::kEpc;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float4* ok = reinterpret_cast<float4*>(p.dK + static_cast<size_t>(kg) * D + (h * G + lane) * H);
+        float4* ov = reinterpret_cast<float4*>(p.dV + static_cast<size_t>(kg) * D + (h * G + lane) * H);
+#pragma unroll
+        for (int i = 0; i < H / 4; ++i) {
+            const float *a = dk + h * H + 4 * i, *b = dv + h * H + 4 * i;
+            ok[i] = make_float4(a[0] * p.scale, a[1] * p.scale, a[2] * p.scale, a[3] * p.scale);
+            ov[i] = make_float4(b[0], b[1], b[2], b[3]);
+        }
+    }
+}
+
+// A key with more entries than this goes to the list of the kernel below.
+constexpr int kDiffHeavy = 64;
+
+// A lane group per key.
+template <typename T, int D, int G, bool MULTI>
+__global__ __launch_bounds__(kBlock) void diff_key_kernel(DiffParams p)
+{
+    using RW = Row<T, D, G>;
+    const int lane = threadIdx.x & (G - 1);
+    uint32_t kg;
+    if (!tile_item<RW::kQpb>(p.tk, xcd_remap(blockIdx.x, gridDim.x), threadIdx.x / G, kg)) return;
+    const KeyPos k = key_pos(p, kg);
+    const int32_t* off = p.offsets + static_cast<size_t>(k.s) * p.nkeys;
+    int total = 0;
+    for (int r = k.r0; r <= k.r1; ++r) total += off[r * p.Wk + k.c1 + 1] - off[r * p.Wk + k.c0];
+    if (total > kDiffHeavy) {
+        if (lane == 0) p.heavy[atomicAdd(p.n_heavy, 1)] = static_cast<int32_t>(kg);
+        return;
+    }
+    uint4 kj[2], vj[2];
+    load_row<T, D, G>(static_cast<const T*>(p.K), kg, lane, kj);
+    load_row<T, D, G>(static_cast<const T*>(p.V), kg, lane, vj);
+    float dk[2 * RW::kEpc], dv[2 * RW::kEpc];
+#pragma unroll
+    for (int i = 0; i < 2 * RW::kEpc; ++i) dk[i] = dv[i] = 0.f;
+    diff_key_sums<T, D, G, MULTI>(p, k, 0, 1, lane, kj, vj, dk, dv);
+    diff_store_key<T, D, G>(p, kg, lane, dk, dv);
+}
+
+// The keys of the list, a wave each: its lane groups take the entries in turn
+// and their sums are added up.
+template <typename T, int D, int G, bool MULTI>
+__global__ __launch_bounds__(kBlock) void diff_heavy_kernel(DiffParams p)
+{
+    constexpr int N = 2 * Row<T, D, G>::kEpc;
+    const int lane = threadIdx.x & (G - 1), member = (threadIdx.x & 63) / G;
+    const int count = *p.n_heavy;
+    for (int h = blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6); h < count; h += gridDim.x * (kBlock / 64)) {
+        const uint32_t kg = static_cast<uint32_t>(p.heavy[h]);
+        const KeyPos k = key_pos(p, kg);
+        uint4 kj[2], vj[2];
+        load_row<T, D, G>(static_cast<const T*>(p.K), kg, lane, kj);
+        load_row<T, D, G>(static_cast<const T*>(p.V), kg, lane, vj);
+        float dk[N], dv[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) dk[i] = dv[i] = 0.f;
+        diff_key_sums<T, D, G, MULTI>(p, k, member, 64 / G, lane, kj, vj, dk, dv);
+#pragma unroll
+        for (int mask = G; mask < 64; mask <<= 1)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                dk[i] += __shfl_xor(dk[i], mask);
+                dv[i] += __shfl_xor(dv[i], mask);
+            }
+        if (member == 0) diff_store_key<T, D, G>(p, kg, lane, dk, dv);
+    }
+}
+
+size_t r256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
+
+// Query blocks: a lane group of one lane at least per query.
+uint64_t query_blocks_most(const Grid& g)
+{
+    uint64_t most = 0;
+    for (uint32_t items = kBlock; items >= kBlock / 16; items /= 2)
+        most = std::max(most, tiling_blocks(make_tiling(g.Hq, g.Wq, items, kLaneSkew), g.S));
+    return most;
+}
+
+template <typename T, int D, bool MULTI>
+hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* offsets, int32_t* sums, int32_t* entries,
+                             hipStream_t st, hipEvent_t start, hipEvent_t stop)
+{
+    constexpr int G = kDiffLanes<T, D>;
+    constexpr uint32_t kQpb = Row<T, D, G>::kQpb;
+    DiffParams p = p0;
+    p.tq = make_tiling(p.Hq, p.Wq, kQpb, kLaneSkew);
+    p.tk = make_tiling(p.Hk, p.Wk, kQpb, kLaneSkew);
+    const uint32_t S = p.n / p.tq.plane;
+    const uint64_t qblocks = tiling_blocks(p.tq, S), kblocks = tiling_blocks(p.tk, S);
+    const size_t N = p.keys_total;
+    hipError_t e;
+    if ((e = launch(zero_i32_kernel, stride_blocks(N), st, start, nullptr, counts, N, p.n_heavy)) != hipSuccess) return e;
+    if constexpr (!MULTI)
+        e = launch(diff_query_kernel<T, D, G, 0>, qblocks, st, nullptr, nullptr, p);
+    else
+        e = p.kappa <= 2 ? launch(diff_query_kernel<T, D, G, 2>, qblocks, st, nullptr, nullptr, p)
+                         : launch(diff_query_kernel<T, D, G, kMaxKappa>, qblocks, st, nullptr, nullptr, p);
+    if (e != hipSuccess) return e;
+    if ((e = run_inverse(p, counts, offsets, sums, entries, st, nullptr, nullptr)) != hipSuccess) return e;
+    if ((e = launch(diff_lam_kernel, S, st, nullptr, nullptr, static_cast<const double*>(p.lam_part), p.tq.div_slice.d, p.dlam)) != hipSuccess)
+        return e;
+    if ((e = launch(diff_key_kernel<T, D, G, MULTI>, kblocks, st, nullptr, nullptr, p)) != hipSuccess) return e;
+    return launch(diff_heavy_kernel<T, D, G, MULTI>, 1024, st, nullptr, stop, p);  // loops over however many there are
+}
+
+}  // namespace
+
+size_t diff_backward_workspace_bytes(const Grid& g, int kappa)
+{
+    const size_t n = static_cast<size_t>(g.S) * g.Hq * g.Wq, N = static_cast<size_t>(g.S) * g.Hk * g.Wk;
+    const size_t tiles = (N + kScanTile - 1) / kScanTile;
+    return r256(4 * N) + r256(4 * (N + 1)) + r256(4 * (tiles + 1)) + 2 * r256(4 * n * kappa) + r256(16 * n) +
+           r256(4 * (N + 1)) + r256(8 * query_blocks_most(g));
+}
+
+hipError_t launch_diff_backward(int dtype, const DiffCall& c, const void* dO, float* dQ, float* dK, float* dV, float* dlam,
+                                void* workspace, hipStream_t stream, hipEvent_t start, hipEvent_t stop)
+{
+    DiffParams p{};
+    fill_diff_params(p, c);
+    p.dO = dO;
+    p.dQ = dQ;
+    p.dK = dK;
+    p.dV = dV;
+    p.dlam = dlam;
+    // workspace: counts, offsets, tile sums, entries, slots, statistics, heavy keys, parts of dlam
+    const size_t N = p.keys_total, total = static_cast<size_t>(p.n) * c.kappa;
+    char* w = static_cast<char*>(workspace);
+    auto take = [&](size_t bytes) {
+        char* at = w;
+        w += r256(bytes);
+        return at;
+    };
+    int32_t* counts = reinterpret_cast<int32_t*>(take(4 * N));
+    int32_t* offsets = reinterpret_cast<int32_t*>(take(4 * (N + 1)));
+    int32_t* sums = reinterpret_cast<int32_t*>(take(4 * ((N + kScanTile - 1) / kScanTile + 1)));
+    int32_t* entries = reinterpret_cast<int32_t*>(take(4 * total));
+    p.slots = reinterpret_cast<int32_t*>(take(4 * total));
+    p.stats = reinterpret_cast<float4*>(take(16 * static_cast<size_t>(p.n)));
+    p.n_heavy = reinterpret_cast<int32_t*>(take(4 * (N + 1)));  // counter, then the list
+    p.heavy = p.n_heavy + 1;
+    p.lam_part = reinterpret_cast<double*>(w);
+    p.counts = counts;
+    p.offsets = offsets;
+    p.entries = entries;
+    return dispatch(dtype, c.g.d, [&](auto ty, auto d) {
+        using T = decltype(ty);
+        constexpr int D = decltype(d)::value;
+        return p.kappa == 1 && !p.causal ? run_diff_backward<T, D, false>(p, counts, offsets, sums, entries, stream, start, stop)
+                                         : run_diff_backward<T, D, true>(p, counts, offsets, sums, entries, stream, start, stop);
+    });
+}
+
+uint64_t diff_backward_max_blocks(const Grid& g)
+{
+    uint64_t most = std::max<uint64_t>(4096, query_blocks_most(g));  // (4096: the grid-stride kernels of the inverse map)
+    for (uint32_t items = kBlock; items >= kBlock / 16; items /= 2)
+        most = std::max(most, tiling_blocks(make_tiling(g.Hk, g.Wk, items, kLaneSkew), g.S));
+    return most;
+}
+
+}  // namespace scram

@@ -1,6 +1,7 @@
 // Internal interface between the C-ABI front end (scram_api.cpp) and the
 // kernels (scram_pm.hip, scram_attend.hip, scram_backward.hip,
-// scram_snis.hip).  Arguments reaching these functions have been
+// scram_snis.hip, scram_diff.hip, scram_diff_backward.hip, scram_rotary.hip,
+// scram_norm.hip).  Arguments reaching these functions have been
 // validated by the front end.
 #pragma once
 
@@ -65,6 +66,55 @@ hipError_t launch_attend_backward(int dtype, const void* Q, const void* K, const
                                   const Grid& g, int window, float scale, bool causal, const void* dO, float* dQ,
                                   float* dK, float* dV, void* workspace, hipStream_t stream, hipEvent_t* events);
 
+// Differential attention around the kappa maps in J and its gradients.
+struct DiffCall {
+    const void *Q, *K, *V;
+    const int32_t* J;
+    int kappa;
+    const float* lam;       // [S]
+    Grid g;
+    int window;
+    float scale;
+    bool causal;
+    int first;              // causal: raster index of a slice's first query among its keys
+    const int32_t* origin;  // causal: the same per slice, on the device (null: first)
+};
+hipError_t launch_diff_attend(int dtype, const DiffCall& c, void* out, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
+size_t diff_backward_workspace_bytes(const Grid& g, int kappa);
+hipError_t launch_diff_backward(int dtype, const DiffCall& c, const void* dO, float* dQ, float* dK, float* dV, float* dlam,
+                                void* workspace, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
+
+// Rotation of channel pairs by the position's angles (scram_rotary).
+struct RotaryCall {
+    int count;
+    const void* src[4];
+    void* dst[4];
+    int slices[4];
+    int T, H, W, d, groups;
+    int pairs[3];           // of time, height, width
+    const double* freq;     // radians per step of each pair
+    const int32_t* origin;  // device [origin_rows, 3] (null: first)
+    int origin_rows;
+    int first[3];
+    bool interleaved, inverse;
+};
+uint64_t rotary_items(int dtype, const RotaryCall& c);
+hipError_t launch_rotary(int dtype, const RotaryCall& c, hipStream_t stream);
+
+// Layer norm of rows.
+struct NormCall {
+    int64_t rows;
+    int channels;
+    int dtype, grad_dtype, weight_dtype;
+    const void *X, *weight, *bias, *dY;  // weight, bias nullable
+    float eps;
+};
+constexpr int kNormMaxChannels = 16384;
+hipError_t launch_norm(const NormCall& c, void* Y, float* mean, float* rstd, hipStream_t stream);
+size_t norm_backward_workspace_bytes(int64_t rows, int channels);
+hipError_t launch_norm_backward(const NormCall& c, const float* mean, const float* rstd, void* dX, float* dweight,
+                                float* dbias, void* workspace, hipStream_t stream);
+
 // Self-normalised importance sampling around the kappa maps in modes
 // ([kappa, n]): samples per query, mixture weight, binomial radius m,
 // softmax scale and Philox seed.
@@ -96,5 +146,7 @@ uint64_t patchmatch_max_blocks(int dtype, const Grid& g);
 uint64_t attend_max_blocks(int dtype, const Grid& g);
 uint64_t snis_max_blocks(int dtype, const Grid& g);
 uint64_t attend_backward_max_blocks(int dtype, const Grid& g, int kappa);
+uint64_t diff_attend_max_blocks(int dtype, const Grid& g);
+uint64_t diff_backward_max_blocks(const Grid& g);
 
 }  // namespace scram
