@@ -38,9 +38,10 @@ COMPILE_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
 LINK_FLAGS = [f"--offload-arch={ARCH}", "-shared", "-fPIC"]
-# per-source additions: the attend step's matrix-core kernel keeps its accumulators in VGPRs (the
+# per-source additions: the attends' matrix-core kernels keep their accumulators in VGPRs (the
 # compiler would otherwise copy them between AGPRs and VGPRs around every rescale)
-EXTRA_FLAGS = {"scram_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+_VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+EXTRA_FLAGS = {"scram_attend.hip": _VGPR_FORM, "scram_diff.hip": _VGPR_FORM}
 
 
 def hipcc() -> str:

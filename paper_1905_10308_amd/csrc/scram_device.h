@@ -521,6 +521,19 @@ hipError_t launch(void (*kernel)(A...), uint64_t blocks, hipStream_t st, hipEven
     return hipGetLastError();
 }
 
+// launch() for kernels of another block size: one wave, by default
+template <uint32_t kThreads = 64, typename P>
+hipError_t launch_wave(void (*kernel)(P), uint64_t blocks, hipStream_t st, hipEvent_t start, hipEvent_t stop,
+                       const P& p)
+{
+    if (blocks == 0 || blocks > 0xFFFFFFFFull / kThreads) return hipErrorInvalidConfiguration;
+    if (start || stop)
+        hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, st, start, stop, 0, p);
+    else
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, st, p);
+    return hipGetLastError();
+}
+
 // (dtype, d) -> instantiation; `none` for an unsupported pair
 template <typename R, typename F>
 R dispatch_value(int dtype, int d, R none, F&& f)

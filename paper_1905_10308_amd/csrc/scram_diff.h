@@ -23,6 +23,7 @@ struct DiffParams : BwdParams {
     const float* lam;      // [S]
     const int32_t* origin; // [S] raster index of each slice's first query among the keys (null: first)
     int first;
+    int tile_blocks;       // most blocks of 16 keys a wave walks on the matrix cores
     float4* stats;         // [n] log2 normaliser and D of both maps (gradients)
     double* lam_part;      // [query blocks] their queries' sum of D of the second map
     float* dlam;           // [S]

@@ -1,32 +1,21 @@
 // Differential attention over the match windows: forward.
 
-#include "scram_diff.h"
+#include "scram_diff_tile.h"
 
 namespace scram {
 namespace {
 
-// A lane group per query (WAVE: the lane groups of a wave share one query and
-// add up at the end, for calls of a few queries).  One walk over the key set
-// keeps two online softmaxes (base-2 domain) and their sums of values.  A key
-// that is left out is not accumulated at all: whatever its rows hold stays out.
+// Query g on a lane group, or on TEAM lane groups that share its keys and add up at the end (all lanes of the team call).
+// One walk over the key set keeps two online softmaxes (base-2 domain) and their sums of values.  A key that is left out is
+// not accumulated at all: whatever its rows hold stays out.
 // MK = 0: one window, no mask; else up to MK windows and/or the causal mask.
-template <typename T, int D, int G, int MK, bool WAVE>
-__global__ __launch_bounds__(WAVE ? 64 : kBlock) void diff_attend_kernel(DiffParams p)
+template <typename T, int D, int G, int MK, int kNb, int TEAM>
+__device__ __forceinline__ void diff_query(const DiffParams& p, uint32_t g, int lane, int member)
 {
     constexpr bool MULTI = MK > 0;
     using RW = Row<T, D, G>;
     static_assert(RW::kCh == 2, "two chunks per lane: one of each half");
     constexpr int E = 2 * RW::kEpc;
-    constexpr int kNb = 4;
-    constexpr int kTeam = WAVE ? 64 / G : 1;
-    const int lane = threadIdx.x & (G - 1);
-    const int member = WAVE ? threadIdx.x / G : 0;
-    uint32_t g;
-    if constexpr (WAVE) {
-        g = blockIdx.x;
-    } else {
-        if (!tile_item<RW::kQpb>(p.tq, xcd_remap(blockIdx.x, gridDim.x), threadIdx.x / G, g)) return;
-    }
     uint32_t s, rem;
     divmod(g, p.div_plane, s, rem);
     const size_t slice = static_cast<size_t>(s) * p.nkeys * D;
@@ -50,7 +39,7 @@ __global__ __launch_bounds__(WAVE ? 64 : kBlock) void diff_attend_kernel(DiffPar
             ws.centre(e, u, v);
         else
             divmod(static_cast<uint32_t>(clamp_index(p.J[g], p.nkeys)), p.div_wk, u, v);
-        walk_window<T, D, G, kNb, MK>(p, Ks, Vs, ws, e, u, v, member, kTeam, lane, [&](const auto& ok, const auto& kr, const auto& vr) {
+        walk_window<T, D, G, kNb, MK>(p, Ks, Vs, ws, e, u, v, member, TEAM, lane, [&](const auto& ok, const auto& kr, const auto& vr) {
             float sc[2][kNb];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -81,9 +70,9 @@ __global__ __launch_bounds__(WAVE ? 64 : kBlock) void diff_attend_kernel(DiffPar
             }
         });
     }
-    if constexpr (WAVE) {
+    if constexpr (TEAM > 1) {
 #pragma unroll
-        for (int mask = G; mask < 64; mask <<= 1) {
+        for (int mask = G; mask < TEAM * G; mask <<= 1) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float mo = __shfl_xor(m[h], mask), top = fmaxf(m[h], mo);
@@ -105,6 +94,145 @@ __global__ __launch_bounds__(WAVE ? 64 : kBlock) void diff_attend_kernel(DiffPar
     store_row<T, D, G>(p.out, g, lane, o, 1.f);
 }
 
+// A lane group per query (WAVE: a wave per query, for calls of a few queries).
+template <typename T, int D, int G, int MK, bool WAVE>
+__global__ __launch_bounds__(WAVE ? 64 : kBlock) void diff_attend_kernel(DiffParams p)
+{
+    const int lane = threadIdx.x & (G - 1);
+    if constexpr (WAVE) {
+        diff_query<T, D, G, MK, 4, 64 / G>(p, blockIdx.x, lane, threadIdx.x / G);
+    } else {
+        uint32_t g;
+        if (tile_item<Row<T, D, G>::kQpb>(p.tq, xcd_remap(blockIdx.x, gridDim.x), threadIdx.x / G, g))
+            diff_query<T, D, G, MK, 4, 1>(p, g, lane, 0);
+    }
+}
+
+// Waves per SIMD that the tile kernel's registers are sized for.
+constexpr int diff_tile_waves(int D, int MK) { return D == 128 ? 2 : MK == 4 ? 3 : 4; }
+
+// On the matrix cores (scram_diff_tile.h), bf16.  Per block of 16 keys
+//   S1^T, S2^T = K_blk Q^T       keys x queries, of each half of the channels
+//   P1, P2 = 2^(S scale log2 e - reference) on the query's keys, 0 elsewhere
+//   O1^T += V_blk^T P1^T, O2^T += V_blk^T P2^T
+// with the weights as two bf16 parts (18 bits: the output keeps 8), and at the end o = O1 / l1 - lam O2 / l2.  A query whose sums are
+// not finite (an infinite value of the box reaches every query of its cluster through 0 * inf, a score that is not a number
+// passes its mask), or whose set is empty, is computed over again on a lane group, and so are a wave's queries whose matches lie too far apart to share rows.
+template <int D, int W, bool CAUSAL, int MK>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(diff_tile_waves(D, MK)))) void
+diff_tile_kernel(DiffParams p)
+{
+    using TR = TileRow<D>;
+    constexpr int kOt = D / 16, kRowB = 2 * D + kRowPad;
+    constexpr int G = kDiffLanes<uint16_t, D>;
+    __shared__ __align__(16) unsigned char tk[16 * kRowB], tv[16 * kRowB];
+    const int lane = threadIdx.x, m = lane & 15, g4 = lane >> 4;
+    // a wave is a block of its own: their work is uneven, and one that is done makes room at once
+    const uint32_t one = xcd_remap(blockIdx.x, gridDim.x), blk = one / 4;
+    const int wave = static_cast<int>(one % 4);
+    const DiffTile<MK> t = diff_tile<W, MK>(p, blk, wave, lane, p.tile_blocks);
+    if (t.tc.nclu == 0) return;  // no query of this wave lies inside the grid
+    uint32_t todo = 0xFFFFu;     // queries left to the lane groups
+    if (t.tc.nclu > 0) {
+        // every item of a tile lies in one slice, whose rows the caller keeps below 4 GiB: 32-bit offsets from a uniform base
+        const size_t slice = static_cast<size_t>(__builtin_amdgcn_readfirstlane(t.s)) * p.nkeys * static_cast<size_t>(2 * D);
+        const unsigned char* const Kb = static_cast<const unsigned char*>(p.K) + slice;
+        const unsigned char* const Vb = static_cast<const unsigned char*>(p.V) + slice;
+        HalfQueries<D> q;
+        q.load(static_cast<const unsigned char*>(p.Q) + static_cast<size_t>(t.gq) * (2 * D), g4);
+        MapReference ref[2];
+        {
+            float s0[2];
+            q.own_scores(Kb + t.centre * (2u * D), g4, s0);
+            const bool held = !CAUSAL || t.centre <= t.limit;
+            ref[0].start(s0[0], held, p.scale_log2e);
+            ref[1].start(s0[1], held, p.scale_log2e);
+        }
+        f32x4_t acc[2][kOt];
+        f32x4_t sum[2];  // of the weights: every row of an all-ones block's product holds query m's
+        const bf16x4_t ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f), static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+        sum[0] = sum[1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int o = 0; o < kOt; ++o) acc[0][o] = acc[1][o] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        diff_walk<D, W, CAUSAL, MK>(p, t, Kb, Vb, tk, tv, lane, [&](f32x4_t bias) {
+            f32x4_t sc[2];
+            q.scores([&](int ds) { return TR::frag(tk + m * kRowB, ds, g4); }, bias, sc);
+            float x[2][4];
+            block_weights(ref, sc, p.scale_log2e, x, [&](int h, float f) {
+                sum[h] *= f;
+#pragma unroll
+                for (int o = 0; o < kOt; ++o) acc[h][o] *= f;
+            });
+            const Parts2 w0 = parts2(x[0]), w1 = parts2(x[1]);
+            sum[0] = product2(ones, w0, sum[0]);
+            sum[1] = product2(ones, w1, sum[1]);
+#pragma unroll
+            for (int o = 0; o < kOt; ++o) {
+                const bf16x4_t vt = column4<D>(tv, m, g4, o);
+                acc[0][o] = product2(vt, w0, acc[0][o]);
+                acc[1][o] = product2(vt, w1, acc[1][o]);
+            }
+        });
+        const float i1 = 1.f / sum[0][0], i2 = p.lam[t.s] / sum[1][0];  // an empty set's are infinite
+        float size = i1 + i2;
+#pragma unroll
+        for (int o = 0; o < kOt; ++o) {
+            acc[0][o] = acc[0][o] * i1 - acc[1][o] * i2;
+            size += (fabsf(acc[0][o][0]) + fabsf(acc[0][o][1])) + (fabsf(acc[0][o][2]) + fabsf(acc[0][o][3]));
+        }
+        const uint64_t bad = __ballot(!(fabsf(size) < INFINITY));
+        todo = static_cast<uint32_t>(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xFFFFu;
+        if (t.valid && !((todo >> m) & 1u)) {
+            // lane holds channels 16 o + 4 g4 + i of query m
+            uint16_t* const row = static_cast<uint16_t*>(p.out) + static_cast<size_t>(t.g) * D + 4 * g4;
+#pragma unroll
+            for (int o = 0; o < kOt; ++o)
+                *reinterpret_cast<uint2*>(row + 16 * o) = make_uint2(bf16_pair(acc[0][o][0], acc[0][o][1]), bf16_pair(acc[0][o][2], acc[0][o][3]));
+        }
+    }
+    for (int i = lane / G; i < 16; i += 64 / G) {
+        uint32_t g;
+        if (((todo >> i) & 1u) && tile_item<kBlock / 4>(p.tq, blk, tile_wave_item(p.tq, wave, i), g))
+            diff_query<uint16_t, D, G, (CAUSAL || MK > 1 ? MK : 0), 2, 1>(p, g, lane & (G - 1), 0);
+    }
+}
+
+// The matrix-core kernel, if it takes this call (false: not launched): bf16 rows of 32 to 128 channels, up to four windows of
+// side 3, 5 or 7, a positive scale, slices of at most 4 GiB of key rows.
+template <int D, int W>
+hipError_t run_diff_tile(const DiffParams& p, uint64_t tiles, hipStream_t st, hipEvent_t e0, hipEvent_t e1)
+{
+    auto with = [&](auto mk) {
+        constexpr int MK = decltype(mk)::value;
+        return p.causal ? launch_wave(diff_tile_kernel<D, W, true, MK>, 4 * tiles, st, e0, e1, p)
+                        : launch_wave(diff_tile_kernel<D, W, false, MK>, 4 * tiles, st, e0, e1, p);
+    };
+    return p.kappa == 1   ? with(std::integral_constant<int, 1>{})
+           : p.kappa == 2 ? with(std::integral_constant<int, 2>{})
+                          : with(std::integral_constant<int, 4>{});
+}
+
+template <typename T, int D>
+bool run_diff_tiles(const DiffParams& p0, hipStream_t st, hipEvent_t e0, hipEvent_t e1, hipError_t& err)
+{
+    if constexpr (std::is_same<T, uint16_t>::value && D >= 32) {
+        if (p0.kappa > 4 || p0.b < 1 || p0.b > 3 || !(p0.scale_log2e > 0.f) ||
+            static_cast<uint64_t>(p0.nkeys) * (2 * D) > 0xFFFFFFFFull)
+            return false;
+        DiffParams p = p0;
+        p.tq = make_tiling(p.Hq, p.Wq, kBlock / 4);
+        const uint64_t tiles = tiling_blocks(p.tq, p.n / p.tq.plane);
+        if (tiles > kMaxBlocks) return false;
+        const int side = 2 * p.b + 1;
+        p.tile_blocks = p.kappa * side * side * (side == 3 ? 5 : 8) / 8;
+        err = side == 3   ? run_diff_tile<D, 3>(p, tiles, st, e0, e1)
+              : side == 5 ? run_diff_tile<D, 5>(p, tiles, st, e0, e1)
+                          : run_diff_tile<D, 7>(p, tiles, st, e0, e1);
+        return true;
+    }
+    return false;
+}
+
 template <typename T, int D, int MK>
 hipError_t run_diff(const DiffParams& p0, hipStream_t st, hipEvent_t e0, hipEvent_t e1)
 {
@@ -117,6 +245,8 @@ hipError_t run_diff(const DiffParams& p0, hipStream_t st, hipEvent_t e0, hipEven
             hipLaunchKernelGGL((diff_attend_kernel<T, D, G, MK, true>), dim3(p.n), dim3(64), 0, st, p);
         return hipGetLastError();
     }
+    hipError_t err = hipSuccess;
+    if (run_diff_tiles<T, D>(p, st, e0, e1, err)) return err;
     p.tq = make_tiling(p.Hq, p.Wq, Row<T, D, G>::kQpb, kLaneSkew);
     return launch(diff_attend_kernel<T, D, G, MK, false>, tiling_blocks(p.tq, p.n / p.tq.plane), st, e0, e1, p);
 }

@@ -10,8 +10,7 @@
 // through the inverse of the maps (scram_inverse.h).  No float atomics: every
 // gradient row has one writer.
 
-#include "scram_diff.h"
-#include "scram_inverse.h"
+#include "scram_strip.h"
 
 #include <algorithm>
 
@@ -360,6 +359,23 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
     if ((e = run_inverse(p, counts, offsets, sums, entries, st, nullptr, nullptr)) != hipSuccess) return e;
     if ((e = launch(diff_lam_kernel, S, st, nullptr, nullptr, static_cast<const double*>(p.lam_part), p.tq.div_slice.d, p.dlam)) != hipSuccess)
         return e;
+    // Key side on the matrix cores for bf16 and windows 3 x 3 .. 15 x 15; the keys that its strips leave, and those of every
+    // other call with many entries, a wave each.
+    if constexpr (std::is_same<T, uint16_t>::value) {
+        if (p.b >= 1 && p.b <= kTileMaxB) {
+            DiffParams pt = p;
+            pt.tk = make_tiling(p.Hk, p.Wk, kTileKeys);
+            const uint64_t halo = static_cast<uint64_t>(std::min(4 + 2 * p.b, p.Hk)) * std::min(4 + 2 * p.b, p.Wk);
+            const uint64_t mean = static_cast<uint64_t>(p.n) * p.kappa * halo / p.keys_total;  // entries of a strip
+            pt.heavy_entries = static_cast<int>(std::min<uint64_t>(std::max<uint64_t>(512, 2 * mean), INT32_MAX));
+            const uint64_t strips = kStripWaves * tiling_blocks(pt.tk, S);
+            e = !MULTI         ? launch_wave(bwd_key_strip_kernel<D, kStripPlain, DiffParams>, strips, st, nullptr, nullptr, pt)
+                : p.kappa == 1 ? launch_wave(bwd_key_strip_kernel<D, kStripCausal, DiffParams>, strips, st, nullptr, nullptr, pt)
+                               : launch_wave(bwd_key_strip_kernel<D, kStripMulti, DiffParams>, strips, st, nullptr, nullptr, pt);
+            if (e != hipSuccess) return e;
+            return launch(diff_heavy_kernel<T, D, G, MULTI>, 1024, st, nullptr, stop, p);
+        }
+    }
     if ((e = launch(diff_key_kernel<T, D, G, MULTI>, kblocks, st, nullptr, nullptr, p)) != hipSuccess) return e;
     return launch(diff_heavy_kernel<T, D, G, MULTI>, 1024, st, nullptr, stop, p);  // loops over however many there are
 }
@@ -415,6 +431,7 @@ hipError_t launch_diff_backward(int dtype, const DiffCall& c, const void* dO, fl
 uint64_t diff_backward_max_blocks(const Grid& g)
 {
     uint64_t most = std::max<uint64_t>(4096, query_blocks_most(g));  // (4096: the grid-stride kernels of the inverse map)
+    most = std::max(most, tiling_blocks(make_tiling(g.Hk, g.Wk, kTileKeys), g.S));  // key tiles on the matrix cores
     for (uint32_t items = kBlock; items >= kBlock / 16; items /= 2)
         most = std::max(most, tiling_blocks(make_tiling(g.Hk, g.Wk, items, kLaneSkew), g.S));
     return most;
