@@ -153,6 +153,16 @@ def _dev_tensor(t, name, ndim=None):
     return t
 
 
+def _plain(name, t, ndim, dtype, index):
+    """``t`` checked in one go: a contiguous tensor of ``ndim`` dims and ``dtype`` on device ``index``."""
+    if not (t.is_cuda and t.dtype == dtype and t.get_device() == index and t.dim() == ndim and t.is_contiguous()):
+        _dev_tensor(t, name, ndim)
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        raise ValueError(f"{name} is on {t.device}, expected device {index}")
+    return t
+
+
 def _same_device(device, **tensors):
     index = device.index
     for name, t in tensors.items():

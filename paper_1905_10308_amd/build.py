@@ -41,7 +41,7 @@ LINK_FLAGS = [f"--offload-arch={ARCH}", "-shared", "-fPIC"]
 # per-source additions: the attends' matrix-core kernels keep their accumulators in VGPRs (the
 # compiler would otherwise copy them between AGPRs and VGPRs around every rescale)
 _VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-EXTRA_FLAGS = {"scram_attend.hip": _VGPR_FORM, "scram_diff.hip": _VGPR_FORM}
+EXTRA_FLAGS = {"scram_attend.hip": _VGPR_FORM, "scram_diff.hip": _VGPR_FORM, "scram_diff_backward.hip": _VGPR_FORM}
 
 
 def hipcc() -> str:

@@ -197,8 +197,6 @@ diff_tile_kernel(DiffParams p)
     }
 }
 
-// The matrix-core kernel, if it takes this call (false: not launched): bf16 rows of 32 to 128 channels, up to four windows of
-// side 3, 5 or 7, a positive scale, slices of at most 4 GiB of key rows.
 template <int D, int W>
 hipError_t run_diff_tile(const DiffParams& p, uint64_t tiles, hipStream_t st, hipEvent_t e0, hipEvent_t e1)
 {
@@ -212,22 +210,17 @@ hipError_t run_diff_tile(const DiffParams& p, uint64_t tiles, hipStream_t st, hi
                           : with(std::integral_constant<int, 4>{});
 }
 
+// On the matrix cores, if they take this call (false: not launched).
 template <typename T, int D>
 bool run_diff_tiles(const DiffParams& p0, hipStream_t st, hipEvent_t e0, hipEvent_t e1, hipError_t& err)
 {
     if constexpr (std::is_same<T, uint16_t>::value && D >= 32) {
-        if (p0.kappa > 4 || p0.b < 1 || p0.b > 3 || !(p0.scale_log2e > 0.f) ||
-            static_cast<uint64_t>(p0.nkeys) * (2 * D) > 0xFFFFFFFFull)
-            return false;
         DiffParams p = p0;
-        p.tq = make_tiling(p.Hq, p.Wq, kBlock / 4);
-        const uint64_t tiles = tiling_blocks(p.tq, p.n / p.tq.plane);
-        if (tiles > kMaxBlocks) return false;
-        const int side = 2 * p.b + 1;
-        p.tile_blocks = p.kappa * side * side * (side == 3 ? 5 : 8) / 8;
-        err = side == 3   ? run_diff_tile<D, 3>(p, tiles, st, e0, e1)
-              : side == 5 ? run_diff_tile<D, 5>(p, tiles, st, e0, e1)
-                          : run_diff_tile<D, 7>(p, tiles, st, e0, e1);
+        const uint64_t tiles = diff_tiles<D>(p);
+        if (tiles == 0) return false;
+        err = p.b == 1   ? run_diff_tile<D, 3>(p, tiles, st, e0, e1)
+              : p.b == 2 ? run_diff_tile<D, 5>(p, tiles, st, e0, e1)
+                         : run_diff_tile<D, 7>(p, tiles, st, e0, e1);
         return true;
     }
     return false;

@@ -10,6 +10,7 @@
 // through the inverse of the maps (scram_inverse.h).  No float atomics: every
 // gradient row has one writer.
 
+#include "scram_diff_tile.h"
 #include "scram_strip.h"
 
 #include <algorithm>
@@ -31,122 +32,260 @@ __device__ double block_sum(double x)
     return t;
 }
 
-// A lane group per query.  As in the attend's gradients the keys enter as
-// k_j - k_ref, k_ref the key at the first match: the weights of a set sum to
-// one, so dQ = scale (A - D B) / l for any fixed k_ref, and A - D B does not
-// cancel where neighbouring keys are alike.
+// The inverse map's count of query g of slice s: one entry per match, and its slot among that match key's.
+__device__ __forceinline__ void count_matches(const DiffParams& p, uint32_t g, uint32_t s)
+{
+    for (int e = 0; e < p.kappa; ++e) {
+        const size_t x = static_cast<size_t>(e) * p.n + g;
+        p.slots[x] = atomicAdd(p.counts + static_cast<size_t>(s) * p.nkeys + clamp_index(p.J[x], p.nkeys), 1);
+    }
+}
+
+// Query g on a lane group: its dQ row and statistics; returns D of the second map (on lane 0, 0 on the others).  As in the
+// attend's gradients the keys enter as k_j - k_ref, k_ref the key at the first match: the weights of a set sum to one, so
+// dQ = scale (A - D B) / l for any fixed k_ref, and A - D B does not cancel where neighbouring keys are alike.
 template <typename T, int D, int G, int MK>
-__global__ __launch_bounds__(kBlock) void diff_query_kernel(DiffParams p)
+__device__ __forceinline__ float diff_query_gradient(const DiffParams& p, uint32_t g, int lane)
 {
     constexpr bool MULTI = MK > 0;
     using RW = Row<T, D, G>;
     static_assert(RW::kCh == 2, "two chunks per lane: one of each half");
     constexpr int H = RW::kEpc;  // channels per lane of each half
     constexpr int kNb = 2;
+    uint32_t s, rem;
+    divmod(g, p.div_plane, s, rem);
+    const size_t slice = static_cast<size_t>(s) * p.nkeys * D;
+    const T* Ks = static_cast<const T*>(p.K) + slice;
+    const T* Vs = static_cast<const T*>(p.V) + slice;
+    uint4 q[2], go[2];
+    load_row<T, D, G>(static_cast<const T*>(p.Q), g, lane, q);
+    load_row<T, D, G>(static_cast<const T*>(p.dO), g, lane, go);
+    WindowSet<(MK > 0 ? MK : 1)> ws;
+    if constexpr (MULTI) {
+        ws = make_window_set<MK>(p, g, rem);
+        ws.local = causal_limit(p, s, rem);
+    }
+    float kref[2 * H];
+    {
+        uint4 kr0[2];
+        load_row<T, D, G>(Ks, clamp_index(p.J[g], p.nkeys), lane, kr0);
+        unpack_row<T, 2>(kr0, kref);
+    }
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, dn[2] = {0.f, 0.f};
+    float A[2][H], B[2][H];
+#pragma unroll
+    for (int i = 0; i < H; ++i) A[0][i] = A[1][i] = B[0][i] = B[1][i] = 0.f;
+    for (int e = 0; e < (MULTI ? p.kappa : 1); ++e) {
+        uint32_t u, v;
+        if constexpr (MULTI)
+            ws.centre(e, u, v);
+        else
+            divmod(static_cast<uint32_t>(clamp_index(p.J[g], p.nkeys)), p.div_wk, u, v);
+        walk_window<T, D, G, kNb, MK>(p, Ks, Vs, ws, e, u, v, 0, 1, lane, [&](const auto& ok, const auto& kr, const auto& vr) {
+            float sc[2][kNb], dp[kNb];
+#pragma unroll
+            for (int j = 0; j < kNb; ++j) dp[j] = row_score<T, D, G>(go, vr[j]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float mb = m[h];
+#pragma unroll
+                for (int j = 0; j < kNb; ++j) {
+                    sc[h][j] = half_score<T, G>(q[h], kr[j][h]) * p.scale_log2e;
+                    mb = ok[j] ? fmaxf(mb, sc[h][j]) : mb;
+                }
+                if (mb > m[h] + kRescaleSlack) {
+                    const float alpha = __builtin_amdgcn_exp2f(m[h] - mb);
+                    l[h] *= alpha;
+                    dn[h] *= alpha;
+#pragma unroll
+                    for (int i = 0; i < H; ++i) A[h][i] *= alpha, B[h][i] *= alpha;
+                    m[h] = mb;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kNb; ++j) {
+                if (!ok[j]) continue;
+                float kf[2 * H];
+                unpack_row<T, 2>(kr[j], kf);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float pj = __builtin_amdgcn_exp2f(sc[h][j] - (m[h] == -INFINITY ? 0.f : m[h]));
+                    const float pd = pj * dp[j];
+                    l[h] += pj;
+                    dn[h] += pd;
+#pragma unroll
+                    for (int i = 0; i < H; ++i) {
+                        const float kd = kf[h * H + i] - kref[h * H + i];
+                        A[h][i] = fmaf(pd, kd, A[h][i]);
+                        B[h][i] = fmaf(pj, kd, B[h][i]);
+                    }
+                }
+            }
+        });
+    }
+    float Dh[2], lse[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float inv = l[h] != 0.f ? 1.f / l[h] : 0.f;
+        Dh[h] = dn[h] * inv;
+        lse[h] = l[h] != 0.f ? m[h] + log2f(l[h]) : INFINITY;  // +inf: every weight is 0
+        const float f = (h == 0 ? p.scale : -p.lam[s] * p.scale) * inv;
+        float4* o = reinterpret_cast<float4*>(p.dQ + static_cast<size_t>(g) * D + (h * G + lane) * H);
+#pragma unroll
+        for (int i = 0; i < H / 4; ++i)
+            o[i] = make_float4((A[h][4 * i] - Dh[h] * B[h][4 * i]) * f, (A[h][4 * i + 1] - Dh[h] * B[h][4 * i + 1]) * f,
+                               (A[h][4 * i + 2] - Dh[h] * B[h][4 * i + 2]) * f, (A[h][4 * i + 3] - Dh[h] * B[h][4 * i + 3]) * f);
+    }
+    if (lane != 0) return 0.f;
+    p.stats[g] = make_float4(lse[0], Dh[0], lse[1], Dh[1]);
+    return Dh[1];
+}
+
+// A lane group per query.
+template <typename T, int D, int G, int MK>
+__global__ __launch_bounds__(kBlock) void diff_query_kernel(DiffParams p)
+{
     const int lane = threadIdx.x & (G - 1);
     const uint32_t blk = xcd_remap(blockIdx.x, gridDim.x);
     uint32_t g;
-    const bool valid = tile_item<RW::kQpb>(p.tq, blk, threadIdx.x / G, g);
     float D2 = 0.f;
-    if (valid) {
-        uint32_t s, rem;
-        divmod(g, p.div_plane, s, rem);
-        // the inverse map's count: one entry per match of this query, and its slot among that match key's
+    if (tile_item<Row<T, D, G>::kQpb>(p.tq, blk, threadIdx.x / G, g)) {
         if (lane == 0) {
-            for (int e = 0; e < (MULTI ? p.kappa : 1); ++e) {
-                const size_t x = static_cast<size_t>(e) * p.n + g;
-                p.slots[x] = atomicAdd(p.counts + static_cast<size_t>(s) * p.nkeys + clamp_index(p.J[x], p.nkeys), 1);
-            }
+            uint32_t s, rem;
+            divmod(g, p.div_plane, s, rem);
+            count_matches(p, g, s);
         }
-        const size_t slice = static_cast<size_t>(s) * p.nkeys * D;
-        const T* Ks = static_cast<const T*>(p.K) + slice;
-        const T* Vs = static_cast<const T*>(p.V) + slice;
-        uint4 q[2], go[2];
-        load_row<T, D, G>(static_cast<const T*>(p.Q), g, lane, q);
-        load_row<T, D, G>(static_cast<const T*>(p.dO), g, lane, go);
-        WindowSet<(MK > 0 ? MK : 1)> ws;
-        if constexpr (MULTI) {
-            ws = make_window_set<MK>(p, g, rem);
-            ws.local = causal_limit(p, s, rem);
-        }
-        float kref[2 * H];
-        {
-            uint4 kr0[2];
-            load_row<T, D, G>(Ks, clamp_index(p.J[g], p.nkeys), lane, kr0);
-            unpack_row<T, 2>(kr0, kref);
-        }
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, dn[2] = {0.f, 0.f};
-        float A[2][H], B[2][H];
-#pragma unroll
-        for (int i = 0; i < H; ++i) A[0][i] = A[1][i] = B[0][i] = B[1][i] = 0.f;
-        for (int e = 0; e < (MULTI ? p.kappa : 1); ++e) {
-            uint32_t u, v;
-            if constexpr (MULTI)
-                ws.centre(e, u, v);
-            else
-                divmod(static_cast<uint32_t>(clamp_index(p.J[g], p.nkeys)), p.div_wk, u, v);
-            walk_window<T, D, G, kNb, MK>(p, Ks, Vs, ws, e, u, v, 0, 1, lane, [&](const auto& ok, const auto& kr, const auto& vr) {
-                float sc[2][kNb], dp[kNb];
-#pragma unroll
-                for (int j = 0; j < kNb; ++j) dp[j] = row_score<T, D, G>(go, vr[j]);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float mb = m[h];
-#pragma unroll
-                    for (int j = 0; j < kNb; ++j) {
-                        sc[h][j] = half_score<T, G>(q[h], kr[j][h]) * p.scale_log2e;
-                        mb = ok[j] ? fmaxf(mb, sc[h][j]) : mb;
-                    }
-                    if (mb > m[h] + kRescaleSlack) {
-                        const float alpha = __builtin_amdgcn_exp2f(m[h] - mb);
-                        l[h] *= alpha;
-                        dn[h] *= alpha;
-#pragma unroll
-                        for (int i = 0; i < H; ++i) A[h][i] *= alpha, B[h][i] *= alpha;
-                        m[h] = mb;
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < kNb; ++j) {
-                    if (!ok[j]) continue;
-                    float kf[2 * H];
-                    unpack_row<T, 2>(kr[j], kf);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float pj = __builtin_amdgcn_exp2f(sc[h][j] - (m[h] == -INFINITY ? 0.f : m[h]));
-                        const float pd = pj * dp[j];
-                        l[h] += pj;
-                        dn[h] += pd;
-#pragma unroll
-                        for (int i = 0; i < H; ++i) {
-                            const float kd = kf[h * H + i] - kref[h * H + i];
-                            A[h][i] = fmaf(pd, kd, A[h][i]);
-                            B[h][i] = fmaf(pj, kd, B[h][i]);
-                        }
-                    }
-                }
-            });
-        }
-        float Dh[2], lse[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float inv = l[h] != 0.f ? 1.f / l[h] : 0.f;
-            Dh[h] = dn[h] * inv;
-            lse[h] = l[h] != 0.f ? m[h] + log2f(l[h]) : INFINITY;  // +inf: every weight is 0
-            const float f = (h == 0 ? p.scale : -p.lam[s] * p.scale) * inv;
-            float4* o = reinterpret_cast<float4*>(p.dQ + static_cast<size_t>(g) * D + (h * G + lane) * H);
-#pragma unroll
-            for (int i = 0; i < H / 4; ++i)
-                o[i] = make_float4((A[h][4 * i] - Dh[h] * B[h][4 * i]) * f, (A[h][4 * i + 1] - Dh[h] * B[h][4 * i + 1]) * f,
-                                   (A[h][4 * i + 2] - Dh[h] * B[h][4 * i + 2]) * f, (A[h][4 * i + 3] - Dh[h] * B[h][4 * i + 3]) * f);
-        }
-        if (lane == 0) {
-            p.stats[g] = make_float4(lse[0], Dh[0], lse[1], Dh[1]);
-            D2 = Dh[1];
-        }
+        D2 = diff_query_gradient<T, D, G, MK>(p, g, lane);
     }
     const double part = block_sum(D2);
     if (threadIdx.x == 0) p.lam_part[blk] = part;
+}
+
+// Waves per SIMD that the tile kernel's registers are sized for.
+constexpr int diff_grad_waves(int D) { return D == 128 ? 1 : D == 64 ? 2 : 3; }
+
+// On the matrix cores (scram_diff_tile.h), bf16, a wave of 16 queries.  Per block of 16 keys
+//   S1^T, S2^T = K_blk Q^T,  dP^T = V_blk dO^T         keys x queries
+//   P1, P2 = 2^(S scale log2 e - reference) on the query's keys, 0 elsewhere;  PD = P dP
+//   B^T += K_blk^T P^T,  A^T += K_blk^T PD^T           channels x queries: the first half's with P1, the last with P2
+//   l += 1^T P^T,  dn += 1^T PD^T                      all-ones blocks, of each map
+// with the weights as three bf16 parts that add up to them (the gradients are fp32).  With D = dn / l and k_ref the key at the
+// first match, dQ = scale ((A - dn k_ref) - D (B - l k_ref)) / l: the lane group's sums, whose subtraction cancels no more.
+// A query whose sums are not finite, or whose set is empty, is computed over again on a lane group, and so are a wave's
+// queries whose matches lie too far apart to share rows.
+template <int D, int W, bool CAUSAL, int MK>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(diff_grad_waves(D)))) void
+diff_query_tile_kernel(DiffParams p)
+{
+    using TR = TileRow<D>;
+    constexpr int kOt = D / 16, kRowB = 2 * D + kRowPad;
+    constexpr int G = kDiffLanes<uint16_t, D>;
+    __shared__ __align__(16) unsigned char tk[16 * kRowB], tv[16 * kRowB];
+    const int lane = threadIdx.x, m = lane & 15, g4 = lane >> 4;
+    const uint32_t one = xcd_remap(blockIdx.x, gridDim.x), blk = one / 4;
+    const int wave = static_cast<int>(one % 4);
+    const DiffTile<MK> t = diff_tile<W, MK>(p, blk, wave, lane, p.tile_blocks);
+    if (t.valid && g4 == 0) count_matches(p, t.g, t.s);
+    uint32_t todo = t.tc.nclu == 0 ? 0u : 0xFFFFu;  // queries left to the lane groups
+    float D2 = 0.f;
+    if (t.tc.nclu > 0) {
+        const size_t slice = static_cast<size_t>(__builtin_amdgcn_readfirstlane(t.s)) * p.nkeys * static_cast<size_t>(2 * D);
+        const unsigned char* const Kb = static_cast<const unsigned char*>(p.K) + slice;
+        const unsigned char* const Vb = static_cast<const unsigned char*>(p.V) + slice;
+        HalfQueries<D> q;
+        q.load(static_cast<const unsigned char*>(p.Q) + static_cast<size_t>(t.gq) * (2 * D), g4);
+        typename TR::Frag go[TR::kDs];
+#pragma unroll
+        for (int ds = 0; ds < TR::kDs; ++ds)
+            go[ds] = TR::frag(static_cast<const unsigned char*>(p.dO) + static_cast<size_t>(t.gq) * (2 * D), ds, g4);
+        MapReference ref[2];
+        {
+            float s0[2];
+            q.own_scores(Kb + t.centre * (2u * D), g4, s0);
+            const bool held = !CAUSAL || t.centre <= t.limit;
+            ref[0].start(s0[0], held, p.scale_log2e);
+            ref[1].start(s0[1], held, p.scale_log2e);
+        }
+        const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+        const bf16x4_t ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f), static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+        f32x4_t A[kOt], B[kOt], l[2], dn[2];
+#pragma unroll
+        for (int o = 0; o < kOt; ++o) A[o] = B[o] = zero;
+        l[0] = l[1] = dn[0] = dn[1] = zero;
+        diff_walk<D, W, CAUSAL, MK>(p, t, Kb, Vb, tk, tv, lane, [&](f32x4_t bias) {
+            f32x4_t sc[2], dp = zero;
+            q.scores([&](int ds) { return TR::frag(tk + m * kRowB, ds, g4); }, bias, sc);
+#pragma unroll
+            for (int ds = 0; ds < TR::kDs; ++ds) dp = TR::product(TR::frag(tv + m * kRowB, ds, g4), go[ds], dp);
+            float x[2][4];
+            block_weights(ref, sc, p.scale_log2e, x, [&](int h, float f) {
+                l[h] *= f;
+                dn[h] *= f;
+#pragma unroll
+                for (int o = 0; o < kOt; ++o)
+                    if (o / (kOt / 2) == h) A[o] *= f, B[o] *= f;
+            });
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const Parts3 w = parts3(x[h]);
+                l[h] = product3(ones, w, l[h]);
+                float y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = x[h][i] * dp[i];
+                const Parts3 wd = parts3(y);
+                dn[h] = product3(ones, wd, dn[h]);
+#pragma unroll
+                for (int o = h * (kOt / 2); o < (h + 1) * (kOt / 2); ++o) {
+                    const bf16x4_t kt = column4<D>(tk, m, g4, o);
+                    B[o] = product3(kt, w, B[o]);
+                    A[o] = product3(kt, wd, A[o]);
+                }
+            }
+        });
+        float inv[2], Dh[2], lse[2], size = 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            inv[h] = 1.f / l[h][0];  // an empty set's is infinite
+            Dh[h] = dn[h][0] * inv[h];
+            lse[h] = ref[h].ref + log2f(l[h][0]);
+            size += inv[h] + fabsf(Dh[h]);
+            inv[h] *= h == 0 ? p.scale : -p.lam[t.s] * p.scale;
+        }
+        // lane holds channels 16 o + 4 g4 + i of query m
+        const unsigned char* const krow = Kb + t.centre * (2u * D);
+#pragma unroll
+        for (int o = 0; o < kOt; ++o) {
+            const int h = o / (kOt / 2);
+            const uint2 kw = *reinterpret_cast<const uint2*>(krow + 32 * o + 8 * g4);
+            const float kref[4] = {__uint_as_float(kw.x << 16), __uint_as_float(kw.x & 0xFFFF0000u), __uint_as_float(kw.y << 16),
+                                   __uint_as_float(kw.y & 0xFFFF0000u)};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                A[o][i] = ((A[o][i] - dn[h][0] * kref[i]) - Dh[h] * (B[o][i] - l[h][0] * kref[i])) * inv[h];
+                size += fabsf(A[o][i]);
+            }
+        }
+        const uint64_t bad = __ballot(!(fabsf(size) < INFINITY));
+        todo = static_cast<uint32_t>(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xFFFFu;
+        if (t.valid && !((todo >> m) & 1u)) {
+            if (g4 == 0) {
+                p.stats[t.g] = make_float4(lse[0], Dh[0], lse[1], Dh[1]);
+                D2 = Dh[1];
+            }
+#pragma unroll
+            for (int o = 0; o < kOt; ++o)
+                *reinterpret_cast<f32x4_t*>(p.dQ + static_cast<size_t>(t.g) * D + 16 * o + 4 * g4) = A[o];
+        }
+    }
+    double part = D2;
+    for (int i = lane / G; i < 16; i += 64 / G) {
+        uint32_t g;
+        if (((todo >> i) & 1u) && tile_item<kBlock / 4>(p.tq, blk, tile_wave_item(p.tq, wave, i), g))
+            part += diff_query_gradient<uint16_t, D, G, (CAUSAL || MK > 1 ? MK : 0)>(p, g, lane & (G - 1));
+    }
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) part += __shfl_xor(part, k);
+    if (lane == 0) p.lam_part[one] = part;
 }
 
 // dlam of a slice: minus the sum of its query blocks' parts.  One block per slice.
@@ -327,13 +466,42 @@ __global__ __launch_bounds__(kBlock) void diff_heavy_kernel(DiffParams p)
 
 size_t r256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
 
-// Query blocks: a lane group of one lane at least per query.
+// Parts of dlam: a block of lane groups (of one lane at least per query), or a wave of 16 queries, each.
 uint64_t query_blocks_most(const Grid& g)
 {
-    uint64_t most = 0;
+    uint64_t most = 4 * tiling_blocks(make_tiling(g.Hq, g.Wq, kBlock / 4), g.S);
     for (uint32_t items = kBlock; items >= kBlock / 16; items /= 2)
         most = std::max(most, tiling_blocks(make_tiling(g.Hq, g.Wq, items, kLaneSkew), g.S));
     return most;
+}
+
+template <int D, int W>
+hipError_t run_diff_query_tile(const DiffParams& p, uint64_t waves, hipStream_t st)
+{
+    auto with = [&](auto mk) {
+        constexpr int MK = decltype(mk)::value;
+        return p.causal ? launch_wave(diff_query_tile_kernel<D, W, true, MK>, waves, st, nullptr, nullptr, p)
+                        : launch_wave(diff_query_tile_kernel<D, W, false, MK>, waves, st, nullptr, nullptr, p);
+    };
+    return p.kappa == 1   ? with(std::integral_constant<int, 1>{})
+           : p.kappa == 2 ? with(std::integral_constant<int, 2>{})
+                          : with(std::integral_constant<int, 4>{});
+}
+
+// The query side on the matrix cores, if it takes this call (false: not launched).
+template <typename T, int D>
+bool run_diff_query_tiles(const DiffParams& p0, hipStream_t st, hipError_t& err)
+{
+    if constexpr (std::is_same<T, uint16_t>::value && D >= 32) {
+        DiffParams p = p0;
+        const uint64_t tiles = diff_tiles<D>(p);
+        if (tiles == 0) return false;
+        err = p.b == 1   ? run_diff_query_tile<D, 3>(p, 4 * tiles, st)
+              : p.b == 2 ? run_diff_query_tile<D, 5>(p, 4 * tiles, st)
+                         : run_diff_query_tile<D, 7>(p, 4 * tiles, st);
+        return true;
+    }
+    return false;
 }
 
 template <typename T, int D, bool MULTI>
@@ -350,14 +518,17 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
     const size_t N = p.keys_total;
     hipError_t e;
     if ((e = launch(zero_i32_kernel, stride_blocks(N), st, start, nullptr, counts, N, p.n_heavy)) != hipSuccess) return e;
-    if constexpr (!MULTI)
+    uint32_t parts = p.tq.div_slice.d;  // of dlam, per slice
+    if (run_diff_query_tiles<T, D>(p, st, e)) {
+        parts = 4 * make_tiling(p.Hq, p.Wq, kBlock / 4).div_slice.d;
+    } else if constexpr (!MULTI)
         e = launch(diff_query_kernel<T, D, G, 0>, qblocks, st, nullptr, nullptr, p);
     else
         e = p.kappa <= 2 ? launch(diff_query_kernel<T, D, G, 2>, qblocks, st, nullptr, nullptr, p)
                          : launch(diff_query_kernel<T, D, G, kMaxKappa>, qblocks, st, nullptr, nullptr, p);
     if (e != hipSuccess) return e;
     if ((e = run_inverse(p, counts, offsets, sums, entries, st, nullptr, nullptr)) != hipSuccess) return e;
-    if ((e = launch(diff_lam_kernel, S, st, nullptr, nullptr, static_cast<const double*>(p.lam_part), p.tq.div_slice.d, p.dlam)) != hipSuccess)
+    if ((e = launch(diff_lam_kernel, S, st, nullptr, nullptr, static_cast<const double*>(p.lam_part), parts, p.dlam)) != hipSuccess)
         return e;
     // Key side on the matrix cores for bf16 and windows 3 x 3 .. 15 x 15; the keys that its strips leave, and those of every
     // other call with many entries, a wave each.
@@ -367,7 +538,7 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
             pt.tk = make_tiling(p.Hk, p.Wk, kTileKeys);
             const uint64_t halo = static_cast<uint64_t>(std::min(4 + 2 * p.b, p.Hk)) * std::min(4 + 2 * p.b, p.Wk);
             const uint64_t mean = static_cast<uint64_t>(p.n) * p.kappa * halo / p.keys_total;  // entries of a strip
-            pt.heavy_entries = static_cast<int>(std::min<uint64_t>(std::max<uint64_t>(512, 2 * mean), INT32_MAX));
+            pt.heavy_entries = static_cast<int>(std::min<uint64_t>(std::max<uint64_t>(1024, 4 * mean), INT32_MAX));
             const uint64_t strips = kStripWaves * tiling_blocks(pt.tk, S);
             e = !MULTI         ? launch_wave(bwd_key_strip_kernel<D, kStripPlain, DiffParams>, strips, st, nullptr, nullptr, pt)
                 : p.kappa == 1 ? launch_wave(bwd_key_strip_kernel<D, kStripCausal, DiffParams>, strips, st, nullptr, nullptr, pt)

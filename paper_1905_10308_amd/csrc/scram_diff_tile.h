@@ -381,6 +381,28 @@ __device__ __forceinline__ f32x4_t product2(bf16x4_t a, const Parts2& b, f32x4_t
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(a, a, 0, 1, 2, 3, 4, 5, 6, 7), b.both, c, 0, 0, 0);
 }
 
+struct Parts3 {
+    bf16x8_t upper;
+    bf16x4_t last;
+};
+
+__device__ __forceinline__ Parts3 parts3(const float (&x)[4])
+{
+    const uint32_t h0 = bf16_pair(x[0], x[1]), h1 = bf16_pair(x[2], x[3]);
+    const float r[4] = {x[0] - __uint_as_float(h0 << 16), x[1] - __uint_as_float(h0 & 0xFFFF0000u),
+                        x[2] - __uint_as_float(h1 << 16), x[3] - __uint_as_float(h1 & 0xFFFF0000u)};
+    const uint32_t m0 = bf16_pair(r[0], r[1]), m1 = bf16_pair(r[2], r[3]);
+    const uint32_t l0 = bf16_pair(r[0] - __uint_as_float(m0 << 16), r[1] - __uint_as_float(m0 & 0xFFFF0000u));
+    const uint32_t l1 = bf16_pair(r[2] - __uint_as_float(m1 << 16), r[3] - __uint_as_float(m1 & 0xFFFF0000u));
+    return Parts3{__builtin_bit_cast(bf16x8_t, make_uint4(h0, h1, m0, m1)), __builtin_bit_cast(bf16x4_t, make_uint2(l0, l1))};
+}
+
+__device__ __forceinline__ f32x4_t product3(bf16x4_t a, const Parts3& b, f32x4_t c)
+{
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(a, a, 0, 1, 2, 3, 4, 5, 6, 7), b.upper, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b.last, c, 0, 0, 0);
+}
+
 // Rows 4 g4 .. 4 g4 + 3 of a staged block at channel 16 o + m: the transposing load hands lane i of each 16 the element e of
 // the 8 bytes that lane 4 e + i / 4 addresses.
 template <int D>
@@ -390,11 +412,22 @@ __device__ __forceinline__ bf16x4_t column4(const unsigned char* tile, int m, in
     return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4_t*)(at));
 }
 
-// Sum over the four lanes of query m.
-__device__ __forceinline__ float over_groups(float x)
+// Host: whether the matrix cores take this call -- up to four windows of side 3, 5 or 7, a positive scale, slices of at most
+// 4 GiB of key rows (bf16 rows of 32 to 128 channels).  Sets the tiling and the blocks up to which a wave walks its boxes;
+// returns the tiles of 64 queries, 0: not taken.
+template <int D>
+uint64_t diff_tiles(DiffParams& p)
 {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    if (p.kappa > 4 || p.b < 1 || p.b > 3 || !(p.scale_log2e > 0.f) || static_cast<uint64_t>(p.nkeys) * (2 * D) > 0xFFFFFFFFull)
+        return 0;
+    p.tq = make_tiling(p.Hq, p.Wq, kBlock / 4);
+    const uint64_t tiles = tiling_blocks(p.tq, p.n / p.tq.plane);
+    // A lane group takes kappa w^2 keys of its query, one after another.  4 x 256 x 256, 64 channels, smooth displacements: up
+    // to as many blocks the boxes are faster (two 5 x 5 windows 119 us, with 5/8 of it 123, 12/8 the same; 128 channels 92,
+    // 104), 3 x 3 up to 5/8 (two windows 70; 12/8 80); on matches of noise 12/8 cost half as much again.
+    const int side = 2 * p.b + 1;
+    p.tile_blocks = p.kappa * side * side * (side == 3 ? 5 : 8) / 8;
+    return tiles > kMaxBlocks / 4 ? 0 : tiles;
 }
 
 }  // namespace

@@ -9,31 +9,33 @@ from __future__ import annotations
 from . import binding as _b
 
 
-def _rows(Q, K, V, argmax, lam, first, causal, extra=()):
+def _rows(Q, K, V, argmax, lam, first, causal, dO=None):
     """Checks of the arguments that the call and its gradients share: (grid, d, dv, kappa, first, origin)."""
     torch = _b._torch()
-    for name, t in (("Q", Q), ("K", K), ("V", V), *extra):
-        _b._dev_tensor(t, name, 4)
-        if t.dtype != Q.dtype:
-            raise TypeError(f"{name} must have the dtype of Q")
-    _b._dev_tensor(argmax, "argmax")
+    kind, index = Q.dtype, Q.get_device()
+    _b._plain("Q", Q, 4, kind, index)
     S, Hq, Wq, d = Q.shape
-    _, Hk, Wk, _ = K.shape
-    if tuple(K.shape[:3]) != tuple(V.shape[:3]) or K.shape[0] != S or K.shape[3] != d:
+    _, Hk, Wk, dv = _b._plain("V", V, 4, kind, index).shape
+    if _b._plain("K", K, 4, kind, index).shape != (S, Hk, Wk, d) or V.shape[0] != S:
         raise ValueError("K and V must share the key grid; K must match Q's slices and channels")
     if d < 2 or d % 2:
         raise ValueError(f"the channels of Q and K are two maps' halves: {d} is not even")
-    if argmax.dtype != torch.int32 or tuple(argmax.shape[-3:]) != (S, Hq, Wq) or argmax.dim() not in (3, 4):
+    maps = argmax.dim()
+    _b._plain("argmax", argmax, maps, torch.int32, index)
+    if argmax.shape[-3:] != (S, Hq, Wq) or maps not in (3, 4):
         raise ValueError("argmax must be int32 [S, Hq, Wq] or [kappa, S, Hq, Wq]")
-    _b._check_buffer(lam, "lam", (S,), torch.float32)
+    if _b._plain("lam", lam, 1, torch.float32, index).shape[0] != S:
+        raise ValueError(f"lam must have {S} weights, one per slice")
+    if dO is not None and _b._plain("dO", dO, 4, kind, index).shape != (S, Hq, Wq, dv):
+        raise ValueError("dO must be [S, Hq, Wq, dv]")
     origin = None
     if isinstance(first, torch.Tensor):
-        _b._check_buffer(first, "first", (S,), torch.int32)
-        first, origin = 0, first
+        first, origin = 0, _b._plain("first", first, 1, torch.int32, index)
+        if origin.shape[0] != S:
+            raise ValueError(f"first must be a place for each of {S} slices")
     if not causal and (first or origin is not None):
         raise ValueError("first is the queries' place under the causal mask: it needs causal=True")
-    _b._same_device(Q.device, K=K, V=V, argmax=argmax, lam=lam, first=origin, **dict(extra))
-    return (S, Hq, Wq, Hk, Wk), d, V.shape[3], 1 if argmax.dim() == 3 else argmax.shape[0], int(first), origin
+    return (S, Hq, Wq, Hk, Wk), d, dv, argmax.shape[0] if maps == 4 else 1, int(first), origin
 
 
 def _width(d: int, dv: int) -> int:
@@ -67,22 +69,22 @@ def differential_attend(Q, K, V, argmax, lam, window: int, scale: float | None =
     torch = _b._torch()
     grid, d, dv, kappa, first, origin = _rows(Q, K, V, argmax, lam, first, causal)
     dev = Q.device
-    shape = tuple(Q.shape[:3]) + (dv,)
-    if out is not None:
-        _b._same_device(dev, out=out)
-        _b._check_buffer(out, "out", shape, Q.dtype)
+    S, Hq, Wq, _, _ = grid
+    if out is not None and _b._plain("out", out, 4, Q.dtype, Q.get_device()).shape != (S, Hq, Wq, dv):
+        raise ValueError(f"out must be {(S, Hq, Wq, dv)}, got {tuple(out.shape)}")
     code = _b._dtype_code(Q)
     if scale is None:
         scale = (d // 2) ** -0.5
     w = _width(d, dv)
-    Q, K = _halves(w, Q, K)
-    V, = _b._pad_channels(w, V)
-    res = out if out is not None and w == dv else torch.empty(shape[:3] + (w,), dtype=Q.dtype, device=dev)
+    if w != d or w != dv:
+        Q, K = _halves(w, Q, K)
+        V, = _b._pad_channels(w, V)
+    res = out if out is not None and w == dv else torch.empty((S, Hq, Wq, w), dtype=Q.dtype, device=dev)
     ev = None if events is None else _b._event_array(events, 2)
     _b._call(_b.lib().scram_differential_attend, "scram_differential_attend", dev,
-             (_b._ptr(Q), _b._ptr(K), _b._ptr(V), code, _b._ptr(argmax), int(kappa), _b._ptr(lam), *grid, w, w, int(window),
-              float(scale), _b.CAUSAL if causal else 0, first, _b._ptr(origin), _b._ptr(res), ev))
-    return _b._unpad_into(res, dv, out)
+             (Q.data_ptr(), K.data_ptr(), V.data_ptr(), code, argmax.data_ptr(), kappa, lam.data_ptr(), *grid, w, w, int(window),
+              float(scale), _b.CAUSAL if causal else 0, first, _b._ptr(origin), res.data_ptr(), ev))
+    return res if w == dv else _b._unpad_into(res, dv, out)
 
 
 def differential_attend_backward(Q, K, V, argmax, lam, dO, window: int, scale: float | None = None, *, causal: bool = False,
@@ -94,9 +96,7 @@ def differential_attend_backward(Q, K, V, argmax, lam, dO, window: int, scale: f
     ``events``: optional 2 timing-enabled events (start and end of the whole call).
     """
     torch = _b._torch()
-    grid, d, dv, kappa, first, origin = _rows(Q, K, V, argmax, lam, first, causal, (("dO", dO),))
-    if tuple(dO.shape) != tuple(Q.shape[:3]) + (dv,):
-        raise ValueError("dO must be [S, Hq, Wq, dv]")
+    grid, d, dv, kappa, first, origin = _rows(Q, K, V, argmax, lam, first, causal, dO)
     dev = Q.device
     _b._same_device(dev, workspace=workspace)
     code = _b._dtype_code(Q)
@@ -109,14 +109,15 @@ def differential_attend_backward(Q, K, V, argmax, lam, dO, window: int, scale: f
     dV = torch.empty((S, Hk, Wk, w), dtype=torch.float32, device=dev)
     dlam = torch.empty((S,), dtype=torch.float32, device=dev)
     kind = Q.dtype
-    Q, K = _halves(w, Q, K)
-    V, dO = _b._pad_channels(w, V, dO)
+    if w != d or w != dv:
+        Q, K = _halves(w, Q, K)
+        V, dO = _b._pad_channels(w, V, dO)
     workspace = _b._workspace(workspace, differential_attend_backward_workspace_bytes(*grid, kappa, d=w, dtype=kind), dev)
     ev = None if events is None else _b._event_array(events, 2)
     _b._call(_b.lib().scram_differential_attend_backward, "scram_differential_attend_backward", dev,
-             (_b._ptr(Q), _b._ptr(K), _b._ptr(V), code, _b._ptr(argmax), int(kappa), _b._ptr(lam), *grid, w, w, int(window),
-              float(scale), _b.CAUSAL if causal else 0, first, _b._ptr(origin), _b._ptr(dO), _b._ptr(dQ), _b._ptr(dK),
-              _b._ptr(dV), _b._ptr(dlam), _b._ptr(workspace), workspace.numel() * workspace.element_size(), ev))
+             (Q.data_ptr(), K.data_ptr(), V.data_ptr(), code, argmax.data_ptr(), kappa, lam.data_ptr(), *grid, w, w, int(window),
+              float(scale), _b.CAUSAL if causal else 0, first, _b._ptr(origin), dO.data_ptr(), dQ.data_ptr(), dK.data_ptr(),
+              dV.data_ptr(), dlam.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), ev))
     if w != d:
         two = [t.view(*t.shape[:-1], 2, w // 2) for t in (dQ, dK)]
         dQ, dK = (t.view(*t.shape[:-2], d) for t in _b._unpad(w // 2, *((t, d // 2) for t in two)))

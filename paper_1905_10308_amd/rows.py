@@ -13,36 +13,14 @@ ROTARY_INTERLEAVED = 1
 ROTARY_INVERSE = 2
 
 
-@functools.lru_cache(maxsize=64)
-def _frequencies(sections, base: float):
-    """base ** (-j / m) for pair j of an axis with m pairs, as a ctypes array."""
-    f = [base ** (-j / m) for m in sections for j in range(m)]
-    return (ctypes.c_double * max(len(f), 1))(*f)
-
-
-def _rotate(tensors, sections, base, freqs, origin, groups, interleaved, out, inverse):
-    torch = _b._torch()
-    if not 1 <= len(tensors) <= 4:
-        raise ValueError(f"one to four tensors, got {len(tensors)}")
-    x = tensors[0]
-    for i, t in enumerate(tensors):
-        _b._dev_tensor(t, f"tensor {i}")
-        if t.dim() not in (4, 5) or t.shape[1:] != x.shape[1:]:
-            raise ValueError("tensors must be [S, H, W, d] or [S, T, H, W, d] of one grid and width, got "
-                             f"{tuple(t.shape)} and {tuple(x.shape)}")
-        if t.dtype != x.dtype:
-            raise TypeError("tensors must share a dtype")
-    dev, code = x.device, _b._dtype_code(x)
-    T, H, W, d = (1,) * (5 - x.dim()) + tuple(x.shape[1:])
-    groups = int(groups)
-    if groups < 1 or d % groups:
-        raise ValueError(f"{d} channels do not split into {groups} groups")
-    if sections is None:  # all pairs; an axis each for height and width, or for time, height and width
-        pairs = d // groups // 2
-        nh = pairs // (2 if x.dim() == 4 else 3)
-        nw = pairs - nh if x.dim() == 4 else nh
+@functools.lru_cache(maxsize=256)
+def _pairs(sections, freqs, base, pairs, axes):
+    """The host arrays of a rotation's channel pairs: (sections, freqs).  ``sections`` None: all ``pairs``, shared among the
+    grid's ``axes``; ``freqs`` None: base ** (-j / m) for pair j of an axis with m."""
+    if sections is None:
+        nh = pairs // axes
+        nw = pairs - nh if axes == 2 else nh
         sections = (pairs - nh - nw, nh, nw)
-    sections = tuple(int(n) for n in sections)
     if len(sections) == 2:
         sections = (0,) + sections
     if len(sections) != 3 or min(sections) < 0:
@@ -50,37 +28,58 @@ def _rotate(tensors, sections, base, freqs, origin, groups, interleaved, out, in
     if freqs is None:
         if not base > 0:
             raise ValueError("base must be positive")
-        freqs = _frequencies(sections, float(base))
-    else:
-        freqs = [float(f) for f in freqs]
-        if len(freqs) != sum(sections):
-            raise ValueError(f"{sum(sections)} pairs need as many freqs, got {len(freqs)}")
-        freqs = (ctypes.c_double * max(len(freqs), 1))(*freqs)
+        freqs = tuple(base ** (-j / m) for m in sections for j in range(m))
+    if len(freqs) != sum(sections):
+        raise ValueError(f"{sum(sections)} pairs need as many freqs, got {len(freqs)}")
+    return (ctypes.c_int * 3)(*sections), (ctypes.c_double * max(len(freqs), 1))(*freqs)
+
+
+_POINTERS = [ctypes.c_void_p * n for n in range(5)]
+_INTS = [ctypes.c_int * n for n in range(5)]
+
+
+def _rotate(tensors, sections, base, freqs, origin, groups, interleaved, out, inverse):
+    torch = _b._torch()
+    n = len(tensors)
+    if not 1 <= n <= 4:
+        raise ValueError(f"one to four tensors, got {n}")
+    x = tensors[0]
+    kind, index, ndim, grid = x.dtype, x.get_device(), x.dim(), x.shape[1:]
+    for i, t in enumerate(tensors):
+        _b._plain(f"tensor {i}", t, ndim, kind, index)
+        if ndim not in (4, 5) or t.shape[1:] != grid:
+            raise ValueError("tensors must be [S, H, W, d] or [S, T, H, W, d] of one grid and width, got "
+                             f"{tuple(t.shape)} and {tuple(x.shape)}")
+    code = _b._dtype_code(x)
+    T, H, W, d = grid if ndim == 5 else (1, *grid)
+    groups = int(groups)
+    if groups < 1 or d % groups:
+        raise ValueError(f"{d} channels do not split into {groups} groups")
+    parts, turns = _pairs(None if sections is None else tuple(map(int, sections)), None if freqs is None else tuple(map(float, freqs)),
+                          float(base), d // groups // 2, ndim - 2)
     rows, at = 0, None
     if isinstance(origin, torch.Tensor):
-        _b._dev_tensor(origin, "origin")
-        if origin.dtype != torch.int32 or origin.dim() > 2 or origin.shape[-1:] != (3,):
+        _b._plain("origin", origin, origin.dim(), torch.int32, index)
+        if origin.dim() not in (1, 2) or origin.shape[-1] != 3:
             raise ValueError("origin must be int32 [3], [1, 3] or [S, 3]: time, height, width")
         rows = origin.numel() // 3
     else:
-        at = tuple(int(n) for n in origin)
-        at = (ctypes.c_int * 3)(*((0,) * (3 - len(at)) + at))
+        at = tuple(int(a) for a in origin)
+        at = _INTS[3](*((0,) * (3 - len(at)) + at))
         origin = None
     if out is None:
         out = [torch.empty_like(t) for t in tensors]
     else:
         out = [out] if isinstance(out, torch.Tensor) else list(out)
-        if len(out) != len(tensors):
-            raise ValueError(f"{len(tensors)} tensors need as many outputs, got {len(out)}")
+        if len(out) != n:
+            raise ValueError(f"{n} tensors need as many outputs, got {len(out)}")
         for i, (o, t) in enumerate(zip(out, tensors)):
-            _b._check_buffer(o, f"out {i}", t.shape, t.dtype)
-    for i, (t, o) in enumerate(zip(tensors, out)):
-        _b._same_device(dev, **{f"tensor {i}": t, f"out {i}": o, "origin": origin})
-    n = len(tensors)
-    _b._call(_b.lib().scram_rotary, "scram_rotary", dev,
-             (n, (ctypes.c_void_p * n)(*(t.data_ptr() for t in tensors)), (ctypes.c_void_p * n)(*(t.data_ptr() for t in out)),
-              (ctypes.c_int * n)(*(t.shape[0] for t in tensors)), code, T, H, W, d, groups, (ctypes.c_int * 3)(*sections), freqs,
-              at, _b._ptr(origin), rows, (ROTARY_INTERLEAVED if interleaved else 0) | (ROTARY_INVERSE if inverse else 0)))
+            if _b._plain(f"out {i}", o, ndim, kind, index).shape != t.shape:
+                raise ValueError(f"out {i} must be {tuple(t.shape)}, got {tuple(o.shape)}")
+    _b._call(_b.lib().scram_rotary, "scram_rotary", x.device,
+             (n, _POINTERS[n](*[t.data_ptr() for t in tensors]), _POINTERS[n](*[t.data_ptr() for t in out]),
+              _INTS[n](*[t.shape[0] for t in tensors]), code, T, H, W, d, groups, parts, turns, at, _b._ptr(origin), rows,
+              (ROTARY_INTERLEAVED if interleaved else 0) | (ROTARY_INVERSE if inverse else 0)))
     return tuple(out) if n > 1 else out[0]
 
 
@@ -107,26 +106,26 @@ def rotary_backward(*grads, sections=None, base: float = 10000.0, freqs=None, or
     return _rotate(grads, sections, base, freqs, origin, groups, interleaved, out, True)
 
 
-def _norm_rows(X, weight, bias, **more):
+def _norm_rows(X, weight, bias, out):
+    """Checks of a norm's tensors: (rows, channels, dtype code, weights' dtype code, device index)."""
     torch = _b._torch()
-    _b._dev_tensor(X, "X")
-    if X.dim() < 1:
+    index, kind, shape = X.get_device(), X.dtype, X.shape
+    _b._plain("X", X, X.dim(), kind, index)
+    if not shape:
         raise ValueError("X must have channels")
-    C = X.shape[-1]
-    code = _b._dtype_code(X)
-    wcode = code
-    for name, t in (("weight", weight), ("bias", bias)):
-        if t is not None:
-            _b._dev_tensor(t, name, 1)
-            if t.shape[0] != C:
+    C = shape[-1]
+    code = wcode = _b._dtype_code_of(kind)
+    if weight is not None or bias is not None:
+        wkind = bias.dtype if weight is None else weight.dtype
+        if wkind != kind and wkind != torch.float32:
+            raise TypeError("weight and bias must be float32 or of X's dtype")
+        wcode = _b._dtype_code_of(wkind)
+        for name, t in (("weight", weight), ("bias", bias)):
+            if t is not None and _b._plain(name, t, 1, wkind, index).shape[0] != C:
                 raise ValueError(f"{name} must have {C} channels, got {t.shape[0]}")
-            if t.dtype not in (X.dtype, torch.float32):
-                raise TypeError(f"{name} must be float32 or of X's dtype")
-            if weight is not None and t.dtype != weight.dtype:
-                raise TypeError("weight and bias must share a dtype")
-            wcode = _b._dtype_code(t)
-    _b._same_device(X.device, weight=weight, bias=bias, **more)
-    return X.numel() // C if C else 0, C, code, wcode
+    if out is not None and out.shape != shape:
+        raise ValueError(f"out must be {tuple(shape)}, got {tuple(out.shape)}")
+    return X.numel() // C if C else 0, C, code, wcode, index
 
 
 def layer_norm(X, weight=None, bias=None, eps: float = 1e-5, *, out=None, stats: bool = False):
@@ -136,16 +135,18 @@ def layer_norm(X, weight=None, bias=None, eps: float = 1e-5, *, out=None, stats:
     ``stats`` ``(rows, mean, rstd)``: fp32 of ``X.shape[:-1]``, for :func:`layer_norm_backward`.  ``out`` may be ``X``.
     """
     torch = _b._torch()
-    rows, C, code, wcode = _norm_rows(X, weight, bias, out=out)
+    rows, C, code, wcode, index = _norm_rows(X, weight, bias, out)
     if out is None:
         out = torch.empty_like(X)
     else:
-        _b._check_buffer(out, "out", X.shape, X.dtype)
+        _b._plain("out", out, X.dim(), X.dtype, index)
     mean = rstd = None
     if stats:
-        mean, rstd = (torch.empty(X.shape[:-1], dtype=torch.float32, device=X.device) for _ in range(2))
+        mean = torch.empty(X.shape[:-1], dtype=torch.float32, device=X.device)
+        rstd = torch.empty_like(mean)
     _b._call(_b.lib().scram_layer_norm, "scram_layer_norm", X.device,
-             (_b._ptr(X), code, _b._ptr(weight), _b._ptr(bias), wcode, rows, C, float(eps), _b._ptr(out), _b._ptr(mean), _b._ptr(rstd)))
+             (X.data_ptr(), code, _b._ptr(weight), _b._ptr(bias), wcode, rows, C, float(eps), out.data_ptr(), _b._ptr(mean),
+              _b._ptr(rstd)))
     return (out, mean, rstd) if stats else out
 
 
@@ -157,23 +158,28 @@ def layer_norm_backward(dY, X, mean, rstd, weight=None, *, out=None, workspace=N
     ``workspace``: optional uint8 device tensor of at least ``layer_norm_backward_workspace_bytes(rows, channels)`` bytes.
     """
     torch = _b._torch()
-    rows, C, code, wcode = _norm_rows(X, weight, None, dY=dY, mean=mean, rstd=rstd, out=out, workspace=workspace)
-    _b._dev_tensor(dY, "dY")
-    if dY.shape != X.shape:
-        raise ValueError(f"dY must be {tuple(X.shape)}, got {tuple(dY.shape)}")
-    if dY.dtype not in (X.dtype, torch.float32):
+    rows, C, code, wcode, index = _norm_rows(X, weight, None, out)
+    kind, gkind, dev = X.dtype, dY.dtype, X.device
+    if gkind != kind and gkind != torch.float32:
         raise TypeError("dY must be float32 or of X's dtype")
+    if _b._plain("dY", dY, X.dim(), gkind, index).shape != X.shape:
+        raise ValueError(f"dY must be {tuple(X.shape)}, got {tuple(dY.shape)}")
     for name, t in (("mean", mean), ("rstd", rstd)):
-        _b._check_buffer(t, name, X.shape[:-1], torch.float32)
+        if _b._plain(name, t, X.dim() - 1, torch.float32, index).shape != X.shape[:-1]:
+            raise ValueError(f"{name} must be {tuple(X.shape[:-1])}, got {tuple(t.shape)}")
     if out is None:
         out = torch.empty_like(dY)
     else:
-        _b._check_buffer(out, "out", dY.shape, dY.dtype)
-    dweight, dbias = (torch.empty(C, dtype=torch.float32, device=X.device) for _ in range(2))
-    workspace = _b._workspace(workspace, layer_norm_backward_workspace_bytes(rows, C), X.device)
-    _b._call(_b.lib().scram_layer_norm_backward, "scram_layer_norm_backward", X.device,
-             (_b._ptr(dY), _b._dtype_code(dY), _b._ptr(X), code, _b._ptr(mean), _b._ptr(rstd), _b._ptr(weight), wcode, rows, C,
-              _b._ptr(out), _b._ptr(dweight), _b._ptr(dbias), _b._ptr(workspace), workspace.numel() * workspace.element_size()))
+        _b._plain("out", out, X.dim(), gkind, index)
+    dweight = torch.empty(C, dtype=torch.float32, device=dev)
+    dbias = torch.empty_like(dweight)
+    if workspace is None:
+        workspace = torch.empty(layer_norm_backward_workspace_bytes(rows, C), dtype=torch.uint8, device=dev)
+    else:
+        _b._workspace(workspace, 0, dev)
+    _b._call(_b.lib().scram_layer_norm_backward, "scram_layer_norm_backward", dev,
+             (dY.data_ptr(), _b._dtype_code_of(gkind), X.data_ptr(), code, mean.data_ptr(), rstd.data_ptr(), _b._ptr(weight), wcode, rows,
+              C, out.data_ptr(), dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size()))
     return out, dweight, dbias
 
 
