@@ -4,9 +4,11 @@
 //   g = dy w:  dx = r (g - mean g - xh mean(g xh)),  dw = sum_rows dy xh,  db = sum_rows dy
 //
 // A row stays in registers between its passes, so every input is read once:
-// bound by memory.  A row is held by `lanes` threads (a power of two), V
-// neighbouring channels a chunk and up to 16 channels a thread; several rows
-// share a wave, or several waves a row.  Sums are fp32: the two of the forward
+// bound by memory.  A row is held by `lanes` threads (a power of two), in
+// chunks of 16 bytes of X, up to 16 channels a thread; several rows share a
+// wave, or several waves a row.  Chunks are read and written whole wherever
+// the row starts (memory takes vectors at any element's address), but for the
+// last one of a row that does not end with a whole one.  Sums are fp32: the two of the forward
 // pass are of the row and then of its centred values, so that a row's offset
 // costs no accuracy.
 //
@@ -39,8 +41,12 @@ struct NormParams {
     float eps;
 };
 
+template <typename T>
+constexpr int kChunk = 16 / static_cast<int>(sizeof(T));  // channels of a chunk of X
+
+// V channels at any element's address.
 template <typename T, int V>
-using vec = T __attribute__((ext_vector_type(V)));
+using vec = T __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 
 template <typename T>
 __device__ __forceinline__ float norm_float(T x)
@@ -60,16 +66,10 @@ __device__ __forceinline__ T norm_round(float x)
         return static_cast<T>(f32_to_bf16_rne(x));
 }
 
-// Element i of a weight vector of either type.
-__device__ __forceinline__ float norm_weight(const void* w, int f32, int i)
-{
-    return f32 ? static_cast<const float*>(w)[i] : norm_float(static_cast<const uint16_t*>(w)[i]);
-}
-
 // Sums of N values over the `lanes` threads of a row, on all of them.  Rows of several waves pass through LDS, in one of
 // two halves in turn so that one barrier per sum is enough.
-template <int N, bool WIDE>
-__device__ __forceinline__ void row_sum(float (&x)[N], int lanes, float (*lds)[kNormThreads / 64][N], int& half)
+template <int N, bool WIDE, typename Lds>
+__device__ __forceinline__ void row_sum(float (&x)[N], int lanes, Lds& lds, int& half)
 {
     for (int m = 1; m < (WIDE ? 64 : lanes); m <<= 1)
 #pragma unroll
@@ -90,137 +90,249 @@ __device__ __forceinline__ void row_sum(float (&x)[N], int lanes, float (*lds)[k
     }
 }
 
-// Every thread of a block takes part in every row of its loop (the sums of wide rows hold barriers); rows past the end
-// are neither read nor written.
-template <typename T, int V, int NC, bool WIDE>
-__global__ __launch_bounds__(WIDE ? kNormThreads : kBlock) void norm_kernel(NormParams p)
+// How many threads hold a row: a part of a wave, a chunk each; a wave; two or four waves; up to the whole block.
+enum NormLayout { kNarrow = 0, kWave = 1, kWide = 2, kHuge = 3 };
+
+constexpr int norm_threads(int layout) { return layout == kHuge ? kNormThreads : kBlock; }
+constexpr bool norm_wide(int layout) { return layout >= kWide; }
+
+// Rows per pass of a block's loop: their loads are in flight together, and wide rows share their barriers.  (262144 x 64,
+// forward: a row at a time 26 us, four 16; 8192 x 4096 backward: one 57 us, two 50.)
+constexpr int norm_rows(int layout, bool backward) { return layout == kHuge ? 1 : layout == kNarrow && !backward ? 4 : 2; }
+
+// N channels at `row` into x from element o on (o a multiple of N below V, the same for every thread).
+template <int N, typename T, int V>
+__device__ __forceinline__ void load_piece(const T* row, int o, vec<T, V>& x)
 {
-    using Vec = vec<T, V>;
-    __shared__ float s_sum[2][kNormThreads / 64][1];
-    int half = 0;
-    const int lane = threadIdx.x & (p.lanes - 1);
-    const int slots = blockDim.x / p.lanes, slot = threadIdx.x / p.lanes;
-    const int chunks = p.C / V;
-    const float inv_c = 1.f / static_cast<float>(p.C);
-    float w[NC][V], b[NC][V];
+    const vec<T, N> y = *reinterpret_cast<const vec<T, N>*>(row + o);
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int q = 0; q < V; q += N)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int at = min(lane + c * p.lanes, chunks - 1) * V + j;
-            w[c][j] = p.weight ? norm_weight(p.weight, p.weight_f32, at) : 1.f;
-            b[c][j] = p.bias ? norm_weight(p.bias, p.weight_f32, at) : 0.f;
-        }
-    for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * slots; r0 < p.rows; r0 += static_cast<int64_t>(gridDim.x) * slots) {
-        const int64_t row = r0 + slot;
-        const bool live = row < p.rows;
-        const T* const x = static_cast<const T*>(p.X) + row * p.C;
-        float v[NC][V];
-        float sum[1] = {0.f};
+        for (int j = 0; j < N; ++j) x[q + j] = q == o ? static_cast<T>(y[j]) : static_cast<T>(x[q + j]);
+}
+
+template <int N, typename T, int V>
+__device__ __forceinline__ void store_piece(T* row, int o, const vec<T, V>& x)
+{
+    vec<T, N> y(T(0));
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int at = lane + c * p.lanes;
-            Vec a = {};
-            if (live && at < chunks) a = reinterpret_cast<const Vec*>(x)[at];
+    for (int q = 0; q < V; q += N)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[c][j] = norm_float(static_cast<T>(a[j]));
-                sum[0] += v[c][j];
-            }
-        }
-        row_sum<1, WIDE>(sum, p.lanes, s_sum, half);
-        const float mean = sum[0] * inv_c;
-        sum[0] = 0.f;
+        for (int j = 0; j < N; ++j) y[j] = q == o ? static_cast<T>(x[q + j]) : static_cast<T>(y[j]);
+    *reinterpret_cast<vec<T, N>*>(row + o) = y;
+}
+
+// Channels at .. at + V - 1 of a row of C, those that it has, zeros after them.  TAIL: C is not a multiple of V, and the
+// last C mod V channels come in pieces of 4, 2 and 1.
+template <bool TAIL, int V, typename T>
+__device__ __forceinline__ vec<T, V> load_chunk(const T* row, int at, int C)
+{
+    if (!TAIL || at + V <= C) return *reinterpret_cast<const vec<T, V>*>(row + at);
+    vec<T, V> x(T(0));
+    const int rest = C % V;
+    if constexpr (V > 4)
+        if (rest & 4) load_piece<4, T, V>(row + at, 0, x);
+    if (rest & 2) load_piece<2, T, V>(row + at, rest & 4, x);
+    if (rest & 1) load_piece<1, T, V>(row + at, rest & 6, x);
+    return x;
+}
+
+template <bool TAIL, int V, typename T>
+__device__ __forceinline__ void store_chunk(T* row, int at, int C, vec<T, V> x)
+{
+    if (!TAIL || at + V <= C) {
+        *reinterpret_cast<vec<T, V>*>(row + at) = x;
+        return;
+    }
+    const int rest = C % V;
+    if constexpr (V > 4)
+        if (rest & 4) store_piece<4, T, V>(row + at, 0, x);
+    if (rest & 2) store_piece<2, T, V>(row + at, rest & 4, x);
+    if (rest & 1) store_piece<1, T, V>(row + at, rest & 6, x);
+}
+
+// The thread's weights (or `none` without any).
+template <bool TAIL, int V, int NC>
+__device__ __forceinline__ void load_weights(const void* w, const NormParams& p, int lane, float none, float (&out)[NC][V])
+{
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const bool in = lane + c * p.lanes < chunks;
+    for (int c = 0; c < NC; ++c) {
+        const int at = (lane + c * p.lanes) * V;
+        if (w != nullptr && at >= p.C) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[c][j] -= mean;
-                sum[0] = in ? fmaf(v[c][j], v[c][j], sum[0]) : sum[0];
-            }
-        }
-        row_sum<1, WIDE>(sum, p.lanes, s_sum, half);
-        const float rstd = 1.f / sqrtf(sum[0] * inv_c + p.eps);
-        if (!live) continue;
-        T* const y = static_cast<T*>(p.out) + row * p.C;
+            for (int j = 0; j < V; ++j) out[c][j] = 0.f;
+        } else if (w != nullptr && p.weight_f32) {
+            const vec<float, V> x = load_chunk<TAIL, V>(static_cast<const float*>(w), at, p.C);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int at = lane + c * p.lanes;
-            Vec a;
+            for (int j = 0; j < V; ++j) out[c][j] = x[j];
+        } else if (w != nullptr) {
+            const vec<uint16_t, V> x = load_chunk<TAIL, V>(static_cast<const uint16_t*>(w), at, p.C);
 #pragma unroll
-            for (int j = 0; j < V; ++j) a[j] = norm_round<T>(fmaf(v[c][j] * rstd, w[c][j], b[c][j]));
-            if (at < chunks) reinterpret_cast<Vec*>(y)[at] = a;
-        }
-        if (lane == 0 && p.mean) {
-            p.mean[row] = mean;
-            p.rstd[row] = rstd;
+            for (int j = 0; j < V; ++j) out[c][j] = norm_float(static_cast<uint16_t>(x[j]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) out[c][j] = none;
         }
     }
 }
 
-template <typename T, typename TG, int V, int NC, bool WIDE>
-__global__ __launch_bounds__(WIDE ? kNormThreads : kBlock) void norm_backward_kernel(NormParams p)
+// Every thread of a block takes part in every pass of its loop (the sums of wide rows hold barriers); rows past the end are
+// neither read nor written.
+template <typename T, int NC, int LAYOUT, bool TAIL>
+__global__ __launch_bounds__(norm_threads(LAYOUT)) void norm_kernel(NormParams p)
 {
+    constexpr int V = kChunk<T>;
     using Vec = vec<T, V>;
-    using VecG = vec<TG, V>;
-    __shared__ float s_sum[2][kNormThreads / 64][2];
-    __shared__ float s_part[WIDE ? kNormThreads : kBlock];
+    constexpr bool WIDE = norm_wide(LAYOUT);
+    constexpr int R = norm_rows(LAYOUT, false);
+    __shared__ float s_sum[2][WIDE ? norm_threads(LAYOUT) / 64 : 1][R];
     int half = 0;
     const int lane = threadIdx.x & (p.lanes - 1);
     const int slots = blockDim.x / p.lanes, slot = threadIdx.x / p.lanes;
-    const int chunks = p.C / V;
+    const float inv_c = 1.f / static_cast<float>(p.C);
+    float w[NC][V], b[NC][V];
+    load_weights<TAIL>(p.weight, p, lane, 1.f, w);
+    load_weights<TAIL>(p.bias, p, lane, 0.f, b);
+    const int64_t step = static_cast<int64_t>(slots) * R;
+    for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * step; r0 < p.rows; r0 += static_cast<int64_t>(gridDim.x) * step) {
+        const int64_t row = r0 + slot;  // and every slots-th row after it
+        Vec a[R][NC];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const T* const x = static_cast<const T*>(p.X) + (row + k * slots) * p.C;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int at = (lane + c * p.lanes) * V;
+                a[k][c] = Vec(T(0));
+                if (row + k * slots < p.rows && at < p.C) a[k][c] = load_chunk<TAIL, V>(x, at, p.C);
+            }
+        }
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            mean[k] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int j = 0; j < V; ++j) mean[k] += norm_float(static_cast<T>(a[k][c][j]));
+        }
+        row_sum<R, WIDE>(mean, p.lanes, s_sum, half);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            mean[k] *= inv_c;
+            rstd[k] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int left = p.C - (lane + c * p.lanes) * V;  // channels of the row from this chunk on
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float v = norm_float(static_cast<T>(a[k][c][j])) - mean[k];
+                    rstd[k] = (TAIL ? j : 0) < left ? fmaf(v, v, rstd[k]) : rstd[k];
+                }
+            }
+        }
+        row_sum<R, WIDE>(rstd, p.lanes, s_sum, half);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            rstd[k] = 1.f / sqrtf(rstd[k] * inv_c + p.eps);
+            if (row + k * slots >= p.rows) continue;
+            T* const y = static_cast<T*>(p.out) + (row + k * slots) * p.C;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int at = (lane + c * p.lanes) * V;
+                Vec o;
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    o[j] = norm_round<T>(fmaf((norm_float(static_cast<T>(a[k][c][j])) - mean[k]) * rstd[k], w[c][j], b[c][j]));
+                if (at < p.C) store_chunk<TAIL, V>(y, at, p.C, o);
+            }
+            if (lane == 0 && p.mean) {
+                p.mean[row + k * slots] = mean[k];
+                p.rstd[row + k * slots] = rstd[k];
+            }
+        }
+    }
+}
+
+template <typename T, typename TG, int NC, int LAYOUT, bool TAIL>
+__global__ __launch_bounds__(norm_threads(LAYOUT)) void norm_backward_kernel(NormParams p)
+{
+    constexpr int V = kChunk<T>;
+    using Vec = vec<T, V>;
+    using VecG = vec<TG, V>;
+    constexpr bool WIDE = norm_wide(LAYOUT);
+    constexpr int R = norm_rows(LAYOUT, true);
+    __shared__ float s_sum[2][WIDE ? norm_threads(LAYOUT) / 64 : 1][2 * R];
+    __shared__ float s_part[norm_threads(LAYOUT)];
+    int half = 0;
+    const int lane = threadIdx.x & (p.lanes - 1);
+    const int slots = blockDim.x / p.lanes, slot = threadIdx.x / p.lanes;
     const float inv_c = 1.f / static_cast<float>(p.C);
     float w[NC][V], dw[NC][V], db[NC][V];
+    load_weights<TAIL>(p.weight, p, lane, 1.f, w);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int at = min(lane + c * p.lanes, chunks - 1) * V + j;
-            w[c][j] = p.weight ? norm_weight(p.weight, p.weight_f32, at) : 1.f;
-            dw[c][j] = db[c][j] = 0.f;
-        }
-    for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * slots; r0 < p.rows; r0 += static_cast<int64_t>(gridDim.x) * slots) {
+        for (int j = 0; j < V; ++j) dw[c][j] = db[c][j] = 0.f;
+    const int64_t step = static_cast<int64_t>(slots) * R;
+    for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * step; r0 < p.rows; r0 += static_cast<int64_t>(gridDim.x) * step) {
         const int64_t row = r0 + slot;
-        const bool live = row < p.rows;
-        float xh[NC][V], g[NC][V];
-        float sum[2] = {0.f, 0.f};
-        const float mean = live ? p.mean_in[row] : 0.f, rstd = live ? p.rstd_in[row] : 0.f;
+        Vec a[R][NC];
+        VecG d[R][NC];
+        float mean[R], rstd[R], sum[2 * R];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int at = lane + c * p.lanes;
-            Vec a = {};
-            VecG d = {};
-            const bool in = live && at < chunks;
-            if (in) {
-                a = reinterpret_cast<const Vec*>(static_cast<const T*>(p.X) + row * p.C)[at];
-                d = reinterpret_cast<const VecG*>(static_cast<const TG*>(p.dY) + row * p.C)[at];
+        for (int k = 0; k < R; ++k) {
+            const int64_t at_row = row + k * slots;
+            const bool live = at_row < p.rows;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int at = (lane + c * p.lanes) * V;
+                a[k][c] = Vec(T(0));
+                d[k][c] = VecG(TG(0));
+                if (live && at < p.C) {
+                    a[k][c] = load_chunk<TAIL, V>(static_cast<const T*>(p.X) + at_row * p.C, at, p.C);
+                    d[k][c] = load_chunk<TAIL, V>(static_cast<const TG*>(p.dY) + at_row * p.C, at, p.C);
+                }
             }
+            mean[k] = live ? p.mean_in[at_row] : 0.f;
+            rstd[k] = live ? p.rstd_in[at_row] : 0.f;
+        }
+        auto xhat = [&](int k, int c, int j) { return (norm_float(static_cast<T>(a[k][c][j])) - mean[k]) * rstd[k]; };
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float dy = norm_float(static_cast<TG>(d[j]));
-                xh[c][j] = in ? (norm_float(static_cast<T>(a[j])) - mean) * rstd : 0.f;
-                dw[c][j] = fmaf(dy, xh[c][j], dw[c][j]);
-                db[c][j] += dy;
-                g[c][j] = dy * w[c][j];
-                sum[0] += g[c][j];
-                sum[1] = fmaf(g[c][j], xh[c][j], sum[1]);
+        for (int k = 0; k < R; ++k) {
+            sum[2 * k] = sum[2 * k + 1] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    // (past the end of the row, or of the rows, dY is 0 and xh finite: nothing is added)
+                    const float dy = norm_float(static_cast<TG>(d[k][c][j])), xh = xhat(k, c, j);
+                    dw[c][j] = fmaf(dy, xh, dw[c][j]);
+                    db[c][j] += dy;
+                    const float g = dy * w[c][j];
+                    sum[2 * k] += g;
+                    sum[2 * k + 1] = fmaf(g, xh, sum[2 * k + 1]);
+                }
             }
         }
-        row_sum<2, WIDE>(sum, p.lanes, s_sum, half);
-        const float mg = sum[0] * inv_c, mx = sum[1] * inv_c;
-        if (!live) continue;
-        TG* const dx = static_cast<TG*>(p.out) + row * p.C;
+        row_sum<2 * R, WIDE>(sum, p.lanes, s_sum, half);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int at = lane + c * p.lanes;
-            VecG d;
+        for (int k = 0; k < R; ++k) {
+            if (row + k * slots >= p.rows) continue;
+            const float mg = sum[2 * k] * inv_c, mx = sum[2 * k + 1] * inv_c;
+            TG* const dx = static_cast<TG*>(p.out) + (row + k * slots) * p.C;
 #pragma unroll
-            for (int j = 0; j < V; ++j) d[j] = norm_round<TG>(rstd * (g[c][j] - mg - xh[c][j] * mx));
-            if (at < chunks) reinterpret_cast<VecG*>(dx)[at] = d;
+            for (int c = 0; c < NC; ++c) {
+                const int at = (lane + c * p.lanes) * V;
+                VecG o;
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    o[j] = norm_round<TG>(rstd[k] * (norm_float(static_cast<TG>(d[k][c][j])) * w[c][j] - mg - xhat(k, c, j) * mx));
+                if (at < p.C) store_chunk<TAIL, V>(dx, at, p.C, o);
+            }
         }
     }
-    // the block's parts: over the threads that hold the same channels
+    // the block's parts: over the threads that hold the same channels, first those of a wave
     float* const parts = p.parts + static_cast<size_t>(blockIdx.x) * 2 * p.C;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -228,15 +340,18 @@ __global__ __launch_bounds__(WIDE ? kNormThreads : kBlock) void norm_backward_ke
         for (int j = 0; j < V; ++j)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                __syncthreads();
-                s_part[threadIdx.x] = k ? db[c][j] : dw[c][j];
-                __syncthreads();
-                const int at = lane + c * p.lanes;
-                if (slot == 0 && at < chunks) {
-                    float x = 0.f;
-                    for (int i = 0; i < slots; ++i) x += s_part[lane + i * p.lanes];
-                    parts[static_cast<size_t>(k) * p.C + at * V + j] = x;
+                float x = k ? db[c][j] : dw[c][j];
+                for (int m = p.lanes; m < 64; m <<= 1) x += __shfl_xor(x, m);
+                const int group = p.lanes < 64 ? 64 : p.lanes;  // threads that hold different channels or a wave's sums
+                if (slots > 1 && group < static_cast<int>(blockDim.x)) {
+                    __syncthreads();
+                    s_part[threadIdx.x] = x;
+                    __syncthreads();
+                    if (threadIdx.x < static_cast<uint32_t>(group))
+                        for (int i = threadIdx.x + group; i < static_cast<int>(blockDim.x); i += group) x += s_part[i];
                 }
+                const int at = (lane + c * p.lanes) * V + j;
+                if (slot == 0 && at < p.C) parts[static_cast<size_t>(k) * p.C + at] = x;
             }
 }
 
@@ -246,8 +361,10 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* parts, in
     __shared__ float s[32][33];
     const int col = blockIdx.x * 32 + (threadIdx.x & 31), first = threadIdx.x >> 5;
     float x = 0.f;
-    if (col < 2 * C)
+    if (col < 2 * C) {
+#pragma unroll 8
         for (int i = first; i < blocks; i += 32) x += parts[static_cast<size_t>(i) * 2 * C + col];
+    }
     s[first][threadIdx.x & 31] = x;
     __syncthreads();
     if (first == 0 && col < 2 * C) {
@@ -257,35 +374,33 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* parts, in
     }
 }
 
-// How a row is held: V channels a chunk (the most, up to 16 bytes of X, that divide the row and to which the tensors are
-// aligned), `chunks` chunks of a row over `lanes` threads, one chunk a thread where a block has enough.
+// How a row is held: its chunks over `lanes` threads, one a thread up to a wave's width, then up to 16 channels a thread.
 struct NormPlan {
-    int v, lanes;
-    bool many;  // several chunks a thread
+    int lanes, layout;
 };
 
-NormPlan norm_plan(const NormCall& c, const void* out)
+NormPlan norm_plan(const NormCall& c)
 {
-    const int elem = c.dtype == SCRAM_BF16 ? 2 : 4;
-    const int grad = c.dY ? (c.grad_dtype == SCRAM_BF16 ? 2 : 4) : elem;
-    auto fits = [&](int n) {
-        return c.channels % n == 0 && reinterpret_cast<uintptr_t>(c.X) % (n * elem) == 0 &&
-               reinterpret_cast<uintptr_t>(out) % (n * grad) == 0 && reinterpret_cast<uintptr_t>(c.dY) % (n * grad) == 0;
-    };
-    NormPlan plan{16 / elem, 1, false};
-    while (plan.v > 1 && !fits(plan.v)) plan.v /= 2;
-    const int chunks = c.channels / plan.v;
-    // one chunk a thread up to a wave's width, then up to 16 channels a thread, then more waves
-    plan.many = chunks > 64;
+    const int chunk = c.dtype == SCRAM_BF16 ? kChunk<uint16_t> : kChunk<float>;
+    const int chunks = (c.channels + chunk - 1) / chunk;
+    NormPlan plan{1, kNarrow};
     while (plan.lanes < 64 && plan.lanes < chunks) plan.lanes *= 2;
-    while (plan.many && plan.lanes * (kPerThread / plan.v) < chunks) plan.lanes *= 2;
+    if (chunks > 64) {
+        while (plan.lanes * (kPerThread / chunk) < chunks) plan.lanes *= 2;
+        plan.layout = plan.lanes <= 64 ? kWave : plan.lanes <= kBlock ? kWide : kHuge;
+    }
     return plan;
 }
 
-int norm_threads(const NormPlan& plan) { return plan.lanes > 256 ? plan.lanes : 256; }
+int block_threads(const NormPlan& plan) { return plan.layout == kHuge ? plan.lanes : kBlock; }
 
-// Blocks of the backward pass: each writes a row of parts.
-int64_t norm_backward_blocks(int64_t rows) { return rows < 512 ? rows : 512; }
+// Blocks of the backward pass, each of which writes a row of parts: two per CU, or one where a row takes more than 256
+// threads.  (8192 x 4096: 512 blocks 50 us, 256 64, 768 64; 2048 x 16384: 256 blocks 70, 512 94.)
+int64_t norm_backward_blocks(int64_t rows, int channels)
+{
+    const int64_t most = channels > kPerThread * kBlock ? 256 : 512;
+    return rows < most ? rows : most;
+}
 
 NormParams norm_params(const NormCall& c, const NormPlan& plan)
 {
@@ -302,40 +417,37 @@ NormParams norm_params(const NormCall& c, const NormPlan& plan)
     return p;
 }
 
-// f(V, NC, WIDE) for a plan of type T
+// f(NC, LAYOUT, TAIL) for a plan of type T
 template <typename T, typename F>
-hipError_t norm_dispatch(const NormPlan& plan, F&& f)
+hipError_t norm_dispatch(const NormPlan& plan, int channels, F&& f)
 {
     using std::integral_constant;
-    auto with = [&](auto v) {
-        constexpr int V = decltype(v)::value;
-        if (!plan.many) return f(v, integral_constant<int, 1>{}, std::false_type{});
-        if (plan.lanes <= 64) return f(v, integral_constant<int, kPerThread / V>{}, std::false_type{});
-        return f(v, integral_constant<int, kPerThread / V>{}, std::true_type{});
+    constexpr integral_constant<int, kPerThread / kChunk<T>> many{};
+    auto with = [&](auto tail) {
+        if (plan.layout == kNarrow) return f(integral_constant<int, 1>{}, integral_constant<int, kNarrow>{}, tail);
+        if (plan.layout == kWave) return f(many, integral_constant<int, kWave>{}, tail);
+        if (plan.layout == kWide) return f(many, integral_constant<int, kWide>{}, tail);
+        return f(many, integral_constant<int, kHuge>{}, tail);
     };
-    if constexpr (sizeof(T) == 2)
-        if (plan.v == 8) return with(integral_constant<int, 8>{});
-    if (plan.v == 4) return with(integral_constant<int, 4>{});
-    if (plan.v == 2) return with(integral_constant<int, 2>{});
-    return with(integral_constant<int, 1>{});
+    return channels % kChunk<T> ? with(std::true_type{}) : with(std::false_type{});
 }
 
 }  // namespace
 
 hipError_t launch_norm(const NormCall& c, void* Y, float* mean, float* rstd, hipStream_t stream)
 {
-    const NormPlan plan = norm_plan(c, Y);
+    const NormPlan plan = norm_plan(c);
     NormParams p = norm_params(c, plan);
     p.out = Y;
     p.mean = mean;
     p.rstd = rstd;
-    const int threads = norm_threads(plan);
-    const int64_t slots = threads / plan.lanes, want = (c.rows + slots - 1) / slots;
-    const dim3 grid(static_cast<uint32_t>(want < 8192 ? want : 8192));
+    const int threads = block_threads(plan);
+    const int64_t slots = threads / plan.lanes, want = (c.rows + slots * 2 - 1) / (slots * 2);
+    const dim3 grid(static_cast<uint32_t>(want < 4096 ? want : 4096));
     auto run = [&](auto type) {
         using T = decltype(type);
-        return norm_dispatch<T>(plan, [&](auto v, auto nc, auto wide) {
-            hipLaunchKernelGGL((norm_kernel<T, decltype(v)::value, decltype(nc)::value, decltype(wide)::value>), grid, dim3(threads), 0,
+        return norm_dispatch<T>(plan, c.channels, [&](auto nc, auto layout, auto tail) {
+            hipLaunchKernelGGL((norm_kernel<T, decltype(nc)::value, decltype(layout)::value, decltype(tail)::value>), grid, dim3(threads), 0,
                                stream, p);
             return hipGetLastError();
         });
@@ -345,25 +457,25 @@ hipError_t launch_norm(const NormCall& c, void* Y, float* mean, float* rstd, hip
 
 size_t norm_backward_workspace_bytes(int64_t rows, int channels)
 {
-    return static_cast<size_t>(norm_backward_blocks(rows)) * 2 * channels * sizeof(float);
+    return static_cast<size_t>(norm_backward_blocks(rows, channels)) * 2 * channels * sizeof(float);
 }
 
 hipError_t launch_norm_backward(const NormCall& c, const float* mean, const float* rstd, void* dX, float* dweight,
                                 float* dbias, void* workspace, hipStream_t stream)
 {
-    const NormPlan plan = norm_plan(c, dX);
+    const NormPlan plan = norm_plan(c);
     NormParams p = norm_params(c, plan);
     p.out = dX;
     p.mean_in = mean;
     p.rstd_in = rstd;
     p.parts = static_cast<float*>(workspace);
-    const int threads = norm_threads(plan);
-    const uint32_t blocks = static_cast<uint32_t>(norm_backward_blocks(c.rows));
+    const int threads = block_threads(plan);
+    const uint32_t blocks = static_cast<uint32_t>(norm_backward_blocks(c.rows, c.channels));
     auto run = [&](auto type, auto grad) {
         using T = decltype(type);
         using TG = decltype(grad);
-        return norm_dispatch<T>(plan, [&](auto v, auto nc, auto wide) {
-            hipLaunchKernelGGL((norm_backward_kernel<T, TG, decltype(v)::value, decltype(nc)::value, decltype(wide)::value>),
+        return norm_dispatch<T>(plan, c.channels, [&](auto nc, auto layout, auto tail) {
+            hipLaunchKernelGGL((norm_backward_kernel<T, TG, decltype(nc)::value, decltype(layout)::value, decltype(tail)::value>),
                                dim3(blocks), dim3(threads), 0, stream, p);
             return hipGetLastError();
         });
