@@ -25,7 +25,8 @@ struct DiffParams : BwdParams {
     int first;
     int tile_blocks;       // most blocks of 16 keys a wave walks on the matrix cores
     float4* stats;         // [n] log2 normaliser and D of both maps (gradients)
-    double* lam_part;      // [query blocks] their queries' sum of D of the second map
+    double* lam_part;      // [slices, parts] sums over some queries each of D of the second map
+    uint32_t slices, parts;
     float* dlam;           // [S]
 };
 

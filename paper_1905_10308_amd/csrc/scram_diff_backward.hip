@@ -288,14 +288,16 @@ diff_query_tile_kernel(DiffParams p)
     if (lane == 0) p.lam_part[one] = part;
 }
 
-// dlam of a slice: minus the sum of its query blocks' parts.  One block per slice.
-__global__ __launch_bounds__(kBlock) void diff_lam_kernel(const double* part, uint32_t blocks, float* dlam)
+// dlam of the slices: minus the sums of their parts, a block per slice at a time.
+__device__ __forceinline__ void slice_sums(const DiffParams& p)
 {
-    const double* const mine = part + static_cast<size_t>(blockIdx.x) * blocks;
-    double x = 0.0;
-    for (uint32_t i = threadIdx.x; i < blocks; i += kBlock) x += mine[i];
-    x = block_sum(x);
-    if (threadIdx.x == 0) dlam[blockIdx.x] = static_cast<float>(-x);
+    for (uint32_t s = blockIdx.x; s < p.slices; s += gridDim.x) {
+        double x = 0.0;
+        for (uint32_t i = threadIdx.x; i < p.parts; i += kBlock) x += p.lam_part[static_cast<size_t>(s) * p.parts + i];
+        x = block_sum(x);
+        if (threadIdx.x == 0) p.dlam[s] = static_cast<float>(-x);
+        __syncthreads();  // before the next sum's writes
+    }
 }
 
 // Contributions of kNb entries (slots x[t], valid where ok[t]) to dK_j, dV_j
@@ -436,10 +438,11 @@ __global__ __launch_bounds__(kBlock) void diff_key_kernel(DiffParams p)
 }
 
 // The keys of the list, a wave each: its lane groups take the entries in turn
-// and their sums are added up.
+// and their sums are added up.  And, as the last launch of a call, dlam.
 template <typename T, int D, int G, bool MULTI>
 __global__ __launch_bounds__(kBlock) void diff_heavy_kernel(DiffParams p)
 {
+    slice_sums(p);
     constexpr int N = 2 * Row<T, D, G>::kEpc;
     const int lane = threadIdx.x & (G - 1), member = (threadIdx.x & 63) / G;
     const int count = *p.n_heavy;
@@ -461,6 +464,246 @@ __global__ __launch_bounds__(kBlock) void diff_heavy_kernel(DiffParams p)
                 dv[i] += __shfl_xor(dv[i], mask);
             }
         if (member == 0) diff_store_key<T, D, G>(p, kg, lane, dk, dv);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Key side on the matrix cores, fp32 storage: the strips of scram_strip.h and the fp32 products (16x16x4), a chunk of 16
+// entries at a time (lane (m, g4)):
+//   S1^T, S2^T = Q_E K_w^T of each half, dP^T = dO_E V_w^T    lane group g4 contracts the channels g4 D / 8 .. of each half;
+//       lane: entries 4 g4 + i, key m
+//   dV_w += (P1 - lam P2) dO_E, dK_w += dS Q_E                step i contracts the entries 4 g4 + i.  Column m of channel tile
+//       o stands for a channel of half o / (tiles / 2): with 16 channels the one tile holds both, m < 8 and the others, and
+//       takes dS1 and dS2 in turn
+// A chunk's rows load while the previous chunk is in the matrix cores, the entry codes a chunk before that.  A strip of more
+// entries than p.heavy_entries, or whose sums are not finite, leaves its keys to the list.
+// ---------------------------------------------------------------------------
+template <int D, int MODE>
+struct DiffStripLds {
+    static constexpr int kRowF = D + 4;  // row stride, floats (padded)
+    __attribute__((aligned(16))) float q[kStripFE * kRowF], g[kStripFE * kRowF];
+    int4 meta[kStripFE];        // match row, match column, lse2 and D bits of the first map
+    float2 second[kStripFE];    // lse2, D of the second
+    int32_t el[MODE != kStripPlain ? kStripFE : 1][2];  // as in the bf16 kernel
+    int32_t lo[kStripMaxRows], pre[kStripMaxRows + 1];
+};
+
+// Products over N channels of a lane's row and key, sums of two in the matrix cores, added pairwise.
+template <int N>
+__device__ __forceinline__ f32x4_t diff_dots(const float* a, const float* b)
+{
+    if constexpr (N == 2) {
+        f32x4_t t = {0.f, 0.f, 0.f, 0.f};
+        t = __builtin_amdgcn_mfma_f32_16x16x4f32(a[0], b[0], t, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(a[1], b[1], t, 0, 0, 0);
+    } else {
+        return diff_dots<N / 2>(a, b) + diff_dots<N / 2>(a + N / 2, b + N / 2);
+    }
+}
+
+template <int D, int MODE>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 : 3))) void diff_key_strip_f32_kernel(DiffParams p)
+{
+    constexpr bool MULTI = MODE == kStripMulti;
+    constexpr bool kQueryIndex = MODE != kStripPlain;
+    constexpr int kCh = D / 8;      // channels of a half per lane group
+    constexpr int kOt = D / 16;     // channel tiles
+    constexpr int kOc = kOt > 1 ? kOt / 2 : 1;  // tiles of a half: consecutive channels of a lane
+    constexpr int kLR = D / 4, kRpi = 64 / kLR, kRep = kStripFE / kRpi;  // lanes per staged row, rows per load, loads
+    using Lds = DiffStripLds<D, MODE>;
+    constexpr int kRowF = Lds::kRowF;
+    __shared__ Lds lds;
+    const int lane = threadIdx.x, m = lane & 15, g4 = lane >> 4;
+    const KeyStripF t(p.tk, xcd_remap(blockIdx.x, gridDim.x));
+    if (t.sr0 >= p.Hk || t.sc0 >= p.Wk) return;  // the strip lies past the grid's edge
+    int nrows;
+    const int E = strip_entries(p, t, lds, lane, nrows);
+    int kx, ky;  // this lane's key: key m of the strip
+    t.key(m, kx, ky);
+    const bool key_ok = kx < p.Hk && ky < p.Wk;
+    const size_t kslice = static_cast<size_t>(t.s) * p.nkeys;
+    const size_t krow = kslice + (key_ok ? static_cast<size_t>(kx) * p.Wk + ky : static_cast<size_t>(t.sr0) * p.Wk + t.sc0);
+    auto leave_keys = [&]() {
+        if (key_ok && g4 == 0) p.heavy[atomicAdd(p.n_heavy, 1)] = static_cast<int32_t>(krow);
+    };
+    if (E > p.heavy_entries) {
+        leave_keys();
+        return;
+    }
+    float kf[2][kCh], vf[2][kCh];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        load_floats<kCh>(kf[h], static_cast<const float*>(p.K) + krow * D + h * (D / 2) + g4 * kCh);
+        load_floats<kCh>(vf[h], static_cast<const float*>(p.V) + krow * D + h * (D / 2) + g4 * kCh);
+    }
+    const uint32_t key_local = static_cast<uint32_t>(kx) * p.Wk + ky;  // raster index (causal test)
+    const float lam = p.lam[t.s];
+    const f32x4_t zero = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    f32x4_t dk[kOt], dv[kOt];
+#pragma unroll
+    for (int o = 0; o < kOt; ++o) dk[o] = dv[o] = zero;
+
+    auto slot_code = [&](int c0) {  // lane group 0's lane m finds entry slot m of a chunk (the others repeat it)
+        const int v = c0 + m;
+        if (v >= E) return -1;
+        int lo = 0, hi = nrows - 1;  // halo row holding flat position v: the last with pre <= v
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (lds.pre[mid] <= v) lo = mid; else hi = mid - 1;
+        }
+        return static_cast<int>(p.entries[lds.lo[lo] + (v - lds.pre[lo])]);
+    };
+    const int er = lane / kLR, ep = lane % kLR;
+    f32x4_t rq[kRep], rg[kRep];  // this lane's pieces of the next chunk's rows
+    int32_t match = -1, earlier = 0;  // the entry's match, and the query's first one
+    float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+    uint32_t qe = 0u, qg = 0u;
+    int code = -1;
+    auto fetch = [&]() {  // the rows and statistics of the chunk whose codes are in `code`
+        if (code >= 0) divmod(static_cast<uint32_t>(code), p.div_n, qe, qg);
+        match = -1;
+        if (code >= 0 && g4 == 0) {
+            match = p.J[code];
+            st = p.stats[qg];
+            if constexpr (MULTI) earlier = p.J[qg];
+        }
+        const int my_q = code >= 0 ? static_cast<int>(qg) : -1;
+#pragma unroll
+        for (int j = 0; j < kRep; ++j) {
+            // (past the entries a zero row keeps the operands finite)
+            const int qj = __shfl(my_q, er + kRpi * j, 64);
+            const size_t at = static_cast<size_t>(max(qj, 0)) * D + 4 * ep;
+            rq[j] = rg[j] = zero;
+            if (qj >= 0) {
+                rq[j] = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p.Q) + at);
+                rg[j] = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p.dO) + at);
+            }
+        }
+    };
+    code = slot_code(0);
+    fetch();
+    int next = slot_code(kStripFE);
+    for (int c0 = 0; c0 < E; c0 += kStripFE) {
+#pragma unroll
+        for (int j = 0; j < kRep; ++j) {
+            *reinterpret_cast<f32x4_t*>(lds.q + (er + kRpi * j) * kRowF + 4 * ep) = rq[j];
+            *reinterpret_cast<f32x4_t*>(lds.g + (er + kRpi * j) * kRowF + 4 * ep) = rg[j];
+        }
+        if (g4 == 0) {
+            int4 meta = make_int4(-(1 << 30), -(1 << 30), 0, 0);  // no key is near this match
+            if constexpr (kQueryIndex) lds.el[m][0] = lds.el[m][1] = 0;
+            if (code >= 0) {
+                uint32_t mu, mv;
+                divmod(static_cast<uint32_t>(clamp_index(match, p.nkeys)), p.div_wk, mu, mv);
+                meta = make_int4(static_cast<int>(mu), static_cast<int>(mv), __float_as_int(st.x), __float_as_int(st.y));
+                if constexpr (kQueryIndex) {
+                    uint32_t sl, rem;
+                    divmod(qg, p.div_plane, sl, rem);
+                    lds.el[m][1] = static_cast<int32_t>(causal_limit(p, sl, rem));
+                }
+                if constexpr (MULTI) {
+                    // the strip's keys that the query's windows 0 .. e - 1 hold
+                    uint32_t held = 0u;
+                    for (int f = 0; f < static_cast<int>(qe); ++f) {
+                        uint32_t fu, fv;
+                        const int32_t at = f == 0 ? earlier : p.J[static_cast<size_t>(f) * p.n + qg];
+                        divmod(static_cast<uint32_t>(clamp_index(at, p.nkeys)), p.div_wk, fu, fv);
+                        const int ru = static_cast<int>(fu) - t.sr0, cv = static_cast<int>(fv) - t.sc0;
+                        held |= t.bits(ru - p.b, ru + p.b, cv - p.b, cv + p.b);
+                    }
+                    lds.el[m][0] = static_cast<int32_t>(held);
+                }
+            }
+            lds.meta[m] = meta;
+            lds.second[m] = make_float2(st.z, st.w);
+        }
+        code = next;
+        if (c0 + kStripFE < E) fetch();
+        next = slot_code(c0 + 2 * kStripFE);
+        wave_lds_sync();
+
+        const float *const qa = lds.q + m * kRowF + g4 * kCh, *const ga = lds.g + m * kRowF + g4 * kCh;
+        float a[kCh];
+        f32x4_t sc[2], dp = zero;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            load_floats<kCh>(a, qa + h * (D / 2));
+            sc[h] = diff_dots<kCh>(a, kf[h]);
+            load_floats<kCh>(a, ga + h * (D / 2));
+            dp += diff_dots<kCh>(a, vf[h]);
+        }
+        float w[4], ds[2][4];  // of (key m, entry 4 g4 + i)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int te = 4 * g4 + i;
+            const int4 mt = lds.meta[te];
+            const float2 s2 = lds.second[te];
+            bool ok = key_ok && abs(mt.x - kx) <= p.b && abs(mt.y - ky) <= p.b;
+            if constexpr (MULTI) ok = ok && !((static_cast<uint32_t>(lds.el[te][0]) >> m) & 1u);
+            if constexpr (kQueryIndex)
+                if (!MULTI || p.causal) ok = ok && key_local <= static_cast<uint32_t>(lds.el[te][1]);
+            const float p1 = __builtin_amdgcn_exp2f(sc[0][i] * p.scale_log2e - __int_as_float(mt.z));
+            const float p2 = lam * __builtin_amdgcn_exp2f(sc[1][i] * p.scale_log2e - s2.x);
+            // (selected: a key that is left out may hold anything)
+            w[i] = ok ? p1 - p2 : 0.f;
+            ds[0][i] = ok ? p1 * (dp[i] - __int_as_float(mt.w)) : 0.f;
+            ds[1][i] = ok ? -p2 * (dp[i] - s2.y) : 0.f;
+        }
+        // the chunk's sums first, then onto the strip's (sums of sums round less than one long sum)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f32x4_t ck[kOc], cv[kOc];
+#pragma unroll
+            for (int o = 0; o < kOc; ++o) ck[o] = cv[o] = zero;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float bq[kOc], bg[kOc];
+                if constexpr (kOt > 1) {
+                    load_floats<kOc>(bq, lds.q + (4 * g4 + i) * kRowF + h * (D / 2) + m * kOc);
+                    load_floats<kOc>(bg, lds.g + (4 * g4 + i) * kRowF + h * (D / 2) + m * kOc);
+                } else {  // the tile's columns of this half
+                    const bool mine = (m < 8) == (h == 0);
+                    bq[0] = mine ? lds.q[(4 * g4 + i) * kRowF + m] : 0.f;
+                    bg[0] = mine ? lds.g[(4 * g4 + i) * kRowF + m] : 0.f;
+                }
+#pragma unroll
+                for (int o = 0; o < kOc; ++o) {
+                    cv[o] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], bg[o], cv[o], 0, 0, 0);
+                    ck[o] = __builtin_amdgcn_mfma_f32_16x16x4f32(ds[h][i], bq[o], ck[o], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int o = 0; o < kOc; ++o) {
+                dk[kOt > 1 ? h * kOc + o : 0] += ck[o];
+                dv[kOt > 1 ? h * kOc + o : 0] += cv[o];
+            }
+        }
+        wave_lds_sync();  // this chunk's LDS reads come before the next chunk's writes
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int o = 0; o < kOt; ++o)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += fabsf(dk[o][r]) + fabsf(dv[o][r]);
+    if (__any(!(sum < INFINITY))) {
+        leave_keys();
+        return;
+    }
+    // lane holds keys 4 g4 + r of the strip, channels h D / 2 + m kOc + o of tile h kOc + o
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        int ox, oy;
+        t.key(4 * g4 + r, ox, oy);
+        if (ox >= p.Hk || oy >= p.Wk) continue;
+        const size_t row = (kslice + static_cast<size_t>(ox) * p.Wk + oy) * D;
+#pragma unroll
+        for (int h = 0; h < (kOt > 1 ? 2 : 1); ++h) {
+            float ok[kOc], ov[kOc];
+#pragma unroll
+            for (int o = 0; o < kOc; ++o) ok[o] = dk[h * kOc + o][r] * p.scale, ov[o] = dv[h * kOc + o][r];
+            store_floats<kOc>(p.dK + row + h * (D / 2) + m * kOc, ok);
+            store_floats<kOc>(p.dV + row + h * (D / 2) + m * kOc, ov);
+        }
     }
 }
 
@@ -518,9 +761,10 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
     const size_t N = p.keys_total;
     hipError_t e;
     if ((e = launch(zero_i32_kernel, stride_blocks(N), st, start, nullptr, counts, N, p.n_heavy)) != hipSuccess) return e;
-    uint32_t parts = p.tq.div_slice.d;  // of dlam, per slice
+    p.slices = S;
+    p.parts = p.tq.div_slice.d;
     if (run_diff_query_tiles<T, D>(p, st, e)) {
-        parts = 4 * make_tiling(p.Hq, p.Wq, kBlock / 4).div_slice.d;
+        p.parts = 4 * make_tiling(p.Hq, p.Wq, kBlock / 4).div_slice.d;
     } else if constexpr (!MULTI)
         e = launch(diff_query_kernel<T, D, G, 0>, qblocks, st, nullptr, nullptr, p);
     else
@@ -528,21 +772,26 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
                          : launch(diff_query_kernel<T, D, G, kMaxKappa>, qblocks, st, nullptr, nullptr, p);
     if (e != hipSuccess) return e;
     if ((e = run_inverse(p, counts, offsets, sums, entries, st, nullptr, nullptr)) != hipSuccess) return e;
-    if ((e = launch(diff_lam_kernel, S, st, nullptr, nullptr, static_cast<const double*>(p.lam_part), parts, p.dlam)) != hipSuccess)
-        return e;
-    // Key side on the matrix cores for bf16 and windows 3 x 3 .. 15 x 15; the keys that its strips leave, and those of every
-    // other call with many entries, a wave each.
-    if constexpr (std::is_same<T, uint16_t>::value) {
-        if (p.b >= 1 && p.b <= kTileMaxB) {
+    // Key side on the matrix cores for windows 3 x 3 .. 15 x 15 (fp32: up to 64 channels); the keys that its strips leave, and
+    // those of every other call with many entries, a wave each.
+    if constexpr (std::is_same<T, uint16_t>::value || D <= 64) {
+        if (p.b >= 1 && p.b <= kTileMaxB && p.nkeys > 1) {  // (one key: dP - D is exactly 0 on the lane groups)
             DiffParams pt = p;
             pt.tk = make_tiling(p.Hk, p.Wk, kTileKeys);
             const uint64_t halo = static_cast<uint64_t>(std::min(4 + 2 * p.b, p.Hk)) * std::min(4 + 2 * p.b, p.Wk);
             const uint64_t mean = static_cast<uint64_t>(p.n) * p.kappa * halo / p.keys_total;  // entries of a strip
             pt.heavy_entries = static_cast<int>(std::min<uint64_t>(std::max<uint64_t>(1024, 4 * mean), INT32_MAX));
             const uint64_t strips = kStripWaves * tiling_blocks(pt.tk, S);
-            e = !MULTI         ? launch_wave(bwd_key_strip_kernel<D, kStripPlain, DiffParams>, strips, st, nullptr, nullptr, pt)
-                : p.kappa == 1 ? launch_wave(bwd_key_strip_kernel<D, kStripCausal, DiffParams>, strips, st, nullptr, nullptr, pt)
-                               : launch_wave(bwd_key_strip_kernel<D, kStripMulti, DiffParams>, strips, st, nullptr, nullptr, pt);
+            auto go = [&](auto mode) {
+                constexpr int MODE = decltype(mode)::value;
+                if constexpr (std::is_same<T, float>::value)
+                    return launch_wave(diff_key_strip_f32_kernel<D, MODE>, strips, st, nullptr, nullptr, pt);
+                else
+                    return launch_wave(bwd_key_strip_kernel<D, MODE, DiffParams>, strips, st, nullptr, nullptr, pt);
+            };
+            e = !MULTI         ? go(std::integral_constant<int, kStripPlain>{})
+                : p.kappa == 1 ? go(std::integral_constant<int, kStripCausal>{})
+                               : go(std::integral_constant<int, kStripMulti>{});
             if (e != hipSuccess) return e;
             return launch(diff_heavy_kernel<T, D, G, MULTI>, 1024, st, nullptr, stop, p);
         }

@@ -1,5 +1,6 @@
-// Key side of the gradients on the matrix cores for bf16 storage: the attend's
-// (scram_backward.hip) and the differential attend's (scram_diff_backward.hip).
+// Key side of the gradients on the matrix cores: the strips of the attend's
+// (scram_backward.hip) and the differential attend's (scram_diff_backward.hip),
+// and their kernel for bf16 storage.
 //
 // Everything here lives in an unnamed namespace, like scram_device.h.
 
@@ -448,6 +449,110 @@ bwd_key_strip_kernel(P p)
             p.dV[row + 16 * o + m] = dv[o][r];
         }
     }
+}
+
+// ---------------------------------------------------------------------------
+// Pieces of the strips with fp32 storage.
+// ---------------------------------------------------------------------------
+constexpr int kStripFE = 16;  // entries per chunk
+
+template <int N>
+__device__ __forceinline__ void load_floats(float (&v)[N], const float* a)
+{
+    if constexpr (N >= 4) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(a + i);
+            v[i] = x[0], v[i + 1] = x[1], v[i + 2] = x[2], v[i + 3] = x[3];
+        }
+    } else if constexpr (N == 2) {
+        const f32x2_t x = *reinterpret_cast<const f32x2_t*>(a);
+        v[0] = x[0], v[1] = x[1];
+    } else {
+        v[0] = a[0];
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void store_floats(float* a, const float (&v)[N])
+{
+    if constexpr (N >= 4) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4_t*>(a + i) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
+    } else if constexpr (N == 2) {
+        *reinterpret_cast<f32x2_t*>(a) = f32x2_t{v[0], v[1]};
+    } else {
+        a[0] = v[0];
+    }
+}
+
+// The 16 keys of a one-wave block, as in the bf16 kernel: rows sr0 .. sr1, columns sc0 .. sc1 of slice s.
+struct KeyStripF {
+    uint32_t s;
+    int lw, x0, y0, it0, sr0, sr1, sc0, sc1;
+    bool quad;
+
+    __device__ __forceinline__ KeyStripF(const Tiling& tk, uint32_t strip)
+    {
+        uint32_t k, tr, tc;
+        divmod(strip / kStripWaves, tk.div_slice, s, k);
+        tile_coords(tk, k, tr, tc);
+        lw = tk.lw;
+        const int tw = 1 << lw, th = kTileKeys >> lw;
+        x0 = static_cast<int>(tr) * th, y0 = static_cast<int>(tc) * tw;
+        const int w4 = static_cast<int>(strip % kStripWaves);
+        quad = lw == 3 && th == 8;
+        it0 = 16 * w4;
+        sr0 = quad ? x0 + 4 * (w4 >> 1) : x0 + (it0 >> lw);
+        sr1 = quad ? sr0 + 3 : x0 + ((it0 + 15) >> lw);
+        sc0 = quad ? y0 + 4 * (w4 & 1) : y0 + (it0 & (tw - 1));
+        sc1 = quad ? sc0 + 3 : sc0 + min(tw, 16) - 1;
+    }
+    __device__ __forceinline__ void key(int i, int& x, int& y) const
+    {
+        x = quad ? sr0 + (i >> 2) : x0 + ((it0 + i) >> lw);
+        y = quad ? sc0 + (i & 3) : y0 + ((it0 + i) & ((1 << lw) - 1));
+    }
+    // bits of the keys in rows rlo .. rhi, columns clo .. chi (relative to the strip's first)
+    __device__ __forceinline__ uint32_t bits(int rlo, int rhi, int clo, int chi) const
+    {
+        const int sC = sc1 - sc0 + 1, sR = 16 / sC;
+        rlo = max(rlo, 0), rhi = min(rhi, sR - 1), clo = max(clo, 0), chi = min(chi, sC - 1);
+        uint32_t set = 0u;
+        if (clo <= chi) {
+            const uint32_t cb = ((2u << chi) - 1u) & ~((1u << clo) - 1u);
+            for (int r = rlo; r <= rhi; ++r) set |= cb << (sC * r);
+        }
+        return set;
+    }
+};
+
+// The entries of a strip's halo: their ranges into lo, pre; returns their number.
+template <typename Lds>
+__device__ __forceinline__ int strip_entries(const BwdParams& p, const KeyStripF& t, Lds& lds, int lane, int& nrows)
+{
+    const int hr0 = max(t.sr0 - p.b, 0), hr1 = min(t.sr1 + p.b, p.Hk - 1);
+    const int hc0 = max(t.sc0 - p.b, 0), hc1 = min(t.sc1 + p.b, p.Wk - 1);
+    nrows = hr1 - hr0 + 1;  // at most kStripMaxRows
+    const int32_t* const off = p.offsets + static_cast<size_t>(t.s) * p.nkeys;
+    int cnt = 0;
+    if (lane < nrows) {
+        const int r = hr0 + lane;
+        const int32_t lo = off[r * p.Wk + hc0];
+        lds.lo[lane] = lo;
+        cnt = off[r * p.Wk + hc1 + 1] - lo;
+    }
+    int incl = cnt;
+#pragma unroll
+    for (int k2 = 1; k2 < 64; k2 <<= 1) {
+        const int y = __shfl_up(incl, k2, 64);
+        if (lane >= k2) incl += y;
+    }
+    if (lane < nrows) lds.pre[lane + 1] = incl;
+    if (lane == 0) lds.pre[0] = 0;
+    const int E = __shfl(incl, nrows - 1, 64);
+    wave_lds_sync();
+    return E;
 }
 
 }  // namespace
