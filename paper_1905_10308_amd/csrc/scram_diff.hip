@@ -94,17 +94,19 @@ __device__ __forceinline__ void diff_query(const DiffParams& p, uint32_t g, int 
     store_row<T, D, G>(p.out, g, lane, o, 1.f);
 }
 
-// A lane group per query (WAVE: a wave per query, for calls of a few queries).
-template <typename T, int D, int G, int MK, bool WAVE>
+// A lane group per query (WAVE: a wave per query, for calls of a few queries); kNb keys at a time: three, or five for one
+// 5 x 5 window, which is then five whole batches (8 x 128 x 128, 32 channels, fp32: two 3 x 3 windows with four 44 us, three
+// 38, five 40; one 5 x 5 window 38, 40, 32).
+template <typename T, int D, int G, int MK, int kNb, bool WAVE>
 __global__ __launch_bounds__(WAVE ? 64 : kBlock) void diff_attend_kernel(DiffParams p)
 {
     const int lane = threadIdx.x & (G - 1);
     if constexpr (WAVE) {
-        diff_query<T, D, G, MK, 4, 64 / G>(p, blockIdx.x, lane, threadIdx.x / G);
+        diff_query<T, D, G, MK, kNb, 64 / G>(p, blockIdx.x, lane, threadIdx.x / G);
     } else {
         uint32_t g;
         if (tile_item<Row<T, D, G>::kQpb>(p.tq, xcd_remap(blockIdx.x, gridDim.x), threadIdx.x / G, g))
-            diff_query<T, D, G, MK, 4, 1>(p, g, lane, 0);
+            diff_query<T, D, G, MK, kNb, 1>(p, g, lane, 0);
     }
 }
 
@@ -231,17 +233,14 @@ hipError_t run_diff(const DiffParams& p0, hipStream_t st, hipEvent_t e0, hipEven
 {
     constexpr int G = kDiffLanes<T, D>;
     DiffParams p = p0;
-    if (p.n <= 4096) {
-        if (e0 || e1)
-            hipExtLaunchKernelGGL((diff_attend_kernel<T, D, G, MK, true>), dim3(p.n), dim3(64), 0, st, e0, e1, 0, p);
-        else
-            hipLaunchKernelGGL((diff_attend_kernel<T, D, G, MK, true>), dim3(p.n), dim3(64), 0, st, p);
-        return hipGetLastError();
-    }
+    if (p.n <= 4096) return launch_wave(diff_attend_kernel<T, D, G, MK, 4, true>, p.n, st, e0, e1, p);
     hipError_t err = hipSuccess;
     if (run_diff_tiles<T, D>(p, st, e0, e1, err)) return err;
     p.tq = make_tiling(p.Hq, p.Wq, Row<T, D, G>::kQpb, kLaneSkew);
-    return launch(diff_attend_kernel<T, D, G, MK, false>, tiling_blocks(p.tq, p.n / p.tq.plane), st, e0, e1, p);
+    const uint64_t blocks = tiling_blocks(p.tq, p.n / p.tq.plane);
+    if constexpr (MK == 0)
+        if (p.b == 2) return launch(diff_attend_kernel<T, D, G, MK, 5, false>, blocks, st, e0, e1, p);
+    return launch(diff_attend_kernel<T, D, G, MK, 3, false>, blocks, st, e0, e1, p);
 }
 
 }  // namespace

@@ -501,8 +501,8 @@ __device__ __forceinline__ f32x4_t diff_dots(const float* a, const float* b)
     }
 }
 
-template <int D, int MODE>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 : 3))) void diff_key_strip_f32_kernel(DiffParams p)
+template <int D, int MODE, int TEAM>
+__global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 : 3))) void diff_key_strip_f32_kernel(DiffParams p)
 {
     constexpr bool MULTI = MODE == kStripMulti;
     constexpr bool kQueryIndex = MODE != kStripPlain;
@@ -512,8 +512,10 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 
     constexpr int kLR = D / 4, kRpi = 64 / kLR, kRep = kStripFE / kRpi;  // lanes per staged row, rows per load, loads
     using Lds = DiffStripLds<D, MODE>;
     constexpr int kRowF = Lds::kRowF;
-    __shared__ Lds lds;
-    const int lane = threadIdx.x, m = lane & 15, g4 = lane >> 4;
+    __shared__ Lds all[TEAM];
+    const int lane = threadIdx.x & 63, wave = TEAM > 1 ? threadIdx.x >> 6 : 0, m = lane & 15, g4 = lane >> 4;
+    Lds& lds = all[wave];
+    constexpr int kStep = kStripFE * TEAM;
     const KeyStripF t(p.tk, xcd_remap(blockIdx.x, gridDim.x));
     if (t.sr0 >= p.Hk || t.sc0 >= p.Wk) return;  // the strip lies past the grid's edge
     int nrows;
@@ -524,7 +526,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 
     const size_t kslice = static_cast<size_t>(t.s) * p.nkeys;
     const size_t krow = kslice + (key_ok ? static_cast<size_t>(kx) * p.Wk + ky : static_cast<size_t>(t.sr0) * p.Wk + t.sc0);
     auto leave_keys = [&]() {
-        if (key_ok && g4 == 0) p.heavy[atomicAdd(p.n_heavy, 1)] = static_cast<int32_t>(krow);
+        if (key_ok && g4 == 0 && wave == 0) p.heavy[atomicAdd(p.n_heavy, 1)] = static_cast<int32_t>(krow);
     };
     if (E > p.heavy_entries) {
         leave_keys();
@@ -580,10 +582,10 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 
             }
         }
     };
-    code = slot_code(0);
+    code = slot_code(kStripFE * wave);
     fetch();
-    int next = slot_code(kStripFE);
-    for (int c0 = 0; c0 < E; c0 += kStripFE) {
+    int next = slot_code(kStripFE * wave + kStep);
+    for (int c0 = kStripFE * wave; c0 < E; c0 += kStep) {
 #pragma unroll
         for (int j = 0; j < kRep; ++j) {
             *reinterpret_cast<f32x4_t*>(lds.q + (er + kRpi * j) * kRowF + 4 * ep) = rq[j];
@@ -618,8 +620,8 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 
             lds.second[m] = make_float2(st.z, st.w);
         }
         code = next;
-        if (c0 + kStripFE < E) fetch();
-        next = slot_code(c0 + 2 * kStripFE);
+        if (c0 + kStep < E) fetch();
+        next = slot_code(c0 + 2 * kStep);
         wave_lds_sync();
 
         const float *const qa = lds.q + m * kRowF + g4 * kCh, *const ga = lds.g + m * kRowF + g4 * kCh;
@@ -680,6 +682,21 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 
         }
         wave_lds_sync();  // this chunk's LDS reads come before the next chunk's writes
     }
+    if constexpr (TEAM > 1) {  // the other waves' sums, from their staging areas
+        static_assert(sizeof(f32x4_t) * 128 * kOt <= sizeof(float) * 2 * kStripFE * kRowF, "16 keys' gradient rows fit 16 entries' rows");
+        f32x4_t* const mine = reinterpret_cast<f32x4_t*>(&lds) + lane;
+        if (wave > 0) {
+#pragma unroll
+            for (int o = 0; o < kOt; ++o) mine[128 * o] = dk[o], mine[128 * o + 64] = dv[o];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+        for (int w = 1; w < TEAM; ++w) {
+            const f32x4_t* const other = reinterpret_cast<const f32x4_t*>(&all[w]) + lane;
+#pragma unroll
+            for (int o = 0; o < kOt; ++o) dk[o] += other[128 * o], dv[o] += other[128 * o + 64];
+        }
+    }
     float sum = 0.f;
 #pragma unroll
     for (int o = 0; o < kOt; ++o)
@@ -706,6 +723,11 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 
         }
     }
 }
+
+// Up to as many strips a team of four waves takes each, up to four times as many a team of two: a wave per strip would not
+// fill the machine, and the strips of many entries would run on alone.  (fp32, 64 channels, 3072 strips: 3 x 3 117 us a call
+// with one wave, 107 with two, 115 with four, 5 x 5 177, 161, 166; bf16, 288 strips: 68, 59, 56; 8192 strips: 252, 268 with four.)
+constexpr uint64_t kTeamStrips = 1024;
 
 size_t r256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
 
@@ -782,12 +804,17 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
             const uint64_t mean = static_cast<uint64_t>(p.n) * p.kappa * halo / p.keys_total;  // entries of a strip
             pt.heavy_entries = static_cast<int>(std::min<uint64_t>(std::max<uint64_t>(1024, 4 * mean), INT32_MAX));
             const uint64_t strips = kStripWaves * tiling_blocks(pt.tk, S);
-            auto go = [&](auto mode) {
-                constexpr int MODE = decltype(mode)::value;
+            auto with = [&](auto mode, auto team) {
+                constexpr int MODE = decltype(mode)::value, TEAM = decltype(team)::value;
                 if constexpr (std::is_same<T, float>::value)
-                    return launch_wave(diff_key_strip_f32_kernel<D, MODE>, strips, st, nullptr, nullptr, pt);
+                    return launch_wave<64 * TEAM>(diff_key_strip_f32_kernel<D, MODE, TEAM>, strips, st, nullptr, nullptr, pt);
                 else
-                    return launch_wave(bwd_key_strip_kernel<D, MODE, DiffParams>, strips, st, nullptr, nullptr, pt);
+                    return launch_wave<64 * TEAM>(bwd_key_strip_kernel<D, MODE, DiffParams, TEAM>, strips, st, nullptr, nullptr, pt);
+            };
+            auto go = [&](auto mode) {
+                return strips <= kTeamStrips ? with(mode, std::integral_constant<int, 4>{})
+                       : strips <= 4 * kTeamStrips ? with(mode, std::integral_constant<int, 2>{})
+                                                   : with(mode, std::integral_constant<int, 1>{});
             };
             e = !MULTI         ? go(std::integral_constant<int, kStripPlain>{})
                 : p.kappa == 1 ? go(std::integral_constant<int, kStripCausal>{})

@@ -80,8 +80,9 @@ constexpr int kStripWaves = kTileKeys / 16;  // strips of a tile, one one-wave b
 // other half of the keys zeroed), P = P1 - lam P2 for dV, and dS1, dS2 = - lam P2 (dP - D2) for the halves of dK.  Strips whose
 // sums are not finite (a row that is not reaches all of the strip's keys through 0 * inf) and those of more entries than
 // p.heavy_entries leave their keys to the list of diff_heavy_kernel.
-template <int D, int MODE, typename P>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(strip_waves(D, std::is_same<P, DiffParams>::value)))) void
+// TEAM waves share a strip, taking its chunks in turn, and their sums are added up through LDS.
+template <int D, int MODE, typename P, int TEAM = 1>
+__global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(strip_waves(D, std::is_same<P, DiffParams>::value)))) void
 bwd_key_strip_kernel(P p)
 {
     constexpr bool DIFF = std::is_same<P, DiffParams>::value;
@@ -89,7 +90,7 @@ bwd_key_strip_kernel(P p)
     constexpr bool kQueryIndex = MODE != kStripPlain;  // entries carry their window and query's raster index
     using KS = KeyStrip<D>;
     constexpr int kCE = kStripCE;
-    constexpr int kW = 1;  // waves per block
+    constexpr int kW = TEAM;  // waves per block
     // q rows of the chunk, then 64 bytes of skew, then its dO rows: lanes 2t and 2t + 1 stage row t of
     // each; with the skew the eight lanes of one 128-bit access (rows t .. t + 3 of both) use disjoint
     // halves of the 32 banks, without it the two rows of each pair share banks
@@ -101,7 +102,7 @@ bwd_key_strip_kernel(P p)
     __shared__ int32_t s_lo[kW][kStripMaxRows], s_pre[kW][kStripMaxRows + 1];
     __shared__ float2 s_second[kW][DIFF ? kCE : 1];  // lse2, D of the second map
 
-    const int lane = threadIdx.x & 63, wave = 0;
+    const int lane = threadIdx.x & 63, wave = TEAM > 1 ? threadIdx.x >> 6 : 0;
     const int m = lane & 15, g4 = lane >> 4;
     const uint32_t blk = xcd_remap(blockIdx.x, gridDim.x);
 
@@ -172,7 +173,7 @@ bwd_key_strip_kernel(P p)
     const size_t kslice = static_cast<size_t>(s) * p.nkeys;
     const size_t krow = kslice + (key_ok ? static_cast<size_t>(kx) * p.Wk + ky : static_cast<size_t>(sr0) * p.Wk + sc0);
     auto leave_keys = [&]() {
-        if (key_ok && g4 == 0) p.heavy[atomicAdd(p.n_heavy, 1)] = static_cast<int32_t>(krow);
+        if (key_ok && g4 == 0 && wave == 0) p.heavy[atomicAdd(p.n_heavy, 1)] = static_cast<int32_t>(krow);
     };
     if constexpr (DIFF) {
         if (E > p.heavy_entries) {
@@ -233,8 +234,8 @@ bwd_key_strip_kernel(P p)
         const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(a + 16 * KS::kRowB));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    int code = slot_code(0);
-    for (int c0 = 0; c0 < E; c0 += kCE) {
+    int code = slot_code(TEAM > 1 ? kCE * wave : 0);
+    for (int c0 = TEAM > 1 ? kCE * wave : 0; c0 < E; c0 += kCE * TEAM) {
         {
             uint32_t qe = 0, qg = 0;
             if (code >= 0) divmod(static_cast<uint32_t>(code), p.div_n, qe, qg);
@@ -320,7 +321,7 @@ bwd_key_strip_kernel(P p)
                 if constexpr (DIFF) s_second[wave][t] = second;
             }
         }
-        code = slot_code(c0 + kCE);  // the next chunk's entries load during the products
+        code = slot_code(c0 + kCE * TEAM);  // the next chunk's entries load during the products
         wave_lds_sync();
 
         // S^T, dP^T for entries 16 et + (0..15) of the chunk against the strip's 16 keys
@@ -425,6 +426,21 @@ bwd_key_strip_kernel(P p)
         wave_lds_sync();  // this chunk's LDS reads come before the next chunk's writes
     }
 
+    if constexpr (TEAM > 1) {
+        // the other waves' sums, from their staging areas (16 keys' two gradient rows fit those of 32 entries)
+        f32x4_t* const mine = reinterpret_cast<f32x4_t*>(s_row[wave]) + lane;
+        if (wave > 0) {
+#pragma unroll
+            for (int o = 0; o < KS::kOt; ++o) mine[128 * o] = dk[o], mine[128 * o + 64] = dv[o];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+        for (int w = 1; w < TEAM; ++w) {
+            const f32x4_t* const other = reinterpret_cast<const f32x4_t*>(s_row[w]) + lane;
+#pragma unroll
+            for (int o = 0; o < KS::kOt; ++o) dk[o] += other[128 * o], dv[o] += other[128 * o + 64];
+        }
+    }
     if constexpr (DIFF) {
         float sum = 0.f;
 #pragma unroll
