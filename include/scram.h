@@ -459,7 +459,8 @@ enum { SCRAM_ROTARY_MAX_PAIRS = 128 };
  *             origin is NULL)
  *   origin    nullable int32 [origin_rows, 3] on the device: the same, one row
  *             for all slices, or one per slice (origin_rows == slices[i])
- * T*H*W * groups * (d / groups - P) < 2^31.  Returns a status code.
+ * T*H*W * groups * (d / groups - P) / v < 2^31, v the channels of the widest
+ * vector up to 16 bytes that divide d / groups and P.  Returns a status code.
  */
 int scram_rotary(int count, const void* const* src, void* const* dst, const int* slices, int dtype, int T, int H, int W,
                  int d, int groups, const int* sections, const double* freqs, const int* first, const int32_t* origin,

@@ -16,7 +16,7 @@
 // adds them up over its threads once at its end and writes one row of parts;
 // a second kernel adds up the parts, in a fixed order.
 
-#include "scram_device.h"
+#include "scram_rows.h"
 
 namespace scram {
 namespace {
@@ -40,31 +40,6 @@ struct NormParams {
     int C, lanes;
     float eps;
 };
-
-template <typename T>
-constexpr int kChunk = 16 / static_cast<int>(sizeof(T));  // channels of a chunk of X
-
-// V channels at any element's address.
-template <typename T, int V>
-using vec = T __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-
-template <typename T>
-__device__ __forceinline__ float norm_float(T x)
-{
-    if constexpr (std::is_same<T, float>::value)
-        return x;
-    else
-        return __uint_as_float(static_cast<uint32_t>(x) << 16);
-}
-
-template <typename T>
-__device__ __forceinline__ T norm_round(float x)
-{
-    if constexpr (std::is_same<T, float>::value)
-        return x;
-    else
-        return static_cast<T>(f32_to_bf16_rne(x));
-}
 
 // Sums of N values over the `lanes` threads of a row, on all of them.  Rows of several waves pass through LDS, in one of
 // two halves in turn so that one barrier per sum is enough.
@@ -100,55 +75,20 @@ constexpr bool norm_wide(int layout) { return layout >= kWide; }
 // forward: a row at a time 26 us, four 16; 8192 x 4096 backward: one 57 us, two 50.)
 constexpr int norm_rows(int layout, bool backward) { return layout == kHuge ? 1 : layout == kNarrow && !backward ? 4 : 2; }
 
-// N channels at `row` into x from element o on (o a multiple of N below V, the same for every thread).
-template <int N, typename T, int V>
-__device__ __forceinline__ void load_piece(const T* row, int o, vec<T, V>& x)
-{
-    const vec<T, N> y = *reinterpret_cast<const vec<T, N>*>(row + o);
-#pragma unroll
-    for (int q = 0; q < V; q += N)
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[q + j] = q == o ? static_cast<T>(y[j]) : static_cast<T>(x[q + j]);
-}
-
-template <int N, typename T, int V>
-__device__ __forceinline__ void store_piece(T* row, int o, const vec<T, V>& x)
-{
-    vec<T, N> y(T(0));
-#pragma unroll
-    for (int q = 0; q < V; q += N)
-#pragma unroll
-        for (int j = 0; j < N; ++j) y[j] = q == o ? static_cast<T>(x[q + j]) : static_cast<T>(y[j]);
-    *reinterpret_cast<vec<T, N>*>(row + o) = y;
-}
-
-// Channels at .. at + V - 1 of a row of C, those that it has, zeros after them.  TAIL: C is not a multiple of V, and the
-// last C mod V channels come in pieces of 4, 2 and 1.
+// Channels at .. at + V - 1 of a row of C, those that it has, zeros after them.  TAIL: C is not a multiple of V.
 template <bool TAIL, int V, typename T>
 __device__ __forceinline__ vec<T, V> load_chunk(const T* row, int at, int C)
 {
-    if (!TAIL || at + V <= C) return *reinterpret_cast<const vec<T, V>*>(row + at);
-    vec<T, V> x(T(0));
-    const int rest = C % V;
-    if constexpr (V > 4)
-        if (rest & 4) load_piece<4, T, V>(row + at, 0, x);
-    if (rest & 2) load_piece<2, T, V>(row + at, rest & 4, x);
-    if (rest & 1) load_piece<1, T, V>(row + at, rest & 6, x);
-    return x;
+    return !TAIL || at + V <= C ? load_vec<T, V>(row + at) : load_part<T, V>(row + at, C % V);
 }
 
 template <bool TAIL, int V, typename T>
 __device__ __forceinline__ void store_chunk(T* row, int at, int C, vec<T, V> x)
 {
-    if (!TAIL || at + V <= C) {
-        *reinterpret_cast<vec<T, V>*>(row + at) = x;
-        return;
-    }
-    const int rest = C % V;
-    if constexpr (V > 4)
-        if (rest & 4) store_piece<4, T, V>(row + at, 0, x);
-    if (rest & 2) store_piece<2, T, V>(row + at, rest & 4, x);
-    if (rest & 1) store_piece<1, T, V>(row + at, rest & 6, x);
+    if (!TAIL || at + V <= C)
+        store_vec<T, V>(row + at, x);
+    else
+        store_part<T, V>(row + at, C % V, x);
 }
 
 // The thread's weights (or `none` without any).
@@ -168,7 +108,7 @@ __device__ __forceinline__ void load_weights(const void* w, const NormParams& p,
         } else if (w != nullptr) {
             const vec<uint16_t, V> x = load_chunk<TAIL, V>(static_cast<const uint16_t*>(w), at, p.C);
 #pragma unroll
-            for (int j = 0; j < V; ++j) out[c][j] = norm_float(static_cast<uint16_t>(x[j]));
+            for (int j = 0; j < V; ++j) out[c][j] = to_float(static_cast<uint16_t>(x[j]));
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j) out[c][j] = none;
@@ -214,7 +154,7 @@ __global__ __launch_bounds__(norm_threads(LAYOUT)) void norm_kernel(NormParams p
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) mean[k] += norm_float(static_cast<T>(a[k][c][j]));
+                for (int j = 0; j < V; ++j) mean[k] += to_float(static_cast<T>(a[k][c][j]));
         }
         row_sum<R, WIDE>(mean, p.lanes, s_sum, half);
 #pragma unroll
@@ -226,7 +166,7 @@ __global__ __launch_bounds__(norm_threads(LAYOUT)) void norm_kernel(NormParams p
                 const int left = p.C - (lane + c * p.lanes) * V;  // channels of the row from this chunk on
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float v = norm_float(static_cast<T>(a[k][c][j])) - mean[k];
+                    const float v = to_float(static_cast<T>(a[k][c][j])) - mean[k];
                     rstd[k] = (TAIL ? j : 0) < left ? fmaf(v, v, rstd[k]) : rstd[k];
                 }
             }
@@ -243,7 +183,7 @@ __global__ __launch_bounds__(norm_threads(LAYOUT)) void norm_kernel(NormParams p
                 Vec o;
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    o[j] = norm_round<T>(fmaf((norm_float(static_cast<T>(a[k][c][j])) - mean[k]) * rstd[k], w[c][j], b[c][j]));
+                    o[j] = from_float<T>(fmaf((to_float(static_cast<T>(a[k][c][j])) - mean[k]) * rstd[k], w[c][j], b[c][j]));
                 if (at < p.C) store_chunk<TAIL, V>(y, at, p.C, o);
             }
             if (lane == 0 && p.mean) {
@@ -297,7 +237,7 @@ __global__ __launch_bounds__(norm_threads(LAYOUT)) void norm_backward_kernel(Nor
             mean[k] = live ? p.mean_in[at_row] : 0.f;
             rstd[k] = live ? p.rstd_in[at_row] : 0.f;
         }
-        auto xhat = [&](int k, int c, int j) { return (norm_float(static_cast<T>(a[k][c][j])) - mean[k]) * rstd[k]; };
+        auto xhat = [&](int k, int c, int j) { return (to_float(static_cast<T>(a[k][c][j])) - mean[k]) * rstd[k]; };
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             sum[2 * k] = sum[2 * k + 1] = 0.f;
@@ -306,7 +246,7 @@ __global__ __launch_bounds__(norm_threads(LAYOUT)) void norm_backward_kernel(Nor
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     // (past the end of the row, or of the rows, dY is 0 and xh finite: nothing is added)
-                    const float dy = norm_float(static_cast<TG>(d[k][c][j])), xh = xhat(k, c, j);
+                    const float dy = to_float(static_cast<TG>(d[k][c][j])), xh = xhat(k, c, j);
                     dw[c][j] = fmaf(dy, xh, dw[c][j]);
                     db[c][j] += dy;
                     const float g = dy * w[c][j];
@@ -327,7 +267,7 @@ __global__ __launch_bounds__(norm_threads(LAYOUT)) void norm_backward_kernel(Nor
                 VecG o;
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    o[j] = norm_round<TG>(rstd[k] * (norm_float(static_cast<TG>(d[k][c][j])) * w[c][j] - mg - xhat(k, c, j) * mx));
+                    o[j] = from_float<TG>(rstd[k] * (to_float(static_cast<TG>(d[k][c][j])) * w[c][j] - mg - xhat(k, c, j) * mx));
                 if (at < p.C) store_chunk<TAIL, V>(dx, at, p.C, o);
             }
         }

@@ -7,7 +7,7 @@
 // by memory.  The angles of a pixel's pairs are the same in every slice and
 // tensor, so a thread computes those of its pairs once and walks the slices.
 
-#include "scram_device.h"
+#include "scram_rows.h"
 
 namespace scram {
 namespace {
@@ -55,24 +55,6 @@ __device__ __forceinline__ void turn_cos_sin(uint64_t x, float& c, float& s)
     s = quarter & 2u ? -x1 : x1;
 }
 
-template <typename T>
-__device__ __forceinline__ float to_float(T x)
-{
-    if constexpr (std::is_same<T, float>::value)
-        return x;
-    else
-        return __uint_as_float(static_cast<uint32_t>(x) << 16);
-}
-
-template <typename T>
-__device__ __forceinline__ T from_float(float x)
-{
-    if constexpr (std::is_same<T, float>::value)
-        return x;
-    else
-        return static_cast<T>(f32_to_bf16_rne(x));
-}
-
 // A thread takes V pairs of one group of one pixel's row, two vectors of V
 // channels (the pairs' first and second channels, or 2 V neighbouring ones when
 // INTER), or one vector of the channels that are not turned; in every slice of
@@ -80,7 +62,7 @@ __device__ __forceinline__ T from_float(float x)
 template <typename T, int V, bool INTER>
 __global__ __launch_bounds__(kBlock) void rotary_kernel(RotaryParams p)
 {
-    typedef T vec __attribute__((ext_vector_type(V)));
+    using Vec = vec<T, V>;
     const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
     if (i >= p.total) return;
     uint32_t pixel, in_row, grp, chunk;
@@ -123,12 +105,12 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(RotaryParams p)
             if (s >= p.slices[t]) continue;
             const T* const from = static_cast<const T*>(p.src[t]) + s * slice + row;
             T* const to = static_cast<T*>(p.dst[t]) + s * slice + row;
-            vec a = *reinterpret_cast<const vec*>(from + at0);
+            Vec a = *reinterpret_cast<const Vec*>(from + at0);
             if (!turned) {
-                *reinterpret_cast<vec*>(to + at0) = a;
+                *reinterpret_cast<Vec*>(to + at0) = a;
                 continue;
             }
-            vec b = *reinterpret_cast<const vec*>(from + at1);
+            Vec b = *reinterpret_cast<const Vec*>(from + at1);
             T in[2 * V], out[2 * V];
 #pragma unroll
             for (int j = 0; j < V; ++j) in[j] = a[j], in[V + j] = b[j];
@@ -141,25 +123,20 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(RotaryParams p)
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) a[j] = out[j], b[j] = out[V + j];
-            *reinterpret_cast<vec*>(to + at0) = a;
-            *reinterpret_cast<vec*>(to + at1) = b;
+            *reinterpret_cast<Vec*>(to + at0) = a;
+            *reinterpret_cast<Vec*>(to + at1) = b;
         }
     }
 }
 
-// Channels per vector: the most, up to 16 bytes, that divide the turned pairs and the group and to which every tensor is
-// aligned.
+// Channels per vector: the most, up to 16 bytes, that divide the turned pairs and the group.  (Whole vectors of 16 bytes with a
+// last one in pieces were slower: 46 pairs of 100 fp32 channels, vectors of 8 bytes 56 us, 16 with a rest 65; 23 pairs of
+// bf16, single channels 32 us, 16 bytes with a rest 44.)
 int rotary_vector(int elem, const RotaryCall& c)
 {
     const int group = c.d / c.groups, pairs = c.pairs[0] + c.pairs[1] + c.pairs[2];
     int v = 16 / elem;
-    auto fits = [&](int n) {
-        if (group % n || pairs % n) return false;
-        for (int t = 0; t < c.count; ++t)
-            if ((reinterpret_cast<uintptr_t>(c.src[t]) | reinterpret_cast<uintptr_t>(c.dst[t])) % (n * elem)) return false;
-        return true;
-    };
-    while (v > 1 && !fits(v)) v /= 2;
+    while (group % v || pairs % v) v /= 2;
     return v;
 }
 
