@@ -222,7 +222,8 @@ bool run_diff_tiles(const DiffParams& p0, hipStream_t st, hipEvent_t e0, hipEven
         if (tiles == 0) return false;
         err = p.b == 1   ? run_diff_tile<D, 3>(p, tiles, st, e0, e1)
               : p.b == 2 ? run_diff_tile<D, 5>(p, tiles, st, e0, e1)
-                         : run_diff_tile<D, 7>(p, tiles, st, e0, e1);
+              : p.b == 3 ? run_diff_tile<D, 7>(p, tiles, st, e0, e1)
+                         : run_diff_tile<D, 9>(p, tiles, st, e0, e1);
         return true;
     }
     return false;

@@ -51,7 +51,7 @@ __device__ __forceinline__ float diff_query_gradient(const DiffParams& p, uint32
     using RW = Row<T, D, G>;
     static_assert(RW::kCh == 2, "two chunks per lane: one of each half");
     constexpr int H = RW::kEpc;  // channels per lane of each half
-    constexpr int kNb = 2;
+    constexpr int kNb = 3;
     uint32_t s, rem;
     divmod(g, p.div_plane, s, rem);
     const size_t slice = static_cast<size_t>(s) * p.nkeys * D;
@@ -478,13 +478,12 @@ __global__ __launch_bounds__(kBlock) void diff_heavy_kernel(DiffParams p)
 // A chunk's rows load while the previous chunk is in the matrix cores, the entry codes a chunk before that.  A strip of more
 // entries than p.heavy_entries, or whose sums are not finite, leaves its keys to the list.
 // ---------------------------------------------------------------------------
-template <int D, int MODE>
+template <int D>
 struct DiffStripLds {
     static constexpr int kRowF = D + 4;  // row stride, floats (padded)
     __attribute__((aligned(16))) float q[kStripFE * kRowF], g[kStripFE * kRowF];
-    int4 meta[kStripFE];        // match row, match column, lse2 and D bits of the first map
-    float2 second[kStripFE];    // lse2, D of the second
-    int32_t el[MODE != kStripPlain ? kStripFE : 1][2];  // as in the bf16 kernel
+    float4 meta[kStripFE];      // lse2 and D of both maps
+    uint32_t in[kStripFE];      // bit k: the entry counts for key k of the strip
     int32_t lo[kStripMaxRows], pre[kStripMaxRows + 1];
 };
 
@@ -505,12 +504,11 @@ template <int D, int MODE, int TEAM>
 __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 64 ? 2 : 3))) void diff_key_strip_f32_kernel(DiffParams p)
 {
     constexpr bool MULTI = MODE == kStripMulti;
-    constexpr bool kQueryIndex = MODE != kStripPlain;
     constexpr int kCh = D / 8;      // channels of a half per lane group
     constexpr int kOt = D / 16;     // channel tiles
     constexpr int kOc = kOt > 1 ? kOt / 2 : 1;  // tiles of a half: consecutive channels of a lane
     constexpr int kLR = D / 4, kRpi = 64 / kLR, kRep = kStripFE / kRpi;  // lanes per staged row, rows per load, loads
-    using Lds = DiffStripLds<D, MODE>;
+    using Lds = DiffStripLds<D>;
     constexpr int kRowF = Lds::kRowF;
     __shared__ Lds all[TEAM];
     const int lane = threadIdx.x & 63, wave = TEAM > 1 ? threadIdx.x >> 6 : 0, m = lane & 15, g4 = lane >> 4;
@@ -538,8 +536,8 @@ __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 
         load_floats<kCh>(kf[h], static_cast<const float*>(p.K) + krow * D + h * (D / 2) + g4 * kCh);
         load_floats<kCh>(vf[h], static_cast<const float*>(p.V) + krow * D + h * (D / 2) + g4 * kCh);
     }
-    const uint32_t key_local = static_cast<uint32_t>(kx) * p.Wk + ky;  // raster index (causal test)
     const float lam = p.lam[t.s];
+    const uint32_t live = static_cast<uint32_t>(__ballot(key_ok)) & 0xFFFFu;  // keys of the strip inside the grid
     const f32x4_t zero = f32x4_t{0.f, 0.f, 0.f, 0.f};
     f32x4_t dk[kOt], dv[kOt];
 #pragma unroll
@@ -592,32 +590,34 @@ __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 
             *reinterpret_cast<f32x4_t*>(lds.g + (er + kRpi * j) * kRowF + 4 * ep) = rg[j];
         }
         if (g4 == 0) {
-            int4 meta = make_int4(-(1 << 30), -(1 << 30), 0, 0);  // no key is near this match
-            if constexpr (kQueryIndex) lds.el[m][0] = lds.el[m][1] = 0;
+            float4 meta = make_float4(0.f, 0.f, 0.f, 0.f);
+            uint32_t in = 0u;  // the strip's keys that the entry counts for
             if (code >= 0) {
                 uint32_t mu, mv;
                 divmod(static_cast<uint32_t>(clamp_index(match, p.nkeys)), p.div_wk, mu, mv);
-                meta = make_int4(static_cast<int>(mu), static_cast<int>(mv), __float_as_int(st.x), __float_as_int(st.y));
-                if constexpr (kQueryIndex) {
-                    uint32_t sl, rem;
+                const int ru = static_cast<int>(mu) - t.sr0, cv = static_cast<int>(mv) - t.sc0;
+                in = t.bits(ru - p.b, ru + p.b, cv - p.b, cv + p.b) & live;
+                if (MODE != kStripPlain && p.causal) {
+                    uint32_t sl, rem, lr, lc;
                     divmod(qg, p.div_plane, sl, rem);
-                    lds.el[m][1] = static_cast<int32_t>(causal_limit(p, sl, rem));
+                    divmod(causal_limit(p, sl, rem), p.div_wk, lr, lc);
+                    const int last = static_cast<int>(lr) - t.sr0;
+                    in &= t.bits(0, last - 1, 0, 15) | t.bits(last, last, 0, static_cast<int>(lc) - t.sc0);
                 }
                 if constexpr (MULTI) {
-                    // the strip's keys that the query's windows 0 .. e - 1 hold
-                    uint32_t held = 0u;
+                    // less those that the query's windows 0 .. e - 1 hold
                     for (int f = 0; f < static_cast<int>(qe); ++f) {
                         uint32_t fu, fv;
                         const int32_t at = f == 0 ? earlier : p.J[static_cast<size_t>(f) * p.n + qg];
                         divmod(static_cast<uint32_t>(clamp_index(at, p.nkeys)), p.div_wk, fu, fv);
-                        const int ru = static_cast<int>(fu) - t.sr0, cv = static_cast<int>(fv) - t.sc0;
-                        held |= t.bits(ru - p.b, ru + p.b, cv - p.b, cv + p.b);
+                        const int hu = static_cast<int>(fu) - t.sr0, hv = static_cast<int>(fv) - t.sc0;
+                        in &= ~t.bits(hu - p.b, hu + p.b, hv - p.b, hv + p.b);
                     }
-                    lds.el[m][0] = static_cast<int32_t>(held);
                 }
+                meta = st;
             }
+            lds.in[m] = in;
             lds.meta[m] = meta;
-            lds.second[m] = make_float2(st.z, st.w);
         }
         code = next;
         if (c0 + kStep < E) fetch();
@@ -638,18 +638,15 @@ __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int te = 4 * g4 + i;
-            const int4 mt = lds.meta[te];
-            const float2 s2 = lds.second[te];
-            bool ok = key_ok && abs(mt.x - kx) <= p.b && abs(mt.y - ky) <= p.b;
-            if constexpr (MULTI) ok = ok && !((static_cast<uint32_t>(lds.el[te][0]) >> m) & 1u);
-            if constexpr (kQueryIndex)
-                if (!MULTI || p.causal) ok = ok && key_local <= static_cast<uint32_t>(lds.el[te][1]);
-            const float p1 = __builtin_amdgcn_exp2f(sc[0][i] * p.scale_log2e - __int_as_float(mt.z));
-            const float p2 = lam * __builtin_amdgcn_exp2f(sc[1][i] * p.scale_log2e - s2.x);
-            // (selected: a key that is left out may hold anything)
-            w[i] = ok ? p1 - p2 : 0.f;
-            ds[0][i] = ok ? p1 * (dp[i] - __int_as_float(mt.w)) : 0.f;
-            ds[1][i] = ok ? -p2 * (dp[i] - s2.y) : 0.f;
+            const float4 mt = lds.meta[te];
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[0][i], p.scale_log2e, -mt.x));
+            const float p2 = lam * __builtin_amdgcn_exp2f(fmaf(sc[1][i], p.scale_log2e, -mt.z));
+            // (selected by bits: a key that is left out may hold anything)
+            const uint32_t in = static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(lds.in[te]), m, 1));
+            auto kept = [&](float x) { return __uint_as_float(__float_as_uint(x) & in); };
+            w[i] = kept(p1 - p2);
+            ds[0][i] = kept(p1 * (dp[i] - mt.y));
+            ds[1][i] = kept(p2 * (mt.w - dp[i]));
         }
         // the chunk's sums first, then onto the strip's (sums of sums round less than one long sum)
 #pragma unroll
@@ -763,7 +760,8 @@ bool run_diff_query_tiles(const DiffParams& p0, hipStream_t st, hipError_t& err)
         if (tiles == 0) return false;
         err = p.b == 1   ? run_diff_query_tile<D, 3>(p, 4 * tiles, st)
               : p.b == 2 ? run_diff_query_tile<D, 5>(p, 4 * tiles, st)
-                         : run_diff_query_tile<D, 7>(p, 4 * tiles, st);
+              : p.b == 3 ? run_diff_query_tile<D, 7>(p, 4 * tiles, st)
+                         : run_diff_query_tile<D, 9>(p, 4 * tiles, st);
         return true;
     }
     return false;

@@ -412,13 +412,13 @@ __device__ __forceinline__ bf16x4_t column4(const unsigned char* tile, int m, in
     return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4_t*)(at));
 }
 
-// Host: whether the matrix cores take this call -- up to four windows of side 3, 5 or 7, a positive scale, slices of at most
+// Host: whether the matrix cores take this call -- up to four windows of side 3, 5, 7 or 9, a positive scale, slices of at most
 // 4 GiB of key rows (bf16 rows of 32 to 128 channels).  Sets the tiling and the blocks up to which a wave walks its boxes;
 // returns the tiles of 64 queries, 0: not taken.
 template <int D>
 uint64_t diff_tiles(DiffParams& p)
 {
-    if (p.kappa > 4 || p.b < 1 || p.b > 3 || !(p.scale_log2e > 0.f) || static_cast<uint64_t>(p.nkeys) * (2 * D) > 0xFFFFFFFFull)
+    if (p.kappa > 4 || p.b < 1 || p.b > 4 || !(p.scale_log2e > 0.f) || static_cast<uint64_t>(p.nkeys) * (2 * D) > 0xFFFFFFFFull)
         return 0;
     p.tq = make_tiling(p.Hq, p.Wq, kBlock / 4);
     const uint64_t tiles = tiling_blocks(p.tq, p.n / p.tq.plane);

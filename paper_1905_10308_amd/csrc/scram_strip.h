@@ -195,6 +195,7 @@ bwd_key_strip_kernel(P p)
     }
     float lam = 0.f;
     if constexpr (DIFF) lam = p.lam[s];
+    const uint32_t live = static_cast<uint32_t>(__ballot(key_ok)) & 0xFFFFu;  // keys of the strip inside the grid
     const uint32_t key_local = static_cast<uint32_t>(kx) * p.Wk + ky;  // raster index (causal test)
 
     // a fragment holds one half's channels, or with 16 and 32 channels both halves': the lane groups before kHalfG, and the others
@@ -239,13 +240,14 @@ bwd_key_strip_kernel(P p)
         {
             uint32_t qe = 0, qg = 0;
             if (code >= 0) divmod(static_cast<uint32_t>(code), p.div_n, qe, qg);
-            int32_t match = -1;
+            int32_t match = -1, earlier = 0;
             float lse = 0.f, dq = 0.f;
             float2 second = make_float2(0.f, 0.f);
             if (hf == 0 && code >= 0) {
                 match = p.J[code];
                 if constexpr (DIFF) {
                     const float4 st = p.stats[qg];
+                    if constexpr (MULTI) earlier = p.J[qg];
                     lse = st.x, dq = st.y;
                     second = make_float2(st.z, st.w);
                 } else {
@@ -284,7 +286,7 @@ bwd_key_strip_kernel(P p)
                         *reinterpret_cast<uint4*>((a ? rows_g : rows_q) + (er + kRpi * j) * KS::kRowB +
                                                   (ep + kLR * k) * 16) = val[a][j][k];
             if (hf == 0) {
-                int4 meta = make_int4(-(1 << 30), -(1 << 30), 0, 0);  // no key is near this match
+                int4 meta = make_int4(DIFF ? 0 : -(1 << 30), -(1 << 30), 0, 0);  // no key is near this match
                 if constexpr (kQueryIndex) s_el[wave][t][0] = s_el[wave][t][1] = 0;
                 if (code >= 0) {
                     uint32_t mu, mv;
@@ -297,7 +299,28 @@ bwd_key_strip_kernel(P p)
                         if constexpr (DIFF) local = causal_limit(p, sl, local);
                         s_el[wave][t][1] = static_cast<int32_t>(local);
                     }
-                    if constexpr (MULTI) {
+                    if constexpr (DIFF) {
+                        // the strip's keys that the entry counts for, once for all: in its window, not after the query, in
+                        // none of the query's earlier windows
+                        const int ru = static_cast<int>(mu) - sr0, cv = static_cast<int>(mv) - sc0;
+                        uint32_t in = strip_bits(ru - p.b, ru + p.b, cv - p.b, cv + p.b) & live;
+                        if (kQueryIndex && p.causal) {
+                            uint32_t lr, lc;
+                            divmod(static_cast<uint32_t>(s_el[wave][t][1]), p.div_wk, lr, lc);
+                            const int last = static_cast<int>(lr) - sr0;
+                            in &= strip_bits(0, last - 1, 0, 15) | strip_bits(last, last, 0, static_cast<int>(lc) - sc0);
+                        }
+                        if constexpr (MULTI) {
+                            for (int f = 0; f < static_cast<int>(qe); ++f) {
+                                uint32_t fu, fv;
+                                const int32_t at = f == 0 ? earlier : p.J[static_cast<size_t>(f) * p.n + qg];
+                                divmod(static_cast<uint32_t>(clamp_index(at, p.nkeys)), p.div_wk, fu, fv);
+                                const int hu = static_cast<int>(fu) - sr0, hv = static_cast<int>(fv) - sc0;
+                                in &= ~strip_bits(hu - p.b, hu + p.b, hv - p.b, hv + p.b);
+                            }
+                        }
+                        meta.x = static_cast<int>(in);
+                    } else if constexpr (MULTI) {
                         // the centres of the query's windows 0 .. e-1 (loaded together), then the strip's
                         // keys their (2 b + 1)^2 neighbourhoods hold
                         int32_t pc[kMaxKappa - 1];
@@ -360,6 +383,18 @@ bwd_key_strip_kernel(P p)
             for (int r = 0; r < 4; ++r) {
                 const int te = et * 16 + 4 * g4 + r;
                 const int4 mt = s_meta[wave][te];
+                if constexpr (DIFF) {
+                    const float2 st = s_second[wave][te];
+                    const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[et][r], p.scale_log2e, -__int_as_float(mt.z)));
+                    const float p2 = lam * __builtin_amdgcn_exp2f(fmaf(sc2[et][r], p.scale_log2e, -st.x));
+                    // (selected by bits: a key that is left out may hold anything)
+                    const uint32_t in = static_cast<uint32_t>(__builtin_amdgcn_sbfe(mt.x, m, 1));
+                    auto kept = [&](float x) { return __uint_as_float(__float_as_uint(x) & in); };
+                    wd[4 * et + r] = kept(p1 - p2);
+                    d1[4 * et + r] = kept(p1 * (dp[et][r] - __int_as_float(mt.w)));
+                    d2[4 * et + r] = kept(p2 * (st.y - dp[et][r]));
+                    continue;
+                }
                 bool ok = key_ok && abs(mt.x - kx) <= p.b && abs(mt.y - ky) <= p.b;
                 if constexpr (MULTI) {
                     // not when an earlier window of the query holds this key (key m of the strip)
@@ -370,15 +405,6 @@ bwd_key_strip_kernel(P p)
                 }
                 const float pr = ok ? __builtin_amdgcn_exp2f(sc[et][r] * p.scale_log2e - __int_as_float(mt.z)) : 0.f;
                 const float dsr = pr * (dp[et][r] - __int_as_float(mt.w));
-                if constexpr (DIFF) {
-                    const float2 st = s_second[wave][te];
-                    const float p2 = lam * __builtin_amdgcn_exp2f(sc2[et][r] * p.scale_log2e - st.x);
-                    // (selected: a key that is left out may hold anything)
-                    wd[4 * et + r] = ok ? pr - p2 : 0.f;
-                    d1[4 * et + r] = ok ? dsr : 0.f;
-                    d2[4 * et + r] = ok ? -p2 * (dp[et][r] - st.y) : 0.f;
-                    continue;
-                }
                 split3(pr, ph[4 * et + r], pm[4 * et + r], pl[4 * et + r]);
                 split3(dsr, sh[4 * et + r], sm[4 * et + r], sl[4 * et + r]);
             }
