@@ -10,6 +10,9 @@ import torch
 
 #: half a step of each type, relative to the value: one rounding is off by at most this
 U32 = 2.0 ** -24
+#: fp32 holds nothing under 2^-126 in full: a weight that small may come out as 0, and so may what is left of its
+#: exponential, its product with the normaliser or with lam, its parts in fewer bits, and its score's gradient's three parts
+TINY = 8 * 2.0 ** -126
 HALF = {torch.float32: U32, torch.bfloat16: 2.0 ** -8}
 
 
@@ -43,7 +46,8 @@ def differential(Q, K, V, mask, lam, scale, dO=None):
     # a weight is off by twice its score's error (it and the normaliser) and by the exponentials' two roundings; the sums over
     # a query's keys by a rounding each, and a few for the products and the end
     rel = 2 * delta + (float(mask.sum(2).max()) + 24) * U32
-    out, out_tol = w @ v, rel * (pw @ v.abs())
+    on = mask.double()
+    out, out_tol = w @ v, rel * (pw @ v.abs()) + TINY * (1 + lam.abs()) * (on @ v.abs())
     if dO is None:
         return out, out_tol
     do = dO.reshape(S, -1, d if V.shape[-1] == d else V.shape[-1]).double()
@@ -52,6 +56,7 @@ def differential(Q, K, V, mask, lam, scale, dO=None):
     c = [torch.ones_like(lam), -lam]
     ds = [c[i] * p[i] * (dp - D[i]) * scale for i in (0, 1)]
     dsa = [c[i].abs() * p[i] * (dpa + Da[i]) * abs(scale) for i in (0, 1)]
+    tiny = [TINY * on * (1 + c[i].abs() * (dpa + Da[i]) * abs(scale)) for i in (0, 1)]
     halves = (slice(0, h), slice(h, d))
     dQ = torch.cat([ds[i] @ k[..., s] for i, s in enumerate(halves)], 2)
     dK = torch.cat([ds[i].transpose(1, 2) @ q[..., s] for i, s in enumerate(halves)], 2)
@@ -61,9 +66,9 @@ def differential(Q, K, V, mask, lam, scale, dO=None):
     kmax = k.abs().amax(1, keepdim=True)
     tol = rel + 16 * U32
     many = float(mask.sum(1).max()) * U32  # a key's queries, one after another
-    dQ_tol = 3 * tol * torch.cat([dsa[i].sum(2, keepdim=True) * 2 * kmax[..., s] for i, s in enumerate(halves)], 2)
-    dK_tol = (2 * tol + many) * torch.cat([dsa[i].transpose(1, 2) @ q[..., s].abs() for i, s in enumerate(halves)], 2)
-    dV_tol = (tol + many) * (pw.transpose(1, 2) @ do.abs())
+    dQ_tol = torch.cat([(3 * tol * dsa[i] + tiny[i]).sum(2, keepdim=True) * 2 * kmax[..., s] for i, s in enumerate(halves)], 2)
+    dK_tol = torch.cat([((2 * tol + many) * dsa[i] + tiny[i]).transpose(1, 2) @ q[..., s].abs() for i, s in enumerate(halves)], 2)
+    dV_tol = ((tol + many) * pw + TINY * (1 + lam.abs()) * on).transpose(1, 2) @ do.abs()
     dlam_tol = 2 * tol * Da[1].sum((1, 2))
     return out, out_tol, (dQ, dK, dV, dlam), (dQ_tol, dK_tol, dV_tol, dlam_tol)
 

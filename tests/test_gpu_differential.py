@@ -92,6 +92,35 @@ def test_shapes(scram, c, dtype):
     run(scram, dict(c, dtype=dtype))
 
 
+def many(c):
+    """The same with slices enough for more than 4096 queries: those of fewer take another way forward."""
+    return dict(c, S=4096 // (c["q"][0] * c["q"][1]) + 1)
+
+
+MANY = SHAPES[:-1] + [
+    dict(S=1, q=(20, 23), d=64, window=9, kappa=1, causal=True),
+    dict(S=1, q=(24, 17), d=128, window=9, kappa=2),
+    dict(S=1, q=(13, 30), k=(30, 13), d=32, window=9, kappa=4),
+    dict(S=1, q=(1, 2), k=(40, 1), d=64, window=7, kappa=2),
+    dict(S=1, q=(5, 4), k=(1, 33), d=32, window=5, kappa=3),
+    dict(S=1, q=(16, 16), k=(2, 2), d=64, window=3, kappa=2),
+]
+
+
+@pytest.mark.parametrize("maps", ["mixed", "random", "constant", "corners"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", MANY, ids=lambda c: f"{c['q'][0]}x{c['q'][1]}_d{c['d']}_w{c['window']}_k{c['kappa']}" + ("_causal" if c.get("causal") else ""))
+def test_many_slices(scram, c, dtype, maps):
+    run(scram, dict(many(c), dtype=dtype, maps=maps), seed=12)
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_scores_far_apart(scram, d, causal):
+    """Scores of hundreds: references are raised on the way, weights underflow, a query's first match may have no weight."""
+    run(scram, dict(many(dict(S=1, q=(18, 22), d=d, window=5, kappa=2)), scale=4.0, causal=causal, dtype="bf16", maps="random"), seed=13)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("maps", ["random", "constant", "own", "corners"])
 @pytest.mark.parametrize("c", [dict(S=2, q=(24, 28), d=64, window=5, kappa=2), dict(S=1, q=(32, 24), d=32, window=3, kappa=1, causal=True),
