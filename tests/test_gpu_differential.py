@@ -114,6 +114,56 @@ def test_many_slices(scram, c, dtype, maps):
     run(scram, dict(many(c), dtype=dtype, maps=maps), seed=12)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S", [40, 140])
+@pytest.mark.parametrize("c", [dict(d=64, window=3, kappa=1), dict(d=32, window=5, kappa=2, causal=True), dict(d=16, window=7, kappa=1, causal=True),
+                               dict(d=128, window=5, kappa=1)], ids=["w3", "w5_two_causal", "w7_causal", "wide"])
+def test_more_strips_of_keys(scram, c, S, dtype):
+    """Fewer waves take each strip of keys where there are many of them."""
+    run(scram, dict(c, S=S, q=(23, 26), maps="mixed" if S == 40 else "random", dtype=dtype), seed=14)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("maps", ["constant", "corners"])
+@pytest.mark.parametrize("c", [dict(d=64, window=7, kappa=1), dict(d=32, window=3, kappa=3, causal=True), dict(d=64, window=15, kappa=2)],
+                         ids=["w7", "w3_three_causal", "w15_two"])
+def test_keys_of_thousands_of_queries(scram, c, maps, dtype):
+    run(scram, dict(c, S=1, q=(70, 66), maps=maps, dtype=dtype), seed=15)
+
+
+@pytest.mark.parametrize("window,kappa", [(11, 1), (13, 2), (15, 1), (19, 1)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_windows(scram, window, kappa, dtype):
+    run(scram, dict(S=12, q=(19, 21), d=64, window=window, kappa=kappa, causal=kappa == 2, dtype=dtype), seed=16)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("window,kappa", [(5, 1), (3, 2)])
+def test_gradients_that_are_not_finite_reach_their_keys_alone(scram, window, kappa, dtype):
+    """One query's dO holds an infinity, another's row a NaN: their own rows and their keys' are hit, all others are right."""
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    S, H, W, d, kind = 2, 22, 25, 64, TYPES[dtype]
+    Q, K, V, dO = (rows(gen, kind, S, H, W, d) for _ in range(4))
+    lam = torch.tensor([0.4, 0.7], device="cuda")
+    J = maps_of("mixed", gen, kappa, S, H, W, H, W)
+    mask = ref.key_mask(J, H, W, H, W, window)
+    _, _, want, tol = ref.differential(Q, K, V, mask, lam, 32 ** -0.5, dO)
+    bad = [100, 333]
+    dO[0].view(-1, d)[bad[0], 5] = float("inf")
+    Q[0].view(-1, d)[bad[1], 50] = float("nan")
+    dQ, dK, dV, dlam = scram.differential_attend_backward(Q, K, V, J, lam, dO, window)
+    hit_q = torch.zeros(S, H * W, dtype=torch.bool, device="cuda")
+    hit_q[0, bad] = True
+    hit_k = mask[0, bad].any(0)
+    hit_k = torch.stack([hit_k, torch.zeros_like(hit_k)])
+    for name, g, w, t, hit in zip(("dQ", "dK", "dV"), (dQ, dK, dV), want, tol, (hit_q, hit_k, hit_k)):
+        off = (g.view(S, H * W, d).double() - w).abs()
+        # (a query's good keys' rows also hold sums of the clean terms that the bad queries would have given: not compared)
+        assert (off[~hit] <= t[~hit]).all(), name
+        assert (~g.view(S, H * W, d).isfinite()).any(2)[hit].all(), name
+    assert not dlam[0].isfinite() and abs(float(dlam[1] - want[3][1])) <= float(tol[3][1])
+
+
 @pytest.mark.parametrize("d", [32, 64, 128])
 @pytest.mark.parametrize("causal", [False, True])
 def test_scores_far_apart(scram, d, causal):
@@ -336,3 +386,29 @@ def test_two_streams_at_once(scram):
                 assert torch.equal(w[i], g[i])
             for i in (2, 3):
                 assert torch.allclose(w[i], g[i], rtol=1e-5, atol=1e-5 * float(w[i].abs().max()))
+
+
+def test_two_graphs_share_a_workspace(scram):
+    """Captured in turn over one workspace and replayed in any order, one after the other."""
+    gen = torch.Generator(device="cuda").manual_seed(18)
+    made = []
+    for H, W, window, causal in ((31, 40, 5, True), (44, 28, 3, False)):
+        Q, K, V, dO = (rows(gen, torch.bfloat16, 2, H, W, 64) for _ in range(4))
+        made.append(((Q, K, V, maps_of("mixed", gen, 2, 2, H, W, H, W), torch.rand(2, generator=gen, device="cuda"), dO, window), causal))
+    size = max(scram.differential_attend_backward_workspace_bytes(*a[0].shape[:3], *a[0].shape[1:3], 2, d=64, dtype=a[0].dtype) for a, _ in made)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    want = [scram.differential_attend_backward(*a, causal=c) for a, c in made]
+    graphs, got = [], []
+    torch.cuda.synchronize()
+    for a, c in made:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            got.append(scram.differential_attend_backward(*a, causal=c, workspace=ws))
+    for turn in (0, 1, 1, 0, 1):
+        for g in got[turn]:
+            g.fill_(3.0)
+        ws.fill_(0x5A)
+        graphs[turn].replay()
+        torch.cuda.synchronize()
+        for i, (w, g) in enumerate(zip(want[turn], got[turn])):
+            assert torch.equal(w, g) if i in (0, 3) else torch.allclose(w, g, rtol=1e-5, atol=1e-5 * float(w.abs().max()))
