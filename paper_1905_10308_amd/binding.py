@@ -546,6 +546,14 @@ def _paddable(*tensors) -> bool:
                for t in tensors) and q.dtype in (torch.float32, torch.bfloat16)
 
 
+def _int32(name, x):
+    """``x`` as an int that a C int holds."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} is an int32, got {x}")
+    return x
+
+
 def _placed(Q, K, norm, positions, groups):
     """Q and K normalised and turned by their grid positions, where asked for."""
     from .rows import layer_norm, rotary

@@ -33,6 +33,7 @@ def _rows(Q, K, V, argmax, lam, first, causal, dO=None):
         first, origin = 0, _b._plain("first", first, 1, torch.int32, index)
         if origin.shape[0] != S:
             raise ValueError(f"first must be a place for each of {S} slices")
+    first = _b._int32("first", first)
     if not causal and (first or origin is not None):
         raise ValueError("first is the queries' place under the causal mask: it needs causal=True")
     return (S, Hq, Wq, Hk, Wk), d, dv, argmax.shape[0] if maps == 4 else 1, int(first), origin

@@ -11,6 +11,7 @@ from . import binding as _b
 
 ROTARY_INTERLEAVED = 1
 ROTARY_INVERSE = 2
+MAX_PAIRS = 128
 
 
 @functools.lru_cache(maxsize=256)
@@ -25,6 +26,8 @@ def _pairs(sections, freqs, base, pairs, axes):
         sections = (0,) + sections
     if len(sections) != 3 or min(sections) < 0:
         raise ValueError(f"sections must be the pairs of (time,) height and width, got {sections}")
+    if sum(sections) > MAX_PAIRS:
+        raise ValueError(f"at most {MAX_PAIRS} pairs are turned, got {sections}")
     if freqs is None:
         if not base > 0:
             raise ValueError("base must be positive")
@@ -64,7 +67,9 @@ def _rotate(tensors, sections, base, freqs, origin, groups, interleaved, out, in
             raise ValueError("origin must be int32 [3], [1, 3] or [S, 3]: time, height, width")
         rows = origin.numel() // 3
     else:
-        at = tuple(int(a) for a in origin)
+        at = tuple(_b._int32("origin", a) for a in origin)
+        if len(at) > 3:
+            raise ValueError(f"origin is time, height, width, got {at}")
         at = _INTS[3](*((0,) * (3 - len(at)) + at))
         origin = None
     if out is None:

@@ -93,6 +93,32 @@ def test_rotary_defaults_own_frequencies_and_images(scram):
     assert torch.equal(scram.rotary(x, origin=(3, 4)), scram.rotary(x, origin=(0, 3, 4)))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("slices,per_slice", [((1,), False), ((70001, 5), False), ((4099, 4099), True), ((3, 300, 2047, 2049), False)])
+def test_rotary_of_single_pixels(scram, slices, per_slice, dtype):
+    """Many slices of one pixel: their rows share blocks."""
+    gen = torch.Generator(device="cuda").manual_seed(19)
+    xs = [torch.randn(s, 1, 1, 20, generator=gen, device="cuda").to(TYPES[dtype]) for s in slices]
+    at = torch.randint(-3000, 3000, (slices[0] if per_slice else 1, 3), generator=gen, device="cuda", dtype=torch.int32)
+    freqs = [10000.0 ** (-j / m) for m in (4, 5) for j in range(m)]
+    got = scram.rotary(*xs, origin=at, sections=(4, 5))
+    for x, y in zip(xs, got if len(xs) > 1 else [got]):
+        want = ref.rotary(x[:, None], (0, 4, 5), freqs, at)
+        near(y[:, None], want, rotary_tolerance(x[:, None], want, 9, 1, False, 3001), "pixels")
+
+
+def test_rotary_of_the_most_slices(scram):
+    """2^31 - 1 slices of one pixel of two channels: the last ones are turned."""
+    n = (1 << 31) - 1
+    x = torch.zeros(n, 1, 1, 2, dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn(4096, 1, 1, 2, generator=torch.Generator(device="cuda").manual_seed(20), device="cuda").bfloat16()
+    x[-4096:], x[:4096] = tail, tail
+    scram.rotary(x, origin=(0, 2, 0), sections=(1, 0), out=x)
+    want = ref.rotary(tail[:, None], (0, 1, 0), [1.0], torch.tensor([[0, 2, 0]], device="cuda"))
+    for y in (x[-4096:], x[:4096]):
+        near(y[:, None], want, rotary_tolerance(tail[:, None], want, 1, 1, False, 3), "slices")
+
+
 def test_rotary_replays(scram):
     gen = torch.Generator(device="cuda").manual_seed(3)
     x = torch.randn(8, 1, 1, 64, generator=gen, device="cuda").bfloat16()

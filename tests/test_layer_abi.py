@@ -153,3 +153,17 @@ def test_binding_rejects():
             call()
     with pytest.raises(ValueError):
         scram.rotary()
+
+
+def test_numbers_that_no_c_int_holds():
+    """They are refused, not cut to 32 bits."""
+    from paper_1905_10308_amd import binding, rows
+
+    assert binding._int32("first", (1 << 31) - 1) == (1 << 31) - 1 and binding._int32("origin", -(1 << 31)) == -(1 << 31)
+    for x in (1 << 31, -(1 << 31) - 1, 1 << 32):
+        with pytest.raises(ValueError, match="int32"):
+            binding._int32("first", x)
+    with pytest.raises(ValueError, match="pairs"):
+        rows._pairs((1 << 40, 0, 0), None, 10000.0, 8, 3)
+    with pytest.raises(ValueError, match="sections"):
+        rows._pairs((1, 1, 1, 1), None, 10000.0, 8, 3)
