@@ -67,8 +67,10 @@ __device__ __forceinline__ float diff_query_gradient(const DiffParams& p, uint32
     }
     float kref[2 * H];
     {
-        uint4 kr0[2];
-        load_row<T, D, G>(Ks, clamp_index(p.J[g], p.nkeys), lane, kr0);
+        uint4 kr0[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+        const uint32_t at = static_cast<uint32_t>(clamp_index(p.J[g], p.nkeys));
+        // (a match after the query is not in its set: its row stays out, and k_ref is 0)
+        if (!MULTI || !p.causal || at <= ws.local) load_row<T, D, G>(Ks, at, lane, kr0);
         unpack_row<T, 2>(kr0, kref);
     }
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, dn[2] = {0.f, 0.f};

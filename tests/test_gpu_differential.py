@@ -273,6 +273,27 @@ def test_rows_outside_the_sets_do_not_reach_the_result(scram, few, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hq", [2, 64])
+def test_matches_after_the_query_may_hold_anything(scram, Hq, dtype):
+    """The rows behind the last query hold NaN and infinities, and half of the first matches are there."""
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    S, H, W, d, kind = 1, Hq + 5, 65, 64, TYPES[dtype]
+    n = Hq * W
+    K, V = rows(gen, kind, S, H, W, d), rows(gen, kind, S, H, W, d)
+    Q, dO = rows(gen, kind, S, Hq, W, d), rows(gen, kind, S, Hq, W, d)
+    lam = torch.rand(S, generator=gen, device="cuda")
+    J = maps_of("own", gen, 2, S, Hq, W, H, W) % n
+    J[0] = torch.where(torch.rand(J[0].shape, generator=gen, device="cuda") < 0.5, n + J[0] % (5 * W), J[0])
+    mask = ref.key_mask(J, Hq, W, H, W, 5, True)
+    K.view(S, H * W, d)[:, n:], V.view(S, H * W, d)[:, n:] = 0, 0
+    want, tol, wg, tg = ref.differential(Q, K, V, mask, lam, 32 ** -0.5, dO)
+    K.view(S, H * W, d)[:, n:], V.view(S, H * W, d)[:, n:] = float("nan"), float("inf")
+    check(scram.differential_attend(Q, K, V, J, lam, 5, causal=True), want, tol + ref.HALF[kind] * (want.abs() + tol), "output")
+    for name, g, w, t in zip(("dQ", "dK", "dV", "dlam"), scram.differential_attend_backward(Q, K, V, J, lam, dO, 5, causal=True), wg, tg):
+        check(g, w, t, name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_values_that_are_not_finite_reach_their_queries_alone(scram, dtype):
     gen = torch.Generator(device="cuda").manual_seed(7)
     S, H, W, d, kind = 1, 70, 72, 64, TYPES[dtype]
