@@ -13,6 +13,12 @@
 //   scram_backward.hip -- gradients of the attend step (maps held fixed)
 //   scram_snis.hip     -- self-normalised importance sampling around the
 //                         matches (Section 4.2, Equations 11-17)
+//   scram_diff.hip, scram_diff_backward.hip
+//                      -- the difference of two softmax maps over the windows,
+//                         and its gradients
+//   scram_rotary.hip, scram_norm.hip
+//                      -- what a layer does to the rows before and after:
+//                         rotary grid positions, layer norm
 //
 // Everything here lives in an unnamed namespace: each kernel file gets its
 // own copy.

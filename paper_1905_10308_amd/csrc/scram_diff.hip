@@ -94,7 +94,9 @@ __device__ __forceinline__ void diff_query(const DiffParams& p, uint32_t g, int 
     store_row<T, D, G>(p.out, g, lane, o, 1.f);
 }
 
-// A lane group per query (WAVE: a wave per query, for calls of a few queries); kNb keys at a time: three, or five for one
+// A lane group per query (WAVE: a wave per query, for calls of up to 4096 queries, which lane groups would leave most of the
+// machine without; 32 single pixels take 11 us, most of it the launch).  fp32 8 x 128 x 128 -> 192 x 192, 32 channels, causal
+// or two windows: 37-45 us, its bytes 21 us at a copy's rate.  kNb keys at a time: three, or five for one
 // 5 x 5 window, which is then five whole batches (8 x 128 x 128, 32 channels, fp32: two 3 x 3 windows with four 44 us, three
 // 38, five 40; one 5 x 5 window 38, 40, 32).
 template <typename T, int D, int G, int MK, int kNb, bool WAVE>
@@ -119,7 +121,11 @@ constexpr int diff_tile_waves(int D, int MK) { return D == 128 ? 2 : MK == 4 ? 3
 //   O1^T += V_blk^T P1^T, O2^T += V_blk^T P2^T
 // with the weights as two bf16 parts (18 bits: the output keeps 8), and at the end o = O1 / l1 - lam O2 / l2.  A query whose sums are
 // not finite (an infinite value of the box reaches every query of its cluster through 0 * inf, a score that is not a number
-// passes its mask), or whose set is empty, is computed over again on a lane group, and so are a wave's queries whose matches lie too far apart to share rows.
+// passes its mask), or whose set is empty, is computed over again on a lane group, and so are a wave's queries whose matches
+// lie too far apart to share rows.
+// 4 x 256 x 256, 64 channels, two 5 x 5 windows: 114 us (a lane group per query 175; its bytes 26 us at a copy's rate), the
+// vector units issuing in 71 % of the cycles and the loads' return path busy in 79 %, at 4 waves per SIMD (3 the same, 5 spill:
+// 284 us).  Weights of three parts were slower and change no bit that the output keeps.
 template <int D, int W, bool CAUSAL, int MK>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(diff_tile_waves(D, MK)))) void
 diff_tile_kernel(DiffParams p)

@@ -175,6 +175,8 @@ constexpr int diff_grad_waves(int D) { return D == 128 ? 1 : D == 64 ? 2 : 3; }
 // first match, dQ = scale ((A - dn k_ref) - D (B - l k_ref)) / l: the lane group's sums, whose subtraction cancels no more.
 // A query whose sums are not finite, or whose set is empty, is computed over again on a lane group, and so are a wave's
 // queries whose matches lie too far apart to share rows.
+// 16 x 128 x 128, 64 channels, two 5 x 5 windows: 190 us, at 2 waves per SIMD the vector units (splitting the weights) issuing
+// in 68 % of the cycles, the loads' return path busy in 73 %, the matrix cores in 32 %.
 template <int D, int W, bool CAUSAL, int MK>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(diff_grad_waves(D)))) void
 diff_query_tile_kernel(DiffParams p)
@@ -479,6 +481,8 @@ __global__ __launch_bounds__(kBlock) void diff_heavy_kernel(DiffParams p)
 //       takes dS1 and dS2 in turn
 // A chunk's rows load while the previous chunk is in the matrix cores, the entry codes a chunk before that.  A strip of more
 // entries than p.heavy_entries, or whose sums are not finite, leaves its keys to the list.
+// 4 x 93 x 125, 32 channels, two 3 x 3 windows: 30-35 us, waiting on results in 43 % of the waves' cycles with 1.7 waves on a
+// SIMD.
 // ---------------------------------------------------------------------------
 template <int D>
 struct DiffStripLds {
@@ -802,6 +806,7 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
             pt.tk = make_tiling(p.Hk, p.Wk, kTileKeys);
             const uint64_t halo = static_cast<uint64_t>(std::min(4 + 2 * p.b, p.Hk)) * std::min(4 + 2 * p.b, p.Wk);
             const uint64_t mean = static_cast<uint64_t>(p.n) * p.kappa * halo / p.keys_total;  // entries of a strip
+            // (a strip of thousands of entries would run on alone; lower and higher limits were slower)
             pt.heavy_entries = static_cast<int>(std::min<uint64_t>(std::max<uint64_t>(1024, 4 * mean), INT32_MAX));
             const uint64_t strips = kStripWaves * tiling_blocks(pt.tk, S);
             auto with = [&](auto mode, auto team) {

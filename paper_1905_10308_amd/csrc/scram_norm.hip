@@ -12,6 +12,9 @@
 // pass are of the row and then of its centred values, so that a row's offset
 // costs no accuracy.
 //
+// 262144 x 64 bf16: forward 14.7 us (67 MB and the statistics; 13.4 at a copy's
+// rate), backward with fp32 gradients 41 us (33); 8192 x 4096 backward 51 (39).
+//
 // The weights' gradients: a block keeps those of its rows in registers,
 // adds them up over its threads once at its end and writes one row of parts;
 // a second kernel adds up the parts, in a fixed order.

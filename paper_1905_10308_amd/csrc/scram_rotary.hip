@@ -4,8 +4,10 @@
 //   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = position * frequency
 //
 // The gradient is the rotation by -t.  One pass, read and written once: bound
-// by memory.  The angles of a pixel's pairs are the same in every slice and
-// tensor, so a thread computes those of its pairs once and walks the slices.
+// by memory (Q and K of 4 x 256 x 256, 64 channels, bf16: 134 MB in 24-28 us;
+// 6 x 16 x 45 x 80, 100 channels, fp32: 276 MB in 56-61; a copy moves 5.15 TB/s).  The
+// angles of a pixel's pairs are the same in every slice and tensor, so a thread
+// computes those of its pairs once and walks the slices.
 
 #include <algorithm>
 
