@@ -433,3 +433,34 @@ def test_two_graphs_share_a_workspace(scram):
         torch.cuda.synchronize()
         for i, (w, g) in enumerate(zip(want[turn], got[turn])):
             assert torch.equal(w, g) if i in (0, 3) else torch.allclose(w, g, rtol=1e-5, atol=1e-5 * float(w.abs().max()))
+
+
+@pytest.mark.parametrize("c", [dict(S=2, q=(72, 67), d=64, window=5, kappa=2), dict(S=1, q=(9, 1100), d=64, window=3, kappa=1, causal=True),
+                               dict(S=2, q=(12, 700), d=32, window=3, kappa=2), dict(S=20, q=(1, 300), d=32, window=7, kappa=1),
+                               dict(S=16, q=(300, 1), d=64, window=3, kappa=1), dict(S=2, q=(56, 56), k=(23, 31), d=64, window=9, kappa=1),
+                               dict(S=2, q=(50, 50), d=128, window=5, kappa=2), dict(S=3, q=(31, 70), d=16, window=7, kappa=1)],
+                         ids=lambda c: f"{c['q'][0]}x{c['q'][1]}_d{c['d']}_w{c['window']}")
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_results_do_not_depend_on_the_launch(scram, c, dtype):
+    """The same calls through a build with other lane-group tiles, bands of tiles and dispatch order."""
+    from paper_1905_10308_amd import binding
+
+    gen = torch.Generator(device="cuda").manual_seed(22)
+    S, Hq, Wq, Hk, Wk, d, kind = c["S"], *c["q"], *c.get("k", c["q"]), c["d"], TYPES[dtype]
+    Q, dO = rows(gen, kind, S, Hq, Wq, d, size=1.5), rows(gen, kind, S, Hq, Wq, d)
+    K, V = rows(gen, kind, S, Hk, Wk, d), rows(gen, kind, S, Hk, Wk, d)
+    J, lam = maps_of("mixed", gen, c["kappa"], S, Hq, Wq, Hk, Wk), torch.rand(S, generator=gen, device="cuda")
+    go = lambda: (scram.differential_attend(Q, K, V, J, lam, c["window"], causal=c.get("causal", False)),  # noqa: E731
+                  *scram.differential_attend_backward(Q, K, V, J, lam, dO, c["window"], causal=c.get("causal", False)))
+    want = go()
+    saved = binding.lib()
+    binding._lib = binding.load(binding.ORDER_LIB_PATH)
+    try:
+        for _ in range(2):
+            got = go()
+            torch.cuda.synchronize()
+            for i, (g, w) in enumerate(zip(got, want)):
+                # dK and dV: in the order that the inverse map was filled in; dlam: its parts in the order of the tiles
+                assert torch.equal(g, w) if i < 2 else torch.allclose(g, w, rtol=1e-5, atol=1e-5 * float(w.abs().max())), i
+    finally:
+        binding._lib = saved
