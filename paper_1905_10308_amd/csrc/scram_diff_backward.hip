@@ -520,6 +520,9 @@ __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 
     const int lane = threadIdx.x & 63, wave = TEAM > 1 ? threadIdx.x >> 6 : 0, m = lane & 15, g4 = lane >> 4;
     Lds& lds = all[wave];
     constexpr int kStep = kStripFE * TEAM;
+    // 128 channels: no rows in flight, so that two waves fit a SIMD (8 x 128 x 128, two 5 x 5 windows: strips 343 us, one wave
+    // with them 411, keys on lane groups 697)
+    constexpr bool kAhead = D < 128;
     const KeyStripF t(p.tk, xcd_remap(blockIdx.x, gridDim.x));
     if (t.sr0 >= p.Hk || t.sc0 >= p.Wk) return;  // the strip lies past the grid's edge
     int nrows;
@@ -587,9 +590,10 @@ __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 
         }
     };
     code = slot_code(kStripFE * wave);
-    fetch();
+    if constexpr (kAhead) fetch();
     int next = slot_code(kStripFE * wave + kStep);
     for (int c0 = kStripFE * wave; c0 < E; c0 += kStep) {
+        if constexpr (!kAhead) fetch();
 #pragma unroll
         for (int j = 0; j < kRep; ++j) {
             *reinterpret_cast<f32x4_t*>(lds.q + (er + kRpi * j) * kRowF + 4 * ep) = rq[j];
@@ -626,7 +630,8 @@ __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 
             lds.meta[m] = meta;
         }
         code = next;
-        if (c0 + kStep < E) fetch();
+        if constexpr (kAhead)
+            if (c0 + kStep < E) fetch();
         next = slot_code(c0 + 2 * kStep);
         wave_lds_sync();
 
@@ -798,35 +803,33 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
                          : launch(diff_query_kernel<T, D, G, kMaxKappa>, qblocks, st, nullptr, nullptr, p);
     if (e != hipSuccess) return e;
     if ((e = run_inverse(p, counts, offsets, sums, entries, st, nullptr, nullptr)) != hipSuccess) return e;
-    // Key side on the matrix cores for windows 3 x 3 .. 15 x 15 (fp32: up to 64 channels); the keys that its strips leave, and
-    // those of every other call with many entries, a wave each.
-    if constexpr (std::is_same<T, uint16_t>::value || D <= 64) {
-        if (p.b >= 1 && p.b <= kTileMaxB && p.nkeys > 1) {  // (one key: dP - D is exactly 0 on the lane groups)
-            DiffParams pt = p;
-            pt.tk = make_tiling(p.Hk, p.Wk, kTileKeys);
-            const uint64_t halo = static_cast<uint64_t>(std::min(4 + 2 * p.b, p.Hk)) * std::min(4 + 2 * p.b, p.Wk);
-            const uint64_t mean = static_cast<uint64_t>(p.n) * p.kappa * halo / p.keys_total;  // entries of a strip
-            // (a strip of thousands of entries would run on alone; lower and higher limits were slower)
-            pt.heavy_entries = static_cast<int>(std::min<uint64_t>(std::max<uint64_t>(1024, 4 * mean), INT32_MAX));
-            const uint64_t strips = kStripWaves * tiling_blocks(pt.tk, S);
-            auto with = [&](auto mode, auto team) {
-                constexpr int MODE = decltype(mode)::value, TEAM = decltype(team)::value;
-                if constexpr (std::is_same<T, float>::value)
-                    return launch_wave<64 * TEAM>(diff_key_strip_f32_kernel<D, MODE, TEAM>, strips, st, nullptr, nullptr, pt);
-                else
-                    return launch_wave<64 * TEAM>(bwd_key_strip_kernel<D, MODE, DiffParams, TEAM>, strips, st, nullptr, nullptr, pt);
-            };
-            auto go = [&](auto mode) {
-                return strips <= kTeamStrips ? with(mode, std::integral_constant<int, 4>{})
-                       : strips <= 4 * kTeamStrips ? with(mode, std::integral_constant<int, 2>{})
-                                                   : with(mode, std::integral_constant<int, 1>{});
-            };
-            e = !MULTI         ? go(std::integral_constant<int, kStripPlain>{})
-                : p.kappa == 1 ? go(std::integral_constant<int, kStripCausal>{})
-                               : go(std::integral_constant<int, kStripMulti>{});
-            if (e != hipSuccess) return e;
-            return launch(diff_heavy_kernel<T, D, G, MULTI>, 1024, st, nullptr, stop, p);
-        }
+    // Key side on the matrix cores for windows 3 x 3 .. 15 x 15; the keys that its strips leave, and those of every other call
+    // with many entries, a wave each.
+    if (p.b >= 1 && p.b <= kTileMaxB && p.nkeys > 1) {  // (one key: dP - D is exactly 0 on the lane groups)
+        DiffParams pt = p;
+        pt.tk = make_tiling(p.Hk, p.Wk, kTileKeys);
+        const uint64_t halo = static_cast<uint64_t>(std::min(4 + 2 * p.b, p.Hk)) * std::min(4 + 2 * p.b, p.Wk);
+        const uint64_t mean = static_cast<uint64_t>(p.n) * p.kappa * halo / p.keys_total;  // entries of a strip
+        // (a strip of thousands of entries would run on alone; lower and higher limits were slower)
+        pt.heavy_entries = static_cast<int>(std::min<uint64_t>(std::max<uint64_t>(1024, 4 * mean), INT32_MAX));
+        const uint64_t strips = kStripWaves * tiling_blocks(pt.tk, S);
+        auto with = [&](auto mode, auto team) {
+            constexpr int MODE = decltype(mode)::value, TEAM = decltype(team)::value;
+            if constexpr (std::is_same<T, float>::value)
+                return launch_wave<64 * TEAM>(diff_key_strip_f32_kernel<D, MODE, TEAM>, strips, st, nullptr, nullptr, pt);
+            else
+                return launch_wave<64 * TEAM>(bwd_key_strip_kernel<D, MODE, DiffParams, TEAM>, strips, st, nullptr, nullptr, pt);
+        };
+        auto go = [&](auto mode) {
+            return strips <= kTeamStrips ? with(mode, std::integral_constant<int, 4>{})
+                   : strips <= 4 * kTeamStrips ? with(mode, std::integral_constant<int, 2>{})
+                                               : with(mode, std::integral_constant<int, 1>{});
+        };
+        e = !MULTI         ? go(std::integral_constant<int, kStripPlain>{})
+            : p.kappa == 1 ? go(std::integral_constant<int, kStripCausal>{})
+                           : go(std::integral_constant<int, kStripMulti>{});
+        if (e != hipSuccess) return e;
+        return launch(diff_heavy_kernel<T, D, G, MULTI>, 1024, st, nullptr, stop, p);
     }
     if ((e = launch(diff_key_kernel<T, D, G, MULTI>, kblocks, st, nullptr, nullptr, p)) != hipSuccess) return e;
     return launch(diff_heavy_kernel<T, D, G, MULTI>, 1024, st, nullptr, stop, p);  // loops over however many there are
