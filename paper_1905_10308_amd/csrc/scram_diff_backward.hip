@@ -803,9 +803,12 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
                          : launch(diff_query_kernel<T, D, G, kMaxKappa>, qblocks, st, nullptr, nullptr, p);
     if (e != hipSuccess) return e;
     if ((e = run_inverse(p, counts, offsets, sums, entries, st, nullptr, nullptr)) != hipSuccess) return e;
-    // Key side on the matrix cores for windows 3 x 3 .. 15 x 15; the keys that its strips leave, and those of every other call
+    // Key side on the matrix cores for windows 3 x 3 .. 15 x 15, and of one key where bf16 has several maps; the keys that its strips leave, and those of every other call
     // with many entries, a wave each.
-    if (p.b >= 1 && p.b <= kTileMaxB && p.nkeys > 1) {  // (one key: dP - D is exactly 0 on the lane groups)
+    // (Sets of one key: dP - D is exactly 0 on the lane groups.  Windows of one key, several maps: 4 x 256 x 256, 64 channels,
+    // bf16 two maps 81 us, on lane groups 120; fp32 four maps 278, on lane groups 253.)
+    const int least = std::is_same<T, uint16_t>::value && p.kappa > 1 ? 0 : 1;
+    if (p.b >= least && p.b <= kTileMaxB && p.nkeys > 1) {
         DiffParams pt = p;
         pt.tk = make_tiling(p.Hk, p.Wk, kTileKeys);
         const uint64_t halo = static_cast<uint64_t>(std::min(4 + 2 * p.b, p.Hk)) * std::min(4 + 2 * p.b, p.Wk);

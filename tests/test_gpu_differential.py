@@ -131,6 +131,14 @@ def test_keys_of_thousands_of_queries(scram, c, maps, dtype):
     run(scram, dict(c, S=1, q=(70, 66), maps=maps, dtype=dtype), seed=15)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 128])
+@pytest.mark.parametrize("maps", ["mixed", "random", "constant"])
+@pytest.mark.parametrize("kappa,causal,S", [(2, False, 3), (4, True, 140)])
+def test_windows_of_one_key(scram, kappa, causal, S, maps, d, dtype):
+    run(scram, dict(S=S, q=(23, 26), d=d, window=1, kappa=kappa, causal=causal, maps=maps, dtype=dtype), seed=23)
+
+
 @pytest.mark.parametrize("window,kappa", [(11, 1), (13, 2), (15, 1), (19, 1)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_windows(scram, window, kappa, dtype):
