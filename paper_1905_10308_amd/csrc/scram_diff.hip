@@ -261,7 +261,11 @@ hipError_t launch_diff_attend(int dtype, const DiffCall& c, void* out, hipStream
         using T = decltype(ty);
         constexpr int D = decltype(d)::value;
         if (p.kappa == 1 && !p.causal) return run_diff<T, D, 0>(p, stream, start, stop);
-        return p.kappa <= 2 ? run_diff<T, D, 2>(p, stream, start, stop) : run_diff<T, D, kMaxKappa>(p, stream, start, stop);
+        // (centres of the windows in registers: 4 x 256 x 256 fp32, 64 channels, four 3 x 3 windows, sized for four 223 us, for
+        // eight 257)
+        return p.kappa <= 2   ? run_diff<T, D, 2>(p, stream, start, stop)
+               : p.kappa <= 4 ? run_diff<T, D, 4>(p, stream, start, stop)
+                              : run_diff<T, D, kMaxKappa>(p, stream, start, stop);
     });
 }
 

@@ -799,8 +799,9 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
     } else if constexpr (!MULTI)
         e = launch(diff_query_kernel<T, D, G, 0>, qblocks, st, nullptr, nullptr, p);
     else
-        e = p.kappa <= 2 ? launch(diff_query_kernel<T, D, G, 2>, qblocks, st, nullptr, nullptr, p)
-                         : launch(diff_query_kernel<T, D, G, kMaxKappa>, qblocks, st, nullptr, nullptr, p);
+        e = p.kappa <= 2   ? launch(diff_query_kernel<T, D, G, 2>, qblocks, st, nullptr, nullptr, p)
+            : p.kappa <= 4 ? launch(diff_query_kernel<T, D, G, 4>, qblocks, st, nullptr, nullptr, p)
+                           : launch(diff_query_kernel<T, D, G, kMaxKappa>, qblocks, st, nullptr, nullptr, p);
     if (e != hipSuccess) return e;
     if ((e = run_inverse(p, counts, offsets, sums, entries, st, nullptr, nullptr)) != hipSuccess) return e;
     // Key side on the matrix cores for windows 3 x 3 .. 15 x 15, and of one key where bf16 has several maps; the keys that its strips leave, and those of every other call
