@@ -123,7 +123,7 @@ constexpr int diff_tile_waves(int D, int MK) { return D == 128 ? 2 : MK == 4 ? 3
 // not finite (an infinite value of the box reaches every query of its cluster through 0 * inf, a score that is not a number
 // passes its mask), or whose set is empty, is computed over again on a lane group, and so are a wave's queries whose matches
 // lie too far apart to share rows.
-// 4 x 256 x 256, 64 channels, two 5 x 5 windows: 114 us (a lane group per query 175; its bytes 26 us at a copy's rate), the
+// 4 x 256 x 256, 64 channels, two 5 x 5 windows: 114-119 us (a lane group per query 175; its bytes 26 us at a copy's rate), the
 // vector units issuing in 71 % of the cycles and the loads' return path busy in 79 %, at 4 waves per SIMD (3 the same, 5 spill:
 // 284 us).  Weights of three parts were slower and change no bit that the output keeps.
 template <int D, int W, bool CAUSAL, int MK>
