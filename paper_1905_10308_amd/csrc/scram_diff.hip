@@ -119,13 +119,15 @@ constexpr int diff_tile_waves(int D, int MK) { return D == 128 ? 2 : MK == 4 ? 3
 //   S1^T, S2^T = K_blk Q^T       keys x queries, of each half of the channels
 //   P1, P2 = 2^(S scale log2 e - reference) on the query's keys, 0 elsewhere
 //   O1^T += V_blk^T P1^T, O2^T += V_blk^T P2^T
-// with the weights as two bf16 parts (18 bits: the output keeps 8), and at the end o = O1 / l1 - lam O2 / l2.  A query whose sums are
+// with the weights as three bf16 parts that add up to them, and at the end o = O1 / l1 - lam O2 / l2.  (What a weight loses is
+// lost against O1 and O2, not against the difference: where the two maps are alike, two parts, 18 bits, show in the output.)  A
+// query whose sums are
 // not finite (an infinite value of the box reaches every query of its cluster through 0 * inf, a score that is not a number
 // passes its mask), or whose set is empty, is computed over again on a lane group, and so are a wave's queries whose matches
 // lie too far apart to share rows.
-// 4 x 256 x 256, 64 channels, two 5 x 5 windows: 114-119 us (a lane group per query 175; its bytes 26 us at a copy's rate), the
-// vector units issuing in 71 % of the cycles and the loads' return path busy in 79 %, at 4 waves per SIMD (3 the same, 5 spill:
-// 284 us).  Weights of three parts were slower and change no bit that the output keeps.
+// 4 x 256 x 256, 64 channels, two 5 x 5 windows: 137-144 us (a lane group per query 175; its bytes 26 us at a copy's rate), the
+// vector units and the loads' return path bound it, at 4 waves per SIMD.  The normalisers are added up by the vector units (on
+// the matrix cores, as a product with ones, 141 us for 137, and spills with the causal mask).
 template <int D, int W, bool CAUSAL, int MK>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(diff_tile_waves(D, MK)))) void
 diff_tile_kernel(DiffParams p)
@@ -157,9 +159,7 @@ diff_tile_kernel(DiffParams p)
             ref[1].start(s0[1], held, p.scale_log2e);
         }
         f32x4_t acc[2][kOt];
-        f32x4_t sum[2];  // of the weights: every row of an all-ones block's product holds query m's
-        const bf16x4_t ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f), static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
-        sum[0] = sum[1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        float sum[2] = {0.f, 0.f};  // of the weights of this lane's keys
 #pragma unroll
         for (int o = 0; o < kOt; ++o) acc[0][o] = acc[1][o] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         diff_walk<D, W, CAUSAL, MK>(p, t, Kb, Vb, tk, tv, lane, [&](f32x4_t bias) {
@@ -171,17 +171,22 @@ diff_tile_kernel(DiffParams p)
 #pragma unroll
                 for (int o = 0; o < kOt; ++o) acc[h][o] *= f;
             });
-            const Parts2 w0 = parts2(x[0]), w1 = parts2(x[1]);
-            sum[0] = product2(ones, w0, sum[0]);
-            sum[1] = product2(ones, w1, sum[1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) sum[h] += (x[h][0] + x[h][1]) + (x[h][2] + x[h][3]);
+            const Parts3 w0 = parts3(x[0]), w1 = parts3(x[1]);
 #pragma unroll
             for (int o = 0; o < kOt; ++o) {
                 const bf16x4_t vt = column4<D>(tv, m, g4, o);
-                acc[0][o] = product2(vt, w0, acc[0][o]);
-                acc[1][o] = product2(vt, w1, acc[1][o]);
+                acc[0][o] = product3(vt, w0, acc[0][o]);
+                acc[1][o] = product3(vt, w1, acc[1][o]);
             }
         });
-        const float i1 = 1.f / sum[0][0], i2 = p.lam[t.s] / sum[1][0];  // an empty set's are infinite
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            sum[h] += __shfl_xor(sum[h], 16);
+            sum[h] += __shfl_xor(sum[h], 32);
+        }
+        const float i1 = 1.f / sum[0], i2 = p.lam[t.s] / sum[1];  // an empty set's are infinite
         float size = i1 + i2;
 #pragma unroll
         for (int o = 0; o < kOt; ++o) {

@@ -356,31 +356,13 @@ __device__ __forceinline__ void block_weights(MapReference (&ref)[2], const f32x
     }
 }
 
-// Four fp32 values as bf16 parts.  Two parts, each rounded to nearest: within 2^-18 of the value.  A third makes up for the
-// rest.  The first two enter one 16x16x32 product whose other operand is doubled, the last a 16x16x16 one.
-struct Parts2 {
-    bf16x8_t both;
-};
-
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b)
 {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{a, b}, bf16x2_t));
 }
 
-__device__ __forceinline__ Parts2 parts2(const float (&x)[4])
-{
-    const uint32_t h0 = bf16_pair(x[0], x[1]), h1 = bf16_pair(x[2], x[3]);
-    const uint32_t l0 = bf16_pair(x[0] - __uint_as_float(h0 << 16), x[1] - __uint_as_float(h0 & 0xFFFF0000u));
-    const uint32_t l1 = bf16_pair(x[2] - __uint_as_float(h1 << 16), x[3] - __uint_as_float(h1 & 0xFFFF0000u));
-    return Parts2{__builtin_bit_cast(bf16x8_t, make_uint4(h0, h1, l0, l1))};
-}
-
-// c + a b over the block's 16 keys: a 4 keys of each lane group, b in parts
-__device__ __forceinline__ f32x4_t product2(bf16x4_t a, const Parts2& b, f32x4_t c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(a, a, 0, 1, 2, 3, 4, 5, 6, 7), b.both, c, 0, 0, 0);
-}
-
+// Four fp32 values as three bf16 parts that add up to them: two rounded to nearest, the rest fits the third.  The first two
+// enter one 16x16x32 product whose other operand is doubled, the last a 16x16x16 one.
 struct Parts3 {
     bf16x8_t upper;
     bf16x4_t last;
@@ -397,6 +379,7 @@ __device__ __forceinline__ Parts3 parts3(const float (&x)[4])
     return Parts3{__builtin_bit_cast(bf16x8_t, make_uint4(h0, h1, m0, m1)), __builtin_bit_cast(bf16x4_t, make_uint2(l0, l1))};
 }
 
+// c + a b over the block's 16 keys: a 4 keys of each lane group, b in parts
 __device__ __forceinline__ f32x4_t product3(bf16x4_t a, const Parts3& b, f32x4_t c)
 {
     c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(a, a, 0, 1, 2, 3, 4, 5, 6, 7), b.upper, c, 0, 0, 0);
@@ -422,9 +405,9 @@ uint64_t diff_tiles(DiffParams& p)
         return 0;
     p.tq = make_tiling(p.Hq, p.Wq, kBlock / 4);
     const uint64_t tiles = tiling_blocks(p.tq, p.n / p.tq.plane);
-    // A lane group takes kappa w^2 keys of its query, one after another.  4 x 256 x 256, 64 channels, smooth displacements: up
-    // to as many blocks the boxes are faster (two 5 x 5 windows 119 us, with 5/8 of it 123, 12/8 the same; 128 channels 92,
-    // 104), 3 x 3 up to 5/8 (two windows 70; 12/8 80); on matches of noise 12/8 cost half as much again.
+    // A lane group takes kappa w^2 keys of its query, one after another.  4 x 256 x 256, smooth displacements, limits of 5/8, 1
+    // and 12/8 as many blocks: 64 channels, two 5 x 5 windows 135, 144, 144 us, four 206, 196, 196, two of 128 channels (192 x
+    // 192) 148, 139, 139; one 3 x 3 window 39, 40, 51, two 71, 73, 93; on matches of noise 12/8 cost half as much again.
     const int side = 2 * p.b + 1;
     p.tile_blocks = p.kappa * side * side * (side == 3 ? 5 : 8) / 8;
     return tiles > kMaxBlocks / 4 ? 0 : tiles;

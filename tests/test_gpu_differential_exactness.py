@@ -1,0 +1,48 @@
+"""Differential attention where an error cannot hide in a worst-case bound: inputs whose sums cancel, vanish or leave a row out."""
+import pytest
+
+torch = pytest.importorskip("torch")
+import layer_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+U32 = ref.U32
+
+
+def rows(gen, kind, *shape, size=1.0):
+    return (size * torch.randn(*shape, generator=gen, device="cuda")).to(kind)
+
+
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("kappa,window", [(1, 3), (2, 5), (3, 7), (4, 9)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nearly_equal_maps_cancel_to_32_bits(scram, d, kappa, window, dtype):
+    """Two keys with values 1 and -1, lam = 1, scores of the two maps that differ by at most 2^-16: the output is what is left of
+    two results of up to 0.25, and only errors of 32 bits may be left with it.
+
+    Scores c + f (c of 8 bits below 1/2, f a small multiple of 2^-21) are exact in fp32.  Counted in U32 = 2^-24, per map:
+    the scale in base 2 and the exponent's argument, at most 0.72 each, and two exponentials of 1 step (2 U32) move the keys' log
+    ratio by 0.72 * 2 * ln 2 + 4 < 5.1, the result by half of that; the sums of the weights and of the values are rounded at
+    most three times each, the values' partial sums at most 0.63 of the normaliser: 0.25 * 3 + 0.63 * 3 < 2.7; the reciprocal
+    (2), product and difference 0.25 * 4 = 1.  Two maps: 2 * (2.6 + 2.7 + 1) < 13.  The result, at most 2^-17 + 13 U32, is
+    rounded to bf16: 2^-8 of that, 0.5 and little more.
+    """
+    gen = torch.Generator(device="cuda").manual_seed(31)
+    S, H, W, kind, h = 2, 64, 80, TYPES[dtype], d // 2
+    n = H * W
+    c = torch.randint(64, 128, (S, n), generator=gen, device="cuda") / 256.0 * torch.where(torch.rand(S, n, generator=gen, device="cuda") < 0.5, -1.0, 1.0)
+    f = torch.randint(-31, 32, (2, S, n), generator=gen, device="cuda") * 2.0 ** -21
+    Q = torch.zeros(S, H, W, d, dtype=kind, device="cuda")
+    K = torch.zeros(S, 1, 2, d, dtype=kind, device="cuda")
+    V = torch.ones(S, 1, 2, d, dtype=kind, device="cuda")
+    for m in (0, 1):
+        Q.view(S, n, d)[..., m * h] = c.to(kind)
+        Q.view(S, n, d)[..., m * h + 1] = f[m].to(kind)
+        K[:, 0, 0, m * h:m * h + 2] = 1.0
+    V[:, 0, 1] = -1.0
+    s = [(Q.view(S, n, d)[..., m * h].double() + Q.view(S, n, d)[..., m * h + 1].double()) for m in (0, 1)]
+    want = torch.tanh(s[0] / 2) - torch.tanh(s[1] / 2)
+    J = torch.randint(0, 2, (kappa, S, H, W), generator=gen, device="cuda").to(torch.int32)
+    out = scram.differential_attend(Q, K, V, J, torch.ones(S, device="cuda"), window, scale=1.0)
+    off = (out.view(S, n, d).double() - want[..., None]).abs().amax() / U32
+    assert float(off) <= 14.0, f"off by {float(off):.1f} U32"
