@@ -203,10 +203,10 @@ diff_query_tile_kernel(DiffParams p)
         for (int ds = 0; ds < TR::kDs; ++ds)
             go[ds] = TR::frag(static_cast<const unsigned char*>(p.dO) + static_cast<size_t>(t.gq) * (2 * D), ds, g4);
         MapReference ref[2];
+        const bool held = !CAUSAL || t.centre <= t.limit;  // the first match is a key of the query's set
         {
             float s0[2];
             q.own_scores(Kb + t.centre * (2u * D), g4, s0);
-            const bool held = !CAUSAL || t.centre <= t.limit;
             ref[0].start(s0[0], held, p.scale_log2e);
             ref[1].start(s0[1], held, p.scale_log2e);
         }
@@ -260,7 +260,8 @@ diff_query_tile_kernel(DiffParams p)
 #pragma unroll
         for (int o = 0; o < kOt; ++o) {
             const int h = o / (kOt / 2);
-            const uint2 kw = *reinterpret_cast<const uint2*>(krow + 32 * o + 8 * g4);
+            uint2 kw = *reinterpret_cast<const uint2*>(krow + 32 * o + 8 * g4);
+            if (CAUSAL && !held) kw = make_uint2(0u, 0u);  // (whatever that row holds stays out: k_ref is 0)
             const float kref[4] = {__uint_as_float(kw.x << 16), __uint_as_float(kw.x & 0xFFFF0000u), __uint_as_float(kw.y << 16),
                                    __uint_as_float(kw.y & 0xFFFF0000u)};
 #pragma unroll

@@ -46,3 +46,38 @@ def test_nearly_equal_maps_cancel_to_32_bits(scram, d, kappa, window, dtype):
     out = scram.differential_attend(Q, K, V, J, torch.ones(S, device="cuda"), window, scale=1.0)
     off = (out.view(S, n, d).double() - want[..., None]).abs().amax() / U32
     assert float(off) <= 14.0, f"off by {float(off):.1f} U32"
+
+
+@pytest.mark.parametrize("d,window,kappa", [(64, 5, 2), (32, 3, 1), (128, 7, 4), (64, 9, 1), (16, 5, 2)])
+@pytest.mark.parametrize("Hq", [2, 64])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_finite_rows_after_the_query_do_not_reach_it(scram, dtype, Hq, d, window, kappa):
+    """Half of the first matches lie behind the last query, whose key may be any number: not a bit of the output, of dQ or of dlam
+    changes with those rows, and all gradients are the definition's."""
+    gen = torch.Generator(device="cuda").manual_seed(32)
+    S, H, W, kind = 1, Hq + 5, 65, TYPES[dtype]
+    n = Hq * W
+    K, V = rows(gen, kind, S, H, W, d), rows(gen, kind, S, H, W, d)
+    Q, dO = rows(gen, kind, S, Hq, W, d), rows(gen, kind, S, Hq, W, d)
+    lam = torch.rand(S, generator=gen, device="cuda")
+    own = torch.arange(n, device="cuda").reshape(Hq, W)
+    J = ((own + 2 * torch.arange(kappa, device="cuda")[:, None, None, None]) % n).expand(kappa, S, Hq, W).to(torch.int32).contiguous()
+    J[0] = torch.where(torch.rand(J[0].shape, generator=gen, device="cuda") < 0.5, n + J[0] % (5 * W), J[0])
+    mask = ref.key_mask(J, Hq, W, H, W, window, True)
+    behind = [t.view(S, H * W, d)[:, n:] for t in (K, V)]
+    for t in behind:
+        t.zero_()
+    want, tol, wg, tg = ref.differential(Q, K, V, mask, lam, (d // 2) ** -0.5, dO)
+    first = None
+    for size in (0.0, 1.0, 1e3, 1e6, 1e20):
+        for t in behind:
+            t.copy_(rows(gen, kind, *t.shape, size=size))
+        got = (scram.differential_attend(Q, K, V, J, lam, window, causal=True),
+               *scram.differential_attend_backward(Q, K, V, J, lam, dO, window, causal=True))
+        off = (got[0].double().reshape(want.shape) - want).abs()
+        assert (off <= tol + ref.HALF[kind] * (want.abs() + tol)).all(), ("output", size)
+        for name, g, w, t in zip(("dQ", "dK", "dV", "dlam"), got[1:], wg, tg):
+            off = (g.double().reshape(w.shape) - w).abs()
+            assert (off <= t).all(), (name, size, float(off.max()))
+        first = first or got
+        assert all(torch.equal(got[i], first[i]) for i in (0, 1, 4)), size
