@@ -24,7 +24,7 @@ struct DiffParams : BwdParams {
     const int32_t* origin; // [S] raster index of each slice's first query among the keys (null: first)
     int first;
     int tile_blocks;       // most blocks of 16 keys a wave walks on the matrix cores
-    float4* stats;         // [n] log2 normaliser and D of both maps (gradients)
+    float4* stats;         // [n] log2 normaliser and D of both maps (gradients); kOneKey
     double* lam_part;      // [slices, parts] sums over some queries each of D of the second map
     uint32_t slices, parts;
     float* dlam;           // [S]
@@ -38,6 +38,47 @@ __device__ __forceinline__ uint32_t causal_limit(const DiffParams& p, uint32_t s
 {
     const int32_t at = p.origin != nullptr ? clamp_index(p.origin[s], p.nkeys) : p.first;
     return static_cast<uint32_t>(at) + rem;
+}
+
+// Whether query g's set is one key: centre(e, u, v) gives the centre of its window e, `limit` its last key.  With windows of
+// more than one key and a grid of more than one only the causal mask leaves so few.
+template <typename Centre>
+__device__ __forceinline__ bool one_key_set(const DiffParams& p, uint32_t limit, int kappa, Centre&& centre)
+{
+    if (p.b > 0 && !p.causal && p.nkeys > 1) return false;
+    if (!p.causal) limit = p.nkeys - 1;
+    uint32_t only = 0xFFFFFFFFu;
+    for (int e = 0; e < kappa; ++e) {
+        int u, v;
+        centre(e, u, v);
+        // the window's first two keys in raster order
+        const int r0 = max(u - p.b, 0), c0 = max(v - p.b, 0);
+        const uint32_t first = static_cast<uint32_t>(r0) * p.Wk + c0;
+        const uint32_t second = c0 < min(v + p.b, p.Wk - 1) ? first + 1 : r0 < min(u + p.b, p.Hk - 1) ? first + p.Wk : 0xFFFFFFFFu;
+        if (first > limit) continue;
+        if (second <= limit || (only != 0xFFFFFFFFu && only != first)) return false;
+        only = first;
+    }
+    return only != 0xFFFFFFFFu;
+}
+
+// A set of one key: both softmaxes are 1 and the gradients of the scores 0, exactly, in whatever order the key side adds up
+// the score and dP.  Such a query's statistics hold this number (a NaN that no sum gives) in the place of D of the second map.
+constexpr uint32_t kOneKey = 0x7FFFFFFFu;
+
+__device__ __forceinline__ bool is_one_key(const float4& stats) { return __float_as_uint(stats.w) == kOneKey; }
+
+// A query's statistics; one: its set is one key, whose numbers are finite (what is not goes the common way and shows).
+__device__ __forceinline__ float4 query_stats(const float (&lse)[2], const float (&D)[2], bool one)
+{
+    // (a NaN of the input's own is not to be taken for that number)
+    const float last = __float_as_uint(D[1]) == kOneKey ? __uint_as_float(0x7FC00000u) : D[1];
+    return make_float4(lse[0], D[0], lse[1], one ? __uint_as_float(kOneKey) : last);
+}
+
+__device__ __forceinline__ bool finite_stats(const float (&lse)[2], const float (&D)[2])
+{
+    return fabsf(lse[0]) < INFINITY && fabsf(lse[1]) < INFINITY && fabsf(D[0]) < INFINITY && fabsf(D[1]) < INFINITY;
 }
 
 // One half's part of a dot product, over the lane group.

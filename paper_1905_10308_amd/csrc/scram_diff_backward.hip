@@ -139,7 +139,14 @@ __device__ __forceinline__ float diff_query_gradient(const DiffParams& p, uint32
                                (A[h][4 * i + 2] - Dh[h] * B[h][4 * i + 2]) * f, (A[h][4 * i + 3] - Dh[h] * B[h][4 * i + 3]) * f);
     }
     if (lane != 0) return 0.f;
-    p.stats[g] = make_float4(lse[0], Dh[0], lse[1], Dh[1]);
+    bool one = p.b == 0 || p.nkeys == 1;  // one window, no mask
+    if constexpr (MULTI)
+        one = one_key_set(p, ws.local, p.kappa, [&](int e, int& u, int& v) {
+            uint32_t uu, vv;
+            ws.centre(e, uu, vv);
+            u = static_cast<int>(uu), v = static_cast<int>(vv);
+        });
+    p.stats[g] = query_stats(lse, Dh, one && finite_stats(lse, Dh));
     return Dh[1];
 }
 
@@ -255,6 +262,17 @@ diff_query_tile_kernel(DiffParams p)
             size += inv[h] + fabsf(Dh[h]);
             inv[h] *= h == 0 ? p.scale : -p.lam[t.s] * p.scale;
         }
+        bool one = false;
+        if (CAUSAL || p.nkeys == 1) {
+            one = one_key_set(p, t.limit, MK, [&](int e, int& u, int& v) {
+                // (unrolled: indexes known at compile time keep the centres in registers; those past kappa repeat the first)
+                u = t.u[0], v = t.v[0];
+#pragma unroll
+                for (int f = 1; f < MK; ++f)
+                    if (f == e) u = t.u[f], v = t.v[f];
+            }) && finite_stats(lse, Dh);
+            if (one) inv[0] = inv[1] = 0.f;
+        }
         // lane holds channels 16 o + 4 g4 + i of query m
         const unsigned char* const krow = Kb + t.centre * (2u * D);
 #pragma unroll
@@ -274,7 +292,7 @@ diff_query_tile_kernel(DiffParams p)
         todo = static_cast<uint32_t>(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xFFFFu;
         if (t.valid && !((todo >> m) & 1u)) {
             if (g4 == 0) {
-                p.stats[t.g] = make_float4(lse[0], Dh[0], lse[1], Dh[1]);
+                p.stats[t.g] = query_stats(lse, Dh, one);
                 D2 = Dh[1];
             }
 #pragma unroll
@@ -342,9 +360,10 @@ __device__ __forceinline__ void diff_key_batch(const DiffParams& p, const int (&
         }
         if (!ok) continue;
         const float dp = row_score<T, D, G>(gr[t], vj);
+        const bool one = is_one_key(st[t]);
         const float p1 = __builtin_amdgcn_exp2f(half_score<T, G>(qr[t][0], kj[0]) * p.scale_log2e - st[t].x);
         const float p2 = lam * __builtin_amdgcn_exp2f(half_score<T, G>(qr[t][1], kj[1]) * p.scale_log2e - st[t].z);
-        const float ds[2] = {p1 * (dp - st[t].y), -p2 * (dp - st[t].w)};
+        const float ds[2] = {one ? 0.f : p1 * (dp - st[t].y), one ? 0.f : -p2 * (dp - st[t].w)};
         const float w = p1 - p2;
         float qf[2 * H], gf[2 * H];
         unpack_row<T, 2>(qr[t], qf);
@@ -490,7 +509,7 @@ struct DiffStripLds {
     static constexpr int kRowF = D + 4;  // row stride, floats (padded)
     __attribute__((aligned(16))) float q[kStripFE * kRowF], g[kStripFE * kRowF];
     float4 meta[kStripFE];      // lse2 and D of both maps
-    uint32_t in[kStripFE];      // bit k: the entry counts for key k of the strip
+    uint32_t in[kStripFE];      // bit k: the entry counts for key k of the strip, bit 16 + k: also its score's gradients
     int32_t lo[kStripMaxRows], pre[kStripMaxRows + 1];
 };
 
@@ -626,6 +645,8 @@ __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 
                     }
                 }
                 meta = st;
+                // (a set of one key: its weights count, its score's gradients do not)
+                if (MODE == kStripPlain || !is_one_key(st)) in |= in << 16;
             }
             lds.in[m] = in;
             lds.meta[m] = meta;
@@ -654,11 +675,12 @@ __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 
             const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[0][i], p.scale_log2e, -mt.x));
             const float p2 = lam * __builtin_amdgcn_exp2f(fmaf(sc[1][i], p.scale_log2e, -mt.z));
             // (selected by bits: a key that is left out may hold anything)
-            const uint32_t in = static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(lds.in[te]), m, 1));
-            auto kept = [&](float x) { return __uint_as_float(__float_as_uint(x) & in); };
-            w[i] = kept(p1 - p2);
-            ds[0][i] = kept(p1 * (dp[i] - mt.y));
-            ds[1][i] = kept(p2 * (mt.w - dp[i]));
+            const int sets = static_cast<int>(lds.in[te]);
+            auto kept = [](float x, int in) { return __uint_as_float(__float_as_uint(x) & static_cast<uint32_t>(in)); };
+            const int in = __builtin_amdgcn_sbfe(sets, m, 1), in_ds = MODE == kStripPlain ? in : __builtin_amdgcn_sbfe(sets, m + 16, 1);
+            w[i] = kept(p1 - p2, in);
+            ds[0][i] = kept(p1 * (dp[i] - mt.y), in_ds);
+            ds[1][i] = kept(p2 * (mt.w - dp[i]), in_ds);
         }
         // the chunk's sums first, then onto the strip's (sums of sums round less than one long sum)
 #pragma unroll
@@ -805,10 +827,10 @@ hipError_t run_diff_backward(const DiffParams& p0, int32_t* counts, int32_t* off
                            : launch(diff_query_kernel<T, D, G, kMaxKappa>, qblocks, st, nullptr, nullptr, p);
     if (e != hipSuccess) return e;
     if ((e = run_inverse(p, counts, offsets, sums, entries, st, nullptr, nullptr)) != hipSuccess) return e;
-    // Key side on the matrix cores for windows 3 x 3 .. 15 x 15, and of one key where bf16 has several maps; the keys that its strips leave, and those of every other call
-    // with many entries, a wave each.
-    // (Sets of one key: dP - D is exactly 0 on the lane groups.  Windows of one key, several maps: 4 x 256 x 256, 64 channels,
-    // bf16 two maps 81 us, on lane groups 120; fp32 four maps 278, on lane groups 253.)
+    // Key side on the matrix cores for windows 3 x 3 .. 15 x 15, and of one key where bf16 has several maps; the keys that its
+    // strips leave, and those of every other call with many entries, a wave each.
+    // (Windows of one key, several maps: 4 x 256 x 256, 64 channels, bf16 two maps 81 us, on lane groups 120; fp32 four maps 278,
+    // on lane groups 253.)
     const int least = std::is_same<T, uint16_t>::value && p.kappa > 1 ? 0 : 1;
     if (p.b >= least && p.b <= kTileMaxB && p.nkeys > 1) {
         DiffParams pt = p;

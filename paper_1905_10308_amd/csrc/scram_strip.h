@@ -322,6 +322,8 @@ bwd_key_strip_kernel(P p)
                                 in &= ~strip_bits(hu - p.b, hu + p.b, hv - p.b, hv + p.b);
                             }
                         }
+                        // (a set of one key: its weights count, its score's gradients do not)
+                        if (!kQueryIndex || __float_as_uint(second.y) != kOneKey) in |= in << 16;
                         meta.x = static_cast<int>(in);
                     } else if constexpr (MULTI) {
                         // the centres of the query's windows 0 .. e-1 (loaded together), then the strip's
@@ -391,11 +393,11 @@ bwd_key_strip_kernel(P p)
                     const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[et][r], p.scale_log2e, -__int_as_float(mt.z)));
                     const float p2 = lam * __builtin_amdgcn_exp2f(fmaf(sc2[et][r], p.scale_log2e, -st.x));
                     // (selected by bits: a key that is left out may hold anything)
-                    const uint32_t in = static_cast<uint32_t>(__builtin_amdgcn_sbfe(mt.x, m, 1));
-                    auto kept = [&](float x) { return __uint_as_float(__float_as_uint(x) & in); };
-                    wd[4 * et + r] = kept(p1 - p2);
-                    d1[4 * et + r] = kept(p1 * (dp[et][r] - __int_as_float(mt.w)));
-                    d2[4 * et + r] = kept(p2 * (st.y - dp[et][r]));
+                    auto kept = [](float x, int in) { return __uint_as_float(__float_as_uint(x) & static_cast<uint32_t>(in)); };
+                    const int in = __builtin_amdgcn_sbfe(mt.x, m, 1), in_ds = kQueryIndex ? __builtin_amdgcn_sbfe(mt.x, m + 16, 1) : in;
+                    wd[4 * et + r] = kept(p1 - p2, in);
+                    d1[4 * et + r] = kept(p1 * (dp[et][r] - __int_as_float(mt.w)), in_ds);
+                    d2[4 * et + r] = kept(p2 * (st.y - dp[et][r]), in_ds);
                     continue;
                 }
                 bool ok = key_ok && abs(mt.x - kx) <= p.b && abs(mt.y - ky) <= p.b;

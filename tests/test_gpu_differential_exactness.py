@@ -81,3 +81,67 @@ def test_finite_rows_after_the_query_do_not_reach_it(scram, dtype, Hq, d, window
             assert (off <= t).all(), (name, size, float(off.max()))
         first = first or got
         assert all(torch.equal(got[i], first[i]) for i in (0, 1, 4)), size
+
+
+def one_key_maps(kind, gen, kappa, S, H, W, b):
+    """int32 [kappa, S, H, W] under the causal mask or windows of one key: sets of one key, the query's own (two far keys for
+    "spread", one key of all queries for "same")."""
+    at = torch.arange(H * W, device="cuda").reshape(H, W)
+    if kind == "corner":  # the window whose first key is the query: the others lie after it
+        at = (at // W + b).clamp(max=H - 1) * W + (at % W + b).clamp(max=W - 1)
+    elif kind == "spread":
+        at = torch.randint(0, H * W, (S, H, W), generator=gen, device="cuda")
+    elif kind == "same":
+        at = torch.full_like(at, H * W // 3)
+    return at.expand(kappa, S, H, W).to(torch.int32).contiguous()
+
+
+@pytest.mark.parametrize("S", [1, 40])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("kind,window,kappa,causal", [("corner", 3, 1, True), ("corner", 5, 2, True), ("corner", 9, 4, True), ("corner", 7, 8, True),
+                                                      ("spread", 1, 2, False), ("spread", 1, 4, True), ("same", 1, 3, False), ("own", 1, 1, False)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sets_of_one_key_leave_the_scores_alone(scram, dtype, kind, window, kappa, causal, d, S):
+    """Both softmaxes of one key are 1 whatever its score: dQ and dK are exactly 0, dV is (1 - lam) dO summed."""
+    gen = torch.Generator(device="cuda").manual_seed(33)
+    H, W, dt, b = 23, 26, TYPES[dtype], window // 2
+    Q, K, V, dO = (rows(gen, dt, S, H, W, d, size=2.0) for _ in range(4))
+    lam = torch.rand(S, generator=gen, device="cuda")
+    J = one_key_maps(kind, gen, kappa, S, H, W, b)
+    mask = ref.key_mask(J, H, W, H, W, window, causal)
+    one = mask.sum(2) == 1
+    assert one.any() and (one | ~mask.any(2) if kind != "corner" else one.view(S, H, W)[:, :H - b, :W - b]).all()
+    wants = ref.differential(Q, K, V, mask, lam, (d // 2) ** -0.5, dO)[2:]
+    dQ, dK, dV, dlam = scram.differential_attend_backward(Q, K, V, J, lam, dO, window, causal=causal)
+    assert (dQ.view(S, H * W, d)[one] == 0).all()
+    alone = ~(mask & ~one[..., None]).any(1)  # keys that only such queries hold
+    assert (dK.view(S, H * W, d)[alone] == 0).all()
+    for name, g, w, t in zip(("dQ", "dK", "dV", "dlam"), (dQ, dK, dV, dlam), *wants):
+        off = (g.double().reshape(w.shape) - w).abs()
+        assert (off <= t).all(), (name, float(off.max()))
+
+
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_what_is_not_finite_passes_sets_of_one_key(scram, dtype, d):
+    """An infinite dO, a NaN query and an infinite key's score in sets of one key: their rows are not finite, all others right."""
+    gen = torch.Generator(device="cuda").manual_seed(34)
+    S, H, W, dt = 3, 23, 26, TYPES[dtype]
+    Q, K, V, dO = (rows(gen, dt, S, H, W, d) for _ in range(4))
+    lam = torch.tensor([0.4, 0.7, 0.9], device="cuda")
+    J = one_key_maps("corner", gen, 2, S, H, W, 2)
+    mask = ref.key_mask(J, H, W, H, W, 5, True)
+    _, _, want, tol = ref.differential(Q, K, V, mask, lam, (d // 2) ** -0.5, dO)
+    bad = [60, 190]
+    dO[0].view(-1, d)[bad[0], 5] = float("inf")
+    Q[1].view(-1, d)[bad[1], d - 1] = float("nan")
+    dQ, dK, dV, dlam = scram.differential_attend_backward(Q, K, V, J, lam, dO, 5, causal=True)
+    assert mask[:, bad].sum() == 2 * S
+    for s, i in ((0, bad[0]), (1, bad[1])):
+        assert not dQ[s].view(-1, d)[i].isfinite().all() and not dV[s].view(-1, d)[i].isfinite().all() and not dlam[s].isfinite()
+    hit = torch.zeros(S, H * W, dtype=torch.bool, device="cuda")
+    hit[0, bad[0]] = hit[1, bad[1]] = True
+    for name, g, w, t in zip(("dQ", "dK", "dV"), (dQ, dK, dV), want, tol):
+        off = (g.view(S, H * W, d).double() - w).abs()
+        assert (off[~hit] <= t[~hit]).all(), name
+    assert abs(float(dlam[2] - want[3][2])) <= float(tol[3][2])
