@@ -13,12 +13,6 @@
 //   scram_backward.hip -- gradients of the attend step (maps held fixed)
 //   scram_snis.hip     -- self-normalised importance sampling around the
 //                         matches (Section 4.2, Equations 11-17)
-//   scram_diff.hip, scram_diff_backward.hip
-//                      -- the difference of two softmax maps over the windows,
-//                         and its gradients
-//   scram_rotary.hip, scram_norm.hip
-//                      -- what a layer does to the rows before and after:
-//                         rotary grid positions, layer norm
 //
 // Everything here lives in an unnamed namespace: each kernel file gets its
 // own copy.
@@ -524,19 +518,6 @@ hipError_t launch(void (*kernel)(A...), uint64_t blocks, hipStream_t st, hipEven
         hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), 0, st, start, stop, 0, args...);
     else
         hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), 0, st, args...);
-    return hipGetLastError();
-}
-
-// launch() for kernels of another block size: one wave, by default
-template <uint32_t kThreads = 64, typename P>
-hipError_t launch_wave(void (*kernel)(P), uint64_t blocks, hipStream_t st, hipEvent_t start, hipEvent_t stop,
-                       const P& p)
-{
-    if (blocks == 0 || blocks > 0xFFFFFFFFull / kThreads) return hipErrorInvalidConfiguration;
-    if (start || stop)
-        hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, st, start, stop, 0, p);
-    else
-        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, st, p);
     return hipGetLastError();
 }
 

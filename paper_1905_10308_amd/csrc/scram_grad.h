@@ -5,7 +5,7 @@
 
 #pragma once
 
-#include "scram_device.h"
+#include "scram_wave.h"
 
 namespace scram {
 namespace {
