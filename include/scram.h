@@ -445,9 +445,10 @@ enum { SCRAM_ROTARY_MAX_PAIRS = 128 };
  *   (a cos t - b sin t, a sin t + b cos t),  t = x * freqs[k].
  * Pair k is channels (k, k + P) of the group, P = sum of the sections, or with
  * SCRAM_ROTARY_INTERLEAVED (2k, 2k + 1).  SCRAM_ROTARY_INVERSE turns by -t:
- * the gradient.  The angle is reduced by whole turns in 64-bit fixed point
- * (frequencies rounded to 2^-53 of their value), so positions over the whole
- * int32 range keep their accuracy; sums are fp32, rounded once.
+ * the gradient.  The angle is reduced by whole turns in 64-bit fixed point:
+ * a frequency is off by up to 2^-52 of its value and 2^-65 of a turn, so
+ * positions over the whole int32 range keep their accuracy; sums are fp32,
+ * rounded once.
  *
  * Arguments:
  *   src, dst  tensors, aligned to their elements (dst[i] == src[i]: in place)

@@ -187,11 +187,11 @@ hipError_t launch_rotary(int dtype, const RotaryCall& c, hipStream_t stream)
     p.per_slice = c.origin_rows > 1 ? 1 : 0;
     for (int a = 0; a < 3; ++a) p.first[a] = c.first[a];
     for (int k = 0; k < p.pairs; ++k) {
-        // whole turns do not count: the fraction, rounded to 2^-64 turns
-        const double turns = c.freq[k] / 6.283185307179586476925;
-        const double part = turns - floor(turns);
-        const uint64_t f = part >= 1.0 ? 0u : static_cast<uint64_t>(ldexp(part, 64));
-        p.turn[k] = c.inverse ? 0u - f : f;
+        // whole turns do not count: the fraction, rounded to 2^-64 turns (of the value without its sign: a small negative one
+        // would lose its low bits in 1 - x)
+        const double turns = fabs(c.freq[k]) / 6.283185307179586476925;
+        const uint64_t f = static_cast<uint64_t>(rint(ldexp(turns - floor(turns), 64)));  // (less than 1 by 2^-53 at least)
+        p.turn[k] = c.inverse != (c.freq[k] < 0.0) ? 0u - f : f;
     }
     dim3 threads(kBlock, 1);
     while (threads.x / 2 >= p.total) threads.x /= 2, threads.y *= 2;
