@@ -246,10 +246,13 @@ __global__ __launch_bounds__(norm_threads(LAYOUT)) void norm_backward_kernel(Nor
             sum[2 * k] = sum[2 * k + 1] = 0.f;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
+                // past the end of the row dY is 0, but (0 - mean) rstd may be infinite: xh is 0 there
+                const int left = p.C - (lane + c * p.lanes) * V;
+                const float r = left > 0 ? rstd[k] : 0.f;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    // (past the end of the row, or of the rows, dY is 0 and xh finite: nothing is added)
-                    const float dy = to_float(static_cast<TG>(d[k][c][j])), xh = xhat(k, c, j);
+                    const float dy = to_float(static_cast<TG>(d[k][c][j]));
+                    const float xh = TAIL && j >= left ? 0.f : (to_float(static_cast<T>(a[k][c][j])) - mean[k]) * r;
                     dw[c][j] = fmaf(dy, xh, dw[c][j]);
                     db[c][j] += dy;
                     const float g = dy * w[c][j];
