@@ -94,9 +94,11 @@ __device__ __forceinline__ void diff_query(const DiffParams& p, uint32_t g, int 
     store_row<T, D, G>(p.out, g, lane, o, 1.f);
 }
 
-// A lane group per query (WAVE: a wave per query, for calls of up to 4096 queries, which lane groups would leave most of the
-// machine without; 32 single pixels take 11 us, most of it the launch).  fp32 8 x 128 x 128 -> 192 x 192, 32 channels, causal
-// or two windows: 37-45 us, its bytes 21 us at a copy's rate.  kNb keys at a time: three, or five for one
+// A lane group per query, or WAVE: a wave per query, for calls of up to 4096 queries, of which lane groups or tiles would leave
+// most of the machine without work.  (Kernel alone, lane groups or tiles and WAVE, bf16, 64 channels, two 5 x 5 windows: 512
+// queries 15 and 7 us, 4096 18 and 14, 8192 23 and 23; two 7 x 7 20 and 15 at 4096, 28 and 25 at 8192; fp32, 64 channels, one
+// 5 x 5 7 and 7 at 4096, two 7 x 7 30 and 14.  One 3 x 3 window is even at 1024 and loses at 4096, 7 and 11.)
+// fp32 8 x 128 x 128 -> 192 x 192, 32 channels, two 3 x 3 windows: 36-37 us, its bytes 21 us at a copy's rate.  kNb keys at a time: three, or five for one
 // 5 x 5 window, which is then five whole batches (8 x 128 x 128, 32 channels, fp32: two 3 x 3 windows with four 44 us, three
 // 38, five 40; one 5 x 5 window 38, 40, 32).
 template <typename T, int D, int G, int MK, int kNb, bool WAVE>

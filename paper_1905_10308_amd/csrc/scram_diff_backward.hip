@@ -179,7 +179,10 @@ constexpr int diff_grad_waves(int D) { return D == 128 ? 1 : D == 64 ? 2 : 3; }
 //   B^T += K_blk^T P^T,  A^T += K_blk^T PD^T           channels x queries: the first half's with P1, the last with P2
 //   l += 1^T P^T,  dn += 1^T PD^T                      all-ones blocks, of each map
 // with the weights as three bf16 parts that add up to them (the gradients are fp32).  With D = dn / l and k_ref the key at the
-// first match, dQ = scale ((A - dn k_ref) - D (B - l k_ref)) / l: the lane group's sums, whose subtraction cancels no more.
+// first match (0 where the causal mask takes it away), dQ = scale ((A - dn k_ref) - D (B - l k_ref)) / l.  In exact arithmetic
+// those are the lane group's sums; here whole keys are added up and k_ref comes off at the end, so a common offset of the keys
+// is rounded with them: keys 8 (64) times their spread away from 0 cost 1.3e-6 (9e-6) of dQ, a plain 32-bit computation 1e-6
+// (8e-6), a lane group 2.8e-7 whatever the offset.
 // A query whose sums are not finite, or whose set is empty, is computed over again on a lane group, and so are a wave's
 // queries whose matches lie too far apart to share rows.
 // 16 x 128 x 128, 64 channels, two 5 x 5 windows: 190 us, at 2 waves per SIMD the vector units (splitting the weights) issuing

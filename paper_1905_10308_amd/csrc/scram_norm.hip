@@ -341,7 +341,9 @@ NormPlan norm_plan(const NormCall& c)
 int block_threads(const NormPlan& plan) { return plan.layout == kHuge ? plan.lanes : kBlock; }
 
 // Blocks of the backward pass, each of which writes a row of parts: two per CU, or one where a row takes more than 256
-// threads.  (8192 x 4096: 512 blocks 50 us, 256 64, 768 64; 2048 x 16384: 256 blocks 70, 512 94.)
+// threads.  (8192 x 4096: 512 blocks 50 us, 256 64, 768 64; 2048 x 16384: 256 blocks 70, 512 94.)  Fewer rows than that leave
+// blocks without one, whose parts are zeros (a call's kernels, with as many blocks as the rows fill beside it, bf16: 512 x 64
+// 12 and 11 us, 2048 x 1024 16 and 14, 512 x 4096 22 and 16; 4096 rows and more the same).
 int64_t norm_backward_blocks(int64_t rows, int channels)
 {
     const int64_t most = channels > kPerThread * kBlock ? 256 : 512;

@@ -140,8 +140,9 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(RotaryParams p)
 }
 
 // Channels per vector: the most, up to 16 bytes, that divide the turned pairs and the group.  (Whole vectors of 16 bytes with a
-// last one in pieces were slower: 46 pairs of 100 fp32 channels, vectors of 8 bytes 56 us, 16 with a rest 65; 23 pairs of
-// bf16, single channels 32 us, 16 bytes with a rest 44.)
+// last one in pieces were slower: 6 x 16 x 45 x 80, 46 pairs of 100 fp32 channels, vectors of 8 bytes 56 us, 16 with a rest 65.
+// An odd number of pairs goes a channel at a time: two tensors of 4 x 256 x 256, bf16, 23 pairs of 46 channels 27 us, 18.7 at a
+// copy's rate; 24 of 48, in vectors of 16 bytes, 21 and 19.5.)
 int rotary_vector(int elem, const RotaryCall& c)
 {
     const int group = c.d / c.groups, pairs = c.pairs[0] + c.pairs[1] + c.pairs[2];
