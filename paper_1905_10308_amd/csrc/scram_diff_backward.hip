@@ -185,8 +185,8 @@ constexpr int diff_grad_waves(int D) { return D == 128 ? 1 : D == 64 ? 2 : 3; }
 // (8e-6), a lane group 2.8e-7 whatever the offset.
 // A query whose sums are not finite, or whose set is empty, is computed over again on a lane group, and so are a wave's
 // queries whose matches lie too far apart to share rows.
-// 16 x 128 x 128, 64 channels, two 5 x 5 windows: 190 us, at 2 waves per SIMD the vector units (splitting the weights) issuing
-// in 68 % of the cycles, the loads' return path busy in 73 %, the matrix cores in 32 %.
+// 16 x 128 x 128, 64 channels, two 5 x 5 windows: 190-203 us, at 2 waves per SIMD the vector units (splitting the weights) issuing
+// in 67 % of the cycles, the loads' return path busy in 73 %, the matrix cores in 31 %.
 template <int D, int W, bool CAUSAL, int MK>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(diff_grad_waves(D)))) void
 diff_query_tile_kernel(DiffParams p)
