@@ -379,15 +379,34 @@ __device__ __forceinline__ void diff_key_batch(const DiffParams& p, const int (&
     }
 }
 
-// The entries of key k's neighbourhood taken by member `member` of a team of
-// `team` lane groups.
-template <typename T, int D, int G, bool MULTI>
-__device__ __forceinline__ void diff_key_sums(const DiffParams& p, const KeyPos& k, int member, int team, int lane,
+// The entries of key k's neighbourhood (`total` of them) taken by member `member` of a team of
+// `team` lane groups.  RUNS: added up in runs of the square root of their
+// number, and the runs then onto the sums: entries whose terms are alike round
+// the same way, and one after another onto a sum of thousands lost 2e-5 of it
+// (65536 queries of one key; 5e-4 at 2^20).
+template <typename T, int D, int G, bool MULTI, bool RUNS>
+__device__ __forceinline__ void diff_key_sums(const DiffParams& p, const KeyPos& k, int total, int member, int team, int lane,
                                               const uint4 (&kj)[2], const uint4 (&vj)[2], float* dk, float* dv)
 {
-    constexpr int kNb = 2;
+    constexpr int kNb = 2, N = 2 * Row<T, D, G>::kEpc;
     const int32_t* off = p.offsets + static_cast<size_t>(k.s) * p.nkeys;
     const float lam = p.lam[k.s];
+    float rk[RUNS ? N : 1], rv[RUNS ? N : 1];
+    const int run = RUNS ? max(16, static_cast<int>(sqrtf(static_cast<float>(total / (kNb * team))))) : 0;
+    int left = run;
+    auto flush = [&](bool first) {
+#pragma unroll
+        for (int i = 0; i < (RUNS ? N : 0); ++i) {
+            if (!first) dk[i] += rk[i], dv[i] += rv[i];
+            rk[i] = rv[i] = 0.f;
+        }
+        left = run;
+    };
+    auto batch = [&](const int (&x)[kNb], const bool (&valid)[kNb]) {
+        diff_key_batch<T, D, G, MULTI, kNb>(p, x, valid, lam, k, lane, kj, vj, RUNS ? rk : dk, RUNS ? rv : dv);
+        if (RUNS && --left == 0) flush(false);
+    };
+    flush(true);
     if (k.r1 - k.r0 + 1 <= kMaxRows) {
         const Neighbourhood nb = load_neighbourhood(off, p.Wk, k.r0, k.r1, k.c0, k.c1);
         for (int v0 = member; v0 < nb.total; v0 += kNb * team) {
@@ -398,7 +417,7 @@ __device__ __forceinline__ void diff_key_sums(const DiffParams& p, const KeyPos&
                 valid[t] = v0 + t * team < nb.total;
                 x[t] = flat_slot(nb, min(v0 + t * team, nb.total - 1));
             }
-            diff_key_batch<T, D, G, MULTI, kNb>(p, x, valid, lam, k, lane, kj, vj, dk, dv);
+            batch(x, valid);
         }
     } else {
         for (int r = k.r0; r <= k.r1; ++r) {
@@ -411,10 +430,20 @@ __device__ __forceinline__ void diff_key_sums(const DiffParams& p, const KeyPos&
                     valid[t] = x0 + t * team < hi;
                     x[t] = min(x0 + t * team, hi - 1);
                 }
-                diff_key_batch<T, D, G, MULTI, kNb>(p, x, valid, lam, k, lane, kj, vj, dk, dv);
+                batch(x, valid);
             }
         }
     }
+    if constexpr (RUNS) flush(false);
+}
+
+// Entries of key k's neighbourhood.
+__device__ __forceinline__ int key_entries(const DiffParams& p, const KeyPos& k)
+{
+    const int32_t* off = p.offsets + static_cast<size_t>(k.s) * p.nkeys;
+    int total = 0;
+    for (int r = k.r0; r <= k.r1; ++r) total += off[r * p.Wk + k.c1 + 1] - off[r * p.Wk + k.c0];
+    return total;
 }
 
 // dK_j (times scale) and dV_j from the lane's channels.
@@ -447,9 +476,7 @@ __global__ __launch_bounds__(kBlock) void diff_key_kernel(DiffParams p)
     uint32_t kg;
     if (!tile_item<RW::kQpb>(p.tk, xcd_remap(blockIdx.x, gridDim.x), threadIdx.x / G, kg)) return;
     const KeyPos k = key_pos(p, kg);
-    const int32_t* off = p.offsets + static_cast<size_t>(k.s) * p.nkeys;
-    int total = 0;
-    for (int r = k.r0; r <= k.r1; ++r) total += off[r * p.Wk + k.c1 + 1] - off[r * p.Wk + k.c0];
+    const int total = key_entries(p, k);
     if (total > kDiffHeavy) {
         if (lane == 0) p.heavy[atomicAdd(p.n_heavy, 1)] = static_cast<int32_t>(kg);
         return;
@@ -460,7 +487,7 @@ __global__ __launch_bounds__(kBlock) void diff_key_kernel(DiffParams p)
     float dk[2 * RW::kEpc], dv[2 * RW::kEpc];
 #pragma unroll
     for (int i = 0; i < 2 * RW::kEpc; ++i) dk[i] = dv[i] = 0.f;
-    diff_key_sums<T, D, G, MULTI>(p, k, 0, 1, lane, kj, vj, dk, dv);
+    diff_key_sums<T, D, G, MULTI, false>(p, k, total, 0, 1, lane, kj, vj, dk, dv);
     diff_store_key<T, D, G>(p, kg, lane, dk, dv);
 }
 
@@ -482,7 +509,7 @@ __global__ __launch_bounds__(kBlock) void diff_heavy_kernel(DiffParams p)
         float dk[N], dv[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) dk[i] = dv[i] = 0.f;
-        diff_key_sums<T, D, G, MULTI>(p, k, member, 64 / G, lane, kj, vj, dk, dv);
+        diff_key_sums<T, D, G, MULTI, true>(p, k, key_entries(p, k), member, 64 / G, lane, kj, vj, dk, dv);
 #pragma unroll
         for (int mask = G; mask < 64; mask <<= 1)
 #pragma unroll

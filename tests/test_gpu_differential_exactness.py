@@ -145,3 +145,30 @@ def test_what_is_not_finite_passes_sets_of_one_key(scram, dtype, d):
         off = (g.view(S, H * W, d).double() - w).abs()
         assert (off[~hit] <= t[~hit]).all(), name
     assert abs(float(dlam[2] - want[3][2])) <= float(tol[3][2])
+
+
+@pytest.mark.parametrize("H,W,window,kappa", [(256, 256, 5, 1), (1024, 1024, 3, 1), (512, 512, 5, 2), (256, 256, 17, 1), (256, 256, 1, 2)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 16), ("f32", 64), ("f32", 128)])
+def test_a_key_of_all_queries_sums_to_32_bits(scram, dtype, d, H, W, window, kappa):
+    """All matches on one key, scores of 0, dO of ones: every key of the window gets n (1 - lam) / w^2, n terms that are alike.
+
+    In U32: a weight, 2^-log2(w^2), carries the logarithm's rounding and last place (3 * 8 / 2 at most, times ln 2) and the
+    exponential's 2, that of the second map 1 more, and their difference is half of the first: 2 * (11 + 12 + 1) < 50.  The sums
+    may be rounded by 3 sqrt(n / (2 teams)) (runs of the square root of a lane group's steps, two terms a step, then as many
+    runs; at least 2 lane groups to a key), and 8 more.
+    """
+    n = H * W
+    kind = TYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(35)
+    Q = torch.zeros(1, H, W, d, dtype=kind, device="cuda")
+    K, V = rows(gen, kind, 1, H, W, d), rows(gen, kind, 1, H, W, d)
+    J = torch.full((kappa, 1, H, W), (H // 2) * W + W // 2, dtype=torch.int32, device="cuda")
+    dV = scram.differential_attend_backward(Q, K, V, J, torch.full((1,), 0.5, device="cuda"), torch.ones_like(Q), window)[2][0]
+    b = window // 2
+    got = dV[H // 2 - b:H // 2 + b + 1, W // 2 - b:W // 2 + b + 1].double()
+    want = n * 0.5 / window ** 2
+    off = float((got / want - 1).abs().max()) / U32
+    lanes = d * (2 if dtype == "bf16" else 4) // 32  # of a lane group; a wave takes a key
+    bound = 58 + 3 * (n / (2 * (64 / lanes))) ** 0.5
+    assert off <= bound, f"off by {off:.0f} U32, may be {bound:.0f}"
+    assert (dV.abs().sum(2) > 0).sum() == window ** 2
