@@ -266,7 +266,7 @@ diff_query_tile_kernel(DiffParams p)
             inv[h] *= h == 0 ? p.scale : -p.lam[t.s] * p.scale;
         }
         bool one = false;
-        if (CAUSAL || p.nkeys == 1) {
+        if constexpr (CAUSAL) {
             one = one_key_set(p, t.limit, MK, [&](int e, int& u, int& v) {
                 // (unrolled: indexes known at compile time keep the centres in registers; those past kappa repeat the first)
                 u = t.u[0], v = t.v[0];
@@ -821,7 +821,8 @@ bool run_diff_query_tiles(const DiffParams& p0, hipStream_t st, hipError_t& err)
     if constexpr (std::is_same<T, uint16_t>::value && D >= 32) {
         DiffParams p = p0;
         const uint64_t tiles = diff_tiles<D>(p);
-        if (tiles == 0) return false;
+        // (a grid of one key: every set is one key, which the tiles expect of the causal mask alone)
+        if (tiles == 0 || p.nkeys == 1) return false;
         err = p.b == 1   ? run_diff_query_tile<D, 3>(p, 4 * tiles, st)
               : p.b == 2 ? run_diff_query_tile<D, 5>(p, 4 * tiles, st)
               : p.b == 3 ? run_diff_query_tile<D, 7>(p, 4 * tiles, st)

@@ -172,3 +172,21 @@ def test_a_key_of_all_queries_sums_to_32_bits(scram, dtype, d, H, W, window, kap
     bound = 58 + 3 * (n / (2 * (64 / lanes))) ** 0.5
     assert off <= bound, f"off by {off:.0f} U32, may be {bound:.0f}"
     assert (dV.abs().sum(2) > 0).sum() == window ** 2
+
+
+@pytest.mark.parametrize("window,kappa", [(3, 1), (5, 2), (9, 4), (1, 1)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_grid_of_one_key(scram, dtype, window, kappa):
+    """Every set is the one key: the output is (1 - lam) v, dV the sum of (1 - lam) dO, dQ and dK are 0."""
+    gen = torch.Generator(device="cuda").manual_seed(36)
+    S, H, W, d, kind = 3, 41, 37, 64, TYPES[dtype]
+    Q, dO, K, V = rows(gen, kind, S, H, W, d), rows(gen, kind, S, H, W, d), rows(gen, kind, S, 1, 1, d), rows(gen, kind, S, 1, 1, d)
+    lam = torch.rand(S, generator=gen, device="cuda")
+    J = torch.zeros(kappa, S, H, W, dtype=torch.int32, device="cuda")
+    want, tol, wg, tg = ref.differential(Q, K, V, torch.ones(S, H * W, 1, dtype=torch.bool, device="cuda"), lam, 32 ** -0.5, dO)
+    out = scram.differential_attend(Q, K, V, J, lam, window)
+    assert ((out.double().reshape(want.shape) - want).abs() <= tol + ref.HALF[kind] * (want.abs() + tol)).all()
+    dQ, dK, dV, dlam = scram.differential_attend_backward(Q, K, V, J, lam, dO, window)
+    assert (dQ == 0).all() and (dK == 0).all()
+    for g, w, t in ((dV, wg[2], tg[2]), (dlam, wg[3], tg[3])):
+        assert ((g.double().reshape(w.shape) - w).abs() <= t).all()
