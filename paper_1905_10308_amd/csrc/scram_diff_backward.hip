@@ -786,7 +786,7 @@ __global__ __launch_bounds__(64 * TEAM) __attribute__((amdgpu_waves_per_eu(D >= 
 }
 
 // Up to as many strips a team of four waves takes each, up to four times as many a team of two: a wave per strip would not
-// fill the machine, and the strips of many entries would run on alone.  (fp32, 64 channels, 3072 strips: 3 x 3 117 us a call
+// fill the machine, and the strips of many entries would run on alone.  (fp32, 64 channels, some 3,000 strips: 3 x 3 117 us a call
 // with one wave, 107 with two, 115 with four, 5 x 5 177, 161, 166; bf16, 288 strips: 68, 59, 56; 8192 strips: 252, 268 with four.)
 constexpr uint64_t kTeamStrips = 1024;
 
