@@ -28,8 +28,14 @@
  * Q, K and V with the maps held fixed.  scram_differential_attend takes the
  * difference of two softmax maps over the same keys instead.
  *
+ * scram_dense_attend attends to every key, without maps (Equations 1-3): for
+ * grids small enough for it, and as the result that the windows approximate.
+ * It takes a learned bias by relative position, which scram_relative_bias
+ * makes of a table by buckets of distance.
+ *
  * Around them, for the layer that uses them: scram_layer_norm (the rows of Q
- * and K, or of the output) and scram_rotary (positions on the grid).
+ * and K, or of the output), scram_group_norm (images, with an activation) and
+ * scram_rotary (positions on the grid).
  *
  * scram_snis_attend replaces the window of step 2 by the self-normalised
  * importance-sampling estimator of Section 4.2 (Monte Carlo estimators,
@@ -497,6 +503,156 @@ int scram_layer_norm_backward(const void* dY, int grad_dtype, const void* X, int
                               const float* rstd, const void* weight, int weight_dtype, int64_t rows, int channels,
                               void* dX, float* dweight, float* dbias, void* workspace, size_t workspace_bytes,
                               hipStream_t stream);
+
+/*
+ * Attention over every key (Equations 1-3), with a learned bias by relative
+ * position.  For query i of slice s, which reads slice s / (S / key_slices) of
+ * K and V,
+ *   out_i = sum_j softmax_j(scale * q_i . k_j + B[s % bias_rows][offset of j from i]) v_j
+ * over the keys j < lengths[its slice of keys], and with SCRAM_CAUSAL at or
+ * before the query's place.  A query without a key, or with scores of minus
+ * infinity alone, gets a zero row.  The softmax is fp32 and online; in bf16 its
+ * weights are rounded to bf16 (half a step each, 2^-8) for their product with
+ * the values, which adds up in fp32 and is rounded once.
+ *
+ * Arguments:
+ *   Q, K, V     [S, Hq, Wq, d], [key_slices, Hk, Wk, d], [key_slices, Hk, Wk, dv]
+ *               in `dtype`, dv == d; finite in the rows of keys that some
+ *               query of the slice sees (the others are not read, or have no
+ *               effect when finite)
+ *   bias        nullable [bias_rows, 2 Hk - 1, 2 Wk - 1] in `dtype`, aligned to
+ *               its elements: a key dy rows below and dx columns right of its
+ *               query meets B[dy + Hk - 1][dx + Wk - 1].  Minus infinity hides a
+ *               key; the type's lowest value hides it behind any other.
+ *               bias_rows >= 1 divides S (slice = image * heads + head: the
+ *               images share the heads' tables).  Not for Hk > 1 with Wk above
+ *               6000 or so (SCRAM_ERR_SHAPE), nor 2^31 offsets
+ *   lengths     nullable int32 [key_slices] on the device: the keys of a slice
+ *               that count, in raster order; clamped into [0, Hk*Wk].  Those
+ *               behind are not read
+ *   key_slices  divides S
+ *   scale       softmax temperature, 1/sqrt(d) for Equation 1; finite
+ *   flags       0 or SCRAM_CAUSAL
+ *   first, origin
+ *               with SCRAM_CAUSAL or a bias the queries of a slice stand at
+ *               the run r, r + 1, ... of the keys' raster, as in
+ *               scram_differential_attend; otherwise 0 and NULL
+ *   out         [S, Hq, Wq, dv] in `dtype` (written)
+ *   workspace   scram_dense_attend_workspace_bytes(...) bytes, 256-byte
+ *               aligned; may be NULL where that is 0
+ *   events      NULL or 2 events stamped with the start and the end
+ * Outputs and the workspace overlap nothing else.  Returns a status code.
+ */
+size_t scram_dense_attend_workspace_bytes(int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dtype,
+                                          int biased);
+
+int scram_dense_attend(const void* Q, const void* K, const void* V, int dtype, const void* bias, int bias_rows,
+                       const int32_t* lengths, int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dv,
+                       float scale, uint32_t flags, int first, const int32_t* origin, void* out, void* workspace,
+                       size_t workspace_bytes, hipEvent_t* events, hipStream_t stream);
+
+/*
+ * Gradients of scram_dense_attend.  With p_ij its weights, dp_ij = dO_i . v_j,
+ * D_i = sum_j p_ij dp_ij and ds_ij = p_ij (dp_ij - D_i):
+ *   dQ_i = scale sum_j ds_ij k_j,  dK_j = scale sum_i ds_ij q_i,  dV_j = sum_i p_ij dO_i,
+ *   dB[r][o] = sum over the slices s with s % bias_rows == r and their pairs at offset o of ds_ij
+ * (dK_j, dV_j over the queries of all slices that read the key's).  The
+ * weights are recomputed; D is formed of fp32 weights and not of the rounded
+ * output, so that what a nearly certain weight leaves is not lost.  fp32
+ * throughout, but that in bf16 p and ds are rounded to bf16 (half a step each,
+ * 2^-8) for the products that give dQ, dK and dV; every result is rounded once
+ * to `dtype`.  Each has one writer and a fixed order of its sums: equal calls
+ * give equal bits.  Keys behind `lengths`, and offsets that no pair has, get
+ * zeros.
+ *
+ * Arguments: as scram_dense_attend, plus
+ *   dO          [S, Hq, Wq, dv] in `dtype`, finite
+ *   dQ, dK, dV  [S, Hq, Wq, d], [key_slices, Hk, Wk, d], [key_slices, Hk, Wk, dv]
+ *               in `dtype` (written), 16-byte aligned
+ *   dbias       nullable [bias_rows, 2 Hk - 1, 2 Wk - 1] in `dtype` (written),
+ *               NULL without a bias
+ *   workspace   scram_dense_attend_backward_workspace_bytes(...) bytes
+ */
+size_t scram_dense_attend_backward_workspace_bytes(int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dtype,
+                                                   int bias_rows);
+
+int scram_dense_attend_backward(const void* Q, const void* K, const void* V, int dtype, const void* bias, int bias_rows,
+                                const int32_t* lengths, int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d,
+                                int dv, float scale, uint32_t flags, int first, const int32_t* origin, const void* dO,
+                                void* dQ, void* dK, void* dV, void* dbias, void* workspace, size_t workspace_bytes,
+                                hipEvent_t* events, hipStream_t stream);
+
+/* most distances at which the buckets of one side of an axis begin */
+enum { SCRAM_BIAS_MAX_EDGES = 64 };
+
+/*
+ * The bias of every offset on an H x W grid from a learned table by buckets of
+ * distance.  An axis with the edges 0 < e_1 < e_2 < ... < e_m has 2 m + 1
+ * buckets: offset t falls into bucket m + sign(t) * #{k : e_k <= |t|} (the
+ * middle one holds the offsets nearer than e_1 on either side).
+ *   bias[h][dy + H - 1][dx + W - 1] = table[h][bucket of dy][bucket of dx]
+ *
+ * Arguments:
+ *   table     [heads, 2 my + 1, 2 mx + 1] in `dtype`, aligned to its elements
+ *   edges_y, my, edges_x, mx  host arrays of the axes' edges, 0 .. SCRAM_BIAS_MAX_EDGES each
+ *   bias      [heads, 2 H - 1, 2 W - 1] in `dtype` (written)
+ * heads * (2 H - 1) * (2 W - 1) < 2^40, one head's < 2^31.  Returns a status code.
+ */
+int scram_relative_bias(const void* table, int dtype, int heads, int H, int W, const int* edges_y, int my,
+                        const int* edges_x, int mx, void* bias, hipStream_t stream);
+
+/*
+ * Its gradient: dtable[h][a][b] = the sum of dbias over the offsets in that
+ * bucket, fp32 in a fixed order, rounded once to `dtype`; zeros where no offset
+ * of the grid falls.  workspace:
+ * scram_relative_bias_backward_workspace_bytes(...) bytes, 256-byte aligned.
+ */
+size_t scram_relative_bias_backward_workspace_bytes(int heads, int H, int W, int mx);
+
+int scram_relative_bias_backward(const void* dbias, int dtype, int heads, int H, int W, const int* edges_y, int my,
+                                 const int* edges_x, int mx, void* dtable, void* workspace, size_t workspace_bytes,
+                                 hipStream_t stream);
+
+/* activations of scram_group_norm */
+enum { SCRAM_ACT_NONE = 0, SCRAM_ACT_SILU = 1 };
+
+/*
+ * Group norm of `images` images of `pixels` pixels of `channels` (1 .. 16384)
+ * channels, channels last, in `groups` groups of neighbouring channels, and an
+ * activation.  Over an image's pixels and a group's channels
+ *   mu = mean x, r = (mean (x - mu)^2 + eps)^-1/2, z = (x - mu) r weight + bias, y = act(z)
+ * in fp32, y rounded to `dtype`; act(z) = z or z / (1 + exp(-z)).
+ *
+ * Arguments:
+ *   X, Y      [images, pixels, channels] in `dtype`, aligned to their elements (Y == X: in place)
+ *   weight, bias  nullable [channels] in `weight_dtype`, which is dtype or
+ *             SCRAM_F32 (NULL: ones, zeros)
+ *   eps       >= 0, finite
+ *   mean, rstd  nullable (both) fp32 [images, groups]: mu and r, for the gradient
+ *   workspace scram_group_norm_workspace_bytes(...) bytes, 256-byte aligned
+ * images * pixels * channels < 2^40, images * groups < 2^31.  Outputs and the
+ * workspace overlap nothing else.  Returns a status code.
+ */
+size_t scram_group_norm_workspace_bytes(int64_t images, int64_t pixels, int channels, int groups, int dtype);
+
+int scram_group_norm(const void* X, int dtype, const void* weight, const void* bias, int weight_dtype, int64_t images,
+                     int64_t pixels, int channels, int groups, float eps, int activation, void* Y, float* mean,
+                     float* rstd, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Gradients of scram_group_norm.  With xh = (x - mean) rstd, z as there,
+ * dz = dY act'(z) and g = dz weight, means over an image's group:
+ *   dX = rstd (g - mean(g) - xh mean(g xh)),  dweight = sum dz xh,  dbias = sum dz
+ * (sums over images and pixels).  dY and dX are in `grad_dtype`, which is dtype
+ * or SCRAM_F32 (dX == dY: in place); dweight and dbias fp32 [channels], summed
+ * in a fixed order.  `bias` is read for the activation alone.
+ */
+size_t scram_group_norm_backward_workspace_bytes(int64_t images, int64_t pixels, int channels, int groups, int dtype);
+
+int scram_group_norm_backward(const void* dY, int grad_dtype, const void* X, int dtype, const float* mean,
+                              const float* rstd, const void* weight, const void* bias, int weight_dtype, int64_t images,
+                              int64_t pixels, int channels, int groups, int activation, void* dX, float* dweight,
+                              float* dbias, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* scram_status_string(int status);

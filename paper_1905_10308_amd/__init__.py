@@ -25,12 +25,26 @@ from .binding import (  # noqa: F401
     sparse_attend_backward_workspace_bytes,
     status_string,
 )
+from .dense import (  # noqa: F401
+    bias_edges,
+    dense_attend,
+    dense_attend_backward,
+    dense_attend_backward_workspace_bytes,
+    dense_attend_workspace_bytes,
+    relative_bias,
+    relative_bias_backward,
+    relative_bias_backward_workspace_bytes,
+)
 from .differential import (  # noqa: F401
     differential_attend,
     differential_attend_backward,
     differential_attend_backward_workspace_bytes,
 )
 from .rows import (  # noqa: F401
+    group_norm,
+    group_norm_backward,
+    group_norm_backward_workspace_bytes,
+    group_norm_workspace_bytes,
     layer_norm,
     layer_norm_backward,
     layer_norm_backward_workspace_bytes,

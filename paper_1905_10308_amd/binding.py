@@ -100,6 +100,28 @@ def load(path: str) -> ctypes.CDLL:
     L.scram_layer_norm_backward.restype = I
     L.scram_layer_norm_backward_workspace_bytes.argtypes = [I64, I]
     L.scram_layer_norm_backward_workspace_bytes.restype = SZ
+    L.scram_dense_attend_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I, I]
+    L.scram_dense_attend_workspace_bytes.restype = SZ
+    L.scram_dense_attend.argtypes = [P, P, P, I, P, I, P, I, I, I, I, I, I, I, I, F, U32, I, P, P, P, SZ, P, P]
+    L.scram_dense_attend.restype = I
+    L.scram_dense_attend_backward_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I, I]
+    L.scram_dense_attend_backward_workspace_bytes.restype = SZ
+    L.scram_dense_attend_backward.argtypes = [P, P, P, I, P, I, P, I, I, I, I, I, I, I, I, F, U32, I, P, P, P, P, P, P, P, SZ, P, P]
+    L.scram_dense_attend_backward.restype = I
+    L.scram_relative_bias.argtypes = [P, I, I, I, I, P, I, P, I, P, P]
+    L.scram_relative_bias.restype = I
+    L.scram_relative_bias_backward_workspace_bytes.argtypes = [I, I, I, I]
+    L.scram_relative_bias_backward_workspace_bytes.restype = SZ
+    L.scram_relative_bias_backward.argtypes = [P, I, I, I, I, P, I, P, I, P, P, SZ, P]
+    L.scram_relative_bias_backward.restype = I
+    L.scram_group_norm_workspace_bytes.argtypes = [I64, I64, I, I, I]
+    L.scram_group_norm_workspace_bytes.restype = SZ
+    L.scram_group_norm.argtypes = [P, I, P, P, I, I64, I64, I, I, F, I, P, P, P, P, SZ, P]
+    L.scram_group_norm.restype = I
+    L.scram_group_norm_backward_workspace_bytes.argtypes = [I64, I64, I, I, I]
+    L.scram_group_norm_backward_workspace_bytes.restype = SZ
+    L.scram_group_norm_backward.argtypes = [P, I, P, I, P, P, P, P, I, I64, I64, I, I, I, P, P, P, P, SZ, P]
+    L.scram_group_norm_backward.restype = I
     L.scram_status_string.argtypes = [I]
     L.scram_status_string.restype = ctypes.c_char_p
     L.scram_abi_version.argtypes = []

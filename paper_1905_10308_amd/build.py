@@ -22,8 +22,9 @@ LIB_PATH = os.path.join(LIB_DIR, "libscram.so")
 ORDER_LIB_PATH = os.path.join(LIB_DIR, "libscram_order.so")
 ORDER_DEFINES = ["-DSCRAM_LANE_TILE_SKEW=1", "-DSCRAM_BAND_TILES=3", "-DSCRAM_BAND_MAX=0", "-DSCRAM_XCD_REMAP=0"]
 SOURCES = [os.path.join(CSRC, f) for f in ("scram_pm.hip", "scram_attend.hip", "scram_backward.hip", "scram_snis.hip",
-                                             "scram_diff.hip", "scram_diff_backward.hip", "scram_rotary.hip",
-                                             "scram_norm.hip", "scram_pad.hip", "scram_noalloc.hip", "scram_api.cpp")]
+                                             "scram_diff.hip", "scram_diff_backward.hip", "scram_dense.hip",
+                                             "scram_dense_backward.hip", "scram_bias.hip", "scram_rotary.hip",
+                                             "scram_norm.hip", "scram_group.hip", "scram_pad.hip", "scram_noalloc.hip", "scram_api.cpp")]
 ARCH = "gfx950"
 
 COMPILE_FLAGS = [
@@ -41,7 +42,8 @@ LINK_FLAGS = [f"--offload-arch={ARCH}", "-shared", "-fPIC"]
 # per-source additions: the attends' matrix-core kernels keep their accumulators in VGPRs (the
 # compiler would otherwise copy them between AGPRs and VGPRs around every rescale)
 _VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-EXTRA_FLAGS = {"scram_attend.hip": _VGPR_FORM, "scram_diff.hip": _VGPR_FORM, "scram_diff_backward.hip": _VGPR_FORM}
+EXTRA_FLAGS = {f: _VGPR_FORM for f in ("scram_attend.hip", "scram_diff.hip", "scram_diff_backward.hip", "scram_dense.hip",
+                                       "scram_dense_backward.hip")}
 
 
 def hipcc() -> str:

@@ -75,6 +75,69 @@ int check_differential(int dtype, const scram::Grid& g, int kappa, int dv, int w
     return SCRAM_OK;
 }
 
+// Arguments that the dense attend and its gradients share, but for pointers.
+int check_dense(int dtype, const scram::DenseCall& c, int dv, uint32_t flags)
+{
+    const scram::Grid& g = c.g;
+    int rc = check_grid(g.S, g.Hq, g.Wq, g.Hk, g.Wk);
+    if (rc) return rc;
+    if (c.key_slices < 1 || g.S % c.key_slices) return SCRAM_ERR_SHAPE;
+    if (!isfinite(c.scale)) return SCRAM_ERR_SHAPE;
+    if ((rc = check_type(dtype, g.d))) return rc;
+    if (dv != g.d) return SCRAM_ERR_UNSUPPORTED;
+    if (flags & ~uint32_t(SCRAM_CAUSAL)) return SCRAM_ERR_UNSUPPORTED;
+    const int64_t nq = int64_t(g.Hq) * g.Wq, nk = int64_t(g.Hk) * g.Wk;
+    if (c.bias) {
+        if (c.bias_rows < 1 || g.S % c.bias_rows) return SCRAM_ERR_SHAPE;
+        if ((2 * int64_t(g.Hk) - 1) * (2 * int64_t(g.Wk) - 1) >= kMaxCount) return SCRAM_ERR_SHAPE;
+        if (scram::dense_bias_window(g.Hk, g.Wk) > scram::kBiasWindowMost) return SCRAM_ERR_SHAPE;
+    }
+    if (!(flags & SCRAM_CAUSAL) && !c.bias) return c.first != 0 || c.origin ? SCRAM_ERR_SHAPE : SCRAM_OK;
+    // the queries are a run of the keys' raster: whole rows, or a part of it as one row
+    if (g.Hq != 1 && g.Wq != g.Wk) return SCRAM_ERR_SHAPE;
+    if (c.first < 0 || (c.origin && c.first != 0) || c.first + nq > nk) return SCRAM_ERR_SHAPE;
+    return SCRAM_OK;
+}
+
+scram::DenseCall dense_call(const void* Q, const void* K, const void* V, const void* bias, int bias_rows, const int32_t* lengths,
+                            int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, float scale, uint32_t flags, int first,
+                            const int32_t* origin)
+{
+    return scram::DenseCall{Q,     K,      V, bias, bias ? bias_rows : 0, lengths, scram::Grid{S, Hq, Wq, Hk, Wk, d}, key_slices, scale,
+                            (flags & SCRAM_CAUSAL) != 0, first, origin};
+}
+
+size_t bias_bytes(const scram::DenseCall& c, size_t eb)
+{
+    return c.bias ? size_t(c.bias_rows) * (2 * size_t(c.g.Hk) - 1) * (2 * size_t(c.g.Wk) - 1) * eb : 0;
+}
+
+int check_relative(int dtype, int heads, int H, int W, const int* edges_y, int my, const int* edges_x, int mx)
+{
+    if (heads < 1 || H < 1 || W < 1 || H > kMaxSide || W > kMaxSide) return SCRAM_ERR_SHAPE;
+    const int64_t plane = (2 * int64_t(H) - 1) * (2 * int64_t(W) - 1);
+    if (plane >= kMaxCount || heads >= (int64_t(1) << 40) / plane) return SCRAM_ERR_SHAPE;
+    if (my < 0 || mx < 0 || my > SCRAM_BIAS_MAX_EDGES || mx > SCRAM_BIAS_MAX_EDGES) return SCRAM_ERR_SHAPE;
+    if ((my && !edges_y) || (mx && !edges_x)) return SCRAM_ERR_NULL;
+    for (int k = 0; k < my; ++k)
+        if (edges_y[k] <= (k ? edges_y[k - 1] : 0)) return SCRAM_ERR_SHAPE;
+    for (int k = 0; k < mx; ++k)
+        if (edges_x[k] <= (k ? edges_x[k - 1] : 0)) return SCRAM_ERR_SHAPE;
+    return dtype == SCRAM_F32 || dtype == SCRAM_BF16 ? SCRAM_OK : SCRAM_ERR_UNSUPPORTED;
+}
+
+int check_group(int64_t images, int64_t pixels, int channels, int groups, int dtype, int weight_dtype, int activation)
+{
+    const int64_t most = int64_t(1) << 40;
+    if (images < 1 || pixels < 1 || channels < 1 || channels > scram::kNormMaxChannels) return SCRAM_ERR_SHAPE;
+    if (images >= most || pixels >= most / images || images * pixels >= most / channels) return SCRAM_ERR_SHAPE;
+    if (groups < 1 || channels % groups || images >= kMaxCount / groups) return SCRAM_ERR_SHAPE;
+    if (dtype != SCRAM_F32 && dtype != SCRAM_BF16) return SCRAM_ERR_UNSUPPORTED;
+    if (weight_dtype != dtype && weight_dtype != SCRAM_F32) return SCRAM_ERR_UNSUPPORTED;
+    if (activation != SCRAM_ACT_NONE && activation != SCRAM_ACT_SILU) return SCRAM_ERR_UNSUPPORTED;
+    return SCRAM_OK;
+}
+
 int check_norm(int64_t rows, int channels, int dtype, int weight_dtype)
 {
     if (rows < 1 || rows >= (int64_t(1) << 40) || channels < 1 || channels > scram::kNormMaxChannels) return SCRAM_ERR_SHAPE;
@@ -561,6 +624,209 @@ int scram_layer_norm_backward(const void* dY, int grad_dtype, const void* X, int
     }
     const scram::NormCall c{rows, channels, dtype, grad_dtype, weight_dtype, X, weight, nullptr, dY, 0.f};
     return scram::launch_norm_backward(c, mean, rstd, dX, dweight, dbias, workspace, stream) == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+size_t scram_dense_attend_workspace_bytes(int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dtype, int biased)
+{
+    if (check_grid(S, Hq, Wq, Hk, Wk) || key_slices < 1 || S % key_slices || check_type(dtype, d)) return 0;
+    return scram::dense_workspace_bytes(dense_call(nullptr, nullptr, nullptr, biased ? "" : nullptr, 1, nullptr, S, key_slices, Hq, Wq,
+                                                   Hk, Wk, d, 1.f, 0, 0, nullptr));
+}
+
+int scram_dense_attend(const void* Q, const void* K, const void* V, int dtype, const void* bias, int bias_rows,
+                       const int32_t* lengths, int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dv, float scale,
+                       uint32_t flags, int first, const int32_t* origin, void* out, void* workspace, size_t workspace_bytes,
+                       hipEvent_t* events, hipStream_t stream)
+{
+    if (!Q || !K || !V || !out) return SCRAM_ERR_NULL;
+    const scram::DenseCall call =
+        dense_call(Q, K, V, bias, bias_rows, lengths, S, key_slices, Hq, Wq, Hk, Wk, d, scale, flags, first, origin);
+    int rc = check_dense(dtype, call, dv, flags);
+    if (rc) return rc;
+    if (scram::dense_blocks(call) > kMaxBlocks) return SCRAM_ERR_SHAPE;
+    const size_t eb = elem_bytes(dtype), need = scram::dense_workspace_bytes(call);
+    if (need && !workspace) return SCRAM_ERR_WORKSPACE;
+    if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(bias, eb) || !aligned(lengths, 4) ||
+        !aligned(origin, 4) || (need && !aligned(workspace, 256)))
+        return SCRAM_ERR_ALIGN;
+    if (workspace_bytes < need) return SCRAM_ERR_WORKSPACE;
+    const size_t n = size_t(S) * Hq * Wq, nk = size_t(key_slices) * Hk * Wk;
+    const Range outs[] = {range(out, n * dv * eb), range(workspace, need)};
+    for (const Range& o : outs) {
+        for (const Range& other : {range(Q, n * d * eb), range(K, nk * d * eb), range(V, nk * dv * eb), range(bias, bias_bytes(call, eb)),
+                                   range(lengths, lengths ? 4 * size_t(key_slices) : 0), range(origin, origin ? 4 * size_t(S) : 0)}) {
+            if (overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+    }
+    if (overlap(outs[0], outs[1])) return SCRAM_ERR_ALIAS;
+    const hipError_t e = scram::launch_dense(dtype, call, out, workspace, stream, events ? events[0] : nullptr,
+                                             events ? events[1] : nullptr);
+    return e == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+size_t scram_dense_attend_backward_workspace_bytes(int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dtype,
+                                                   int bias_rows)
+{
+    if (check_grid(S, Hq, Wq, Hk, Wk) || key_slices < 1 || S % key_slices || check_type(dtype, d)) return 0;
+    if (bias_rows < 0 || (bias_rows && S % bias_rows)) return 0;
+    return scram::dense_backward_workspace_bytes(dense_call(nullptr, nullptr, nullptr, bias_rows ? "" : nullptr, bias_rows, nullptr, S,
+                                                            key_slices, Hq, Wq, Hk, Wk, d, 1.f, 0, 0, nullptr));
+}
+
+int scram_dense_attend_backward(const void* Q, const void* K, const void* V, int dtype, const void* bias, int bias_rows,
+                                const int32_t* lengths, int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dv,
+                                float scale, uint32_t flags, int first, const int32_t* origin, const void* dO, void* dQ, void* dK,
+                                void* dV, void* dbias, void* workspace, size_t workspace_bytes, hipEvent_t* events,
+                                hipStream_t stream)
+{
+    if (!Q || !K || !V || !dO || !dQ || !dK || !dV) return SCRAM_ERR_NULL;
+    if (dbias && !bias) return SCRAM_ERR_NULL;
+    const scram::DenseCall call =
+        dense_call(Q, K, V, bias, bias_rows, lengths, S, key_slices, Hq, Wq, Hk, Wk, d, scale, flags, first, origin);
+    int rc = check_dense(dtype, call, dv, flags);
+    if (rc) return rc;
+    if (scram::dense_backward_blocks(call) > kMaxBlocks) return SCRAM_ERR_SHAPE;
+    if (!workspace) return SCRAM_ERR_WORKSPACE;
+    const size_t eb = elem_bytes(dtype), need = scram::dense_backward_workspace_bytes(call);
+    if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(dO, 16) || !aligned(bias, eb) || !aligned(lengths, 4) ||
+        !aligned(origin, 4) || !aligned(dQ, 16) || !aligned(dK, 16) || !aligned(dV, 16) || !aligned(dbias, eb) ||
+        !aligned(workspace, 256))
+        return SCRAM_ERR_ALIGN;
+    if (workspace_bytes < need) return SCRAM_ERR_WORKSPACE;
+    const size_t n = size_t(S) * Hq * Wq, nk = size_t(key_slices) * Hk * Wk, bb = bias_bytes(call, eb);
+    const Range outs[] = {range(dQ, n * d * eb), range(dK, nk * d * eb), range(dV, nk * dv * eb), range(dbias, dbias ? bb : 0),
+                          range(workspace, need)};
+    for (const Range& o : outs) {
+        for (const Range& other : {range(Q, n * d * eb), range(K, nk * d * eb), range(V, nk * dv * eb), range(dO, n * dv * eb),
+                                   range(bias, bb), range(lengths, lengths ? 4 * size_t(key_slices) : 0),
+                                   range(origin, origin ? 4 * size_t(S) : 0)}) {
+            if (overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+        for (const Range& other : outs) {
+            if (&o != &other && overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+    }
+    const hipError_t e = scram::launch_dense_backward(dtype, call, dO, dQ, dK, dV, dbias, workspace, stream,
+                                                      events ? events[0] : nullptr, events ? events[1] : nullptr);
+    return e == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+int scram_relative_bias(const void* table, int dtype, int heads, int H, int W, const int* edges_y, int my, const int* edges_x, int mx,
+                        void* bias, hipStream_t stream)
+{
+    if (!table || !bias) return SCRAM_ERR_NULL;
+    int rc = check_relative(dtype, heads, H, W, edges_y, my, edges_x, mx);
+    if (rc) return rc;
+    const size_t eb = elem_bytes(dtype);
+    if (!aligned(table, eb) || !aligned(bias, eb)) return SCRAM_ERR_ALIGN;
+    if (overlap(range(bias, size_t(heads) * (2 * size_t(H) - 1) * (2 * size_t(W) - 1) * eb),
+                range(table, size_t(heads) * (2 * my + 1) * (2 * mx + 1) * eb)))
+        return SCRAM_ERR_ALIAS;
+    const scram::BiasCall c{dtype, heads, H, W, {my, mx}, {edges_y, edges_x}};
+    return scram::launch_relative_bias(c, table, bias, stream) == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+size_t scram_relative_bias_backward_workspace_bytes(int heads, int H, int W, int mx)
+{
+    if (mx < 0 || mx > SCRAM_BIAS_MAX_EDGES || check_relative(SCRAM_F32, heads, H, W, nullptr, 0, nullptr, 0)) return 0;
+    return scram::relative_bias_backward_workspace_bytes(scram::BiasCall{SCRAM_F32, heads, H, W, {0, mx}, {nullptr, nullptr}});
+}
+
+int scram_relative_bias_backward(const void* dbias, int dtype, int heads, int H, int W, const int* edges_y, int my, const int* edges_x,
+                                 int mx, void* dtable, void* workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    if (!dbias || !dtable) return SCRAM_ERR_NULL;
+    int rc = check_relative(dtype, heads, H, W, edges_y, my, edges_x, mx);
+    if (rc) return rc;
+    if (!workspace) return SCRAM_ERR_WORKSPACE;
+    const size_t eb = elem_bytes(dtype);
+    if (!aligned(dbias, eb) || !aligned(dtable, eb) || !aligned(workspace, 256)) return SCRAM_ERR_ALIGN;
+    const scram::BiasCall c{dtype, heads, H, W, {my, mx}, {edges_y, edges_x}};
+    const size_t need = scram::relative_bias_backward_workspace_bytes(c);
+    if (workspace_bytes < need) return SCRAM_ERR_WORKSPACE;
+    const Range in = range(dbias, size_t(heads) * (2 * size_t(H) - 1) * (2 * size_t(W) - 1) * eb);
+    const Range out = range(dtable, size_t(heads) * (2 * my + 1) * (2 * mx + 1) * eb), ws = range(workspace, need);
+    if (overlap(in, out) || overlap(in, ws) || overlap(out, ws)) return SCRAM_ERR_ALIAS;
+    return scram::launch_relative_bias_backward(c, dbias, dtable, workspace, stream) == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+size_t scram_group_norm_workspace_bytes(int64_t images, int64_t pixels, int channels, int groups, int dtype)
+{
+    if (check_group(images, pixels, channels, groups, dtype, dtype, SCRAM_ACT_NONE)) return 0;
+    return scram::group_norm_workspace_bytes(
+        scram::GroupCall{images, pixels, channels, groups, dtype, dtype, dtype, 0, nullptr, nullptr, nullptr, nullptr, 0.f});
+}
+
+int scram_group_norm(const void* X, int dtype, const void* weight, const void* bias, int weight_dtype, int64_t images, int64_t pixels,
+                     int channels, int groups, float eps, int activation, void* Y, float* mean, float* rstd, void* workspace,
+                     size_t workspace_bytes, hipStream_t stream)
+{
+    if (!X || !Y || !mean != !rstd) return SCRAM_ERR_NULL;
+    int rc = check_group(images, pixels, channels, groups, dtype, weight_dtype, activation);
+    if (rc) return rc;
+    if (!(eps >= 0.f) || !isfinite(eps)) return SCRAM_ERR_SHAPE;
+    if (!workspace) return SCRAM_ERR_WORKSPACE;
+    const size_t eb = elem_bytes(dtype), wb = elem_bytes(weight_dtype);
+    if (!aligned(X, eb) || !aligned(Y, eb) || !aligned(weight, wb) || !aligned(bias, wb) || !aligned(mean, 4) || !aligned(rstd, 4) ||
+        !aligned(workspace, 256))
+        return SCRAM_ERR_ALIGN;
+    const scram::GroupCall c{images, pixels, channels, groups, dtype, dtype, weight_dtype, activation, X, weight, bias, nullptr, eps};
+    const size_t need = scram::group_norm_workspace_bytes(c);
+    if (workspace_bytes < need) return SCRAM_ERR_WORKSPACE;
+    const size_t n = size_t(images) * pixels * channels, stat = mean ? 4 * size_t(images) * groups : 0;
+    const Range outs[] = {range(Y, n * eb), range(mean, stat), range(rstd, stat), range(workspace, need)};
+    for (const Range& o : outs) {
+        // Y may be X: an element is read before it is written, and after the statistics
+        if (overlap(o, range(X, n * eb)) && !(&o == &outs[0] && Y == X)) return SCRAM_ERR_ALIAS;
+        if (overlap(o, range(weight, weight ? wb * channels : 0)) || overlap(o, range(bias, bias ? wb * channels : 0)))
+            return SCRAM_ERR_ALIAS;
+        for (const Range& other : outs) {
+            if (&o != &other && overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+    }
+    return scram::launch_group_norm(c, Y, mean, rstd, workspace, stream) == hipSuccess ? SCRAM_OK : SCRAM_ERR_HIP;
+}
+
+size_t scram_group_norm_backward_workspace_bytes(int64_t images, int64_t pixels, int channels, int groups, int dtype)
+{
+    if (check_group(images, pixels, channels, groups, dtype, dtype, SCRAM_ACT_NONE)) return 0;
+    return scram::group_norm_backward_workspace_bytes(
+        scram::GroupCall{images, pixels, channels, groups, dtype, dtype, dtype, 0, nullptr, nullptr, nullptr, nullptr, 0.f});
+}
+
+int scram_group_norm_backward(const void* dY, int grad_dtype, const void* X, int dtype, const float* mean, const float* rstd,
+                              const void* weight, const void* bias, int weight_dtype, int64_t images, int64_t pixels, int channels,
+                              int groups, int activation, void* dX, float* dweight, float* dbias, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream)
+{
+    if (!dY || !X || !mean || !rstd || !dX || !dweight || !dbias) return SCRAM_ERR_NULL;
+    int rc = check_group(images, pixels, channels, groups, dtype, weight_dtype, activation);
+    if (rc) return rc;
+    if (grad_dtype != dtype && grad_dtype != SCRAM_F32) return SCRAM_ERR_UNSUPPORTED;
+    if (!workspace) return SCRAM_ERR_WORKSPACE;
+    const size_t eb = elem_bytes(dtype), gb = elem_bytes(grad_dtype), wb = elem_bytes(weight_dtype);
+    if (!aligned(X, eb) || !aligned(dY, gb) || !aligned(dX, gb) || !aligned(weight, wb) || !aligned(bias, wb) || !aligned(mean, 4) ||
+        !aligned(rstd, 4) || !aligned(dweight, 4) || !aligned(dbias, 4) || !aligned(workspace, 256))
+        return SCRAM_ERR_ALIGN;
+    const scram::GroupCall c{images, pixels, channels, groups, dtype, grad_dtype, weight_dtype, activation, X, weight, bias, dY, 0.f};
+    const size_t need = scram::group_norm_backward_workspace_bytes(c);
+    if (workspace_bytes < need) return SCRAM_ERR_WORKSPACE;
+    const size_t n = size_t(images) * pixels * channels, stat = 4 * size_t(images) * groups;
+    const Range outs[] = {range(dX, n * gb), range(dweight, 4 * size_t(channels)), range(dbias, 4 * size_t(channels)),
+                          range(workspace, need)};
+    for (const Range& o : outs) {
+        // dX may be dY: an element is read before it is written, and after the sums
+        if (overlap(o, range(dY, n * gb)) && !(&o == &outs[0] && dX == dY)) return SCRAM_ERR_ALIAS;
+        for (const Range& other : {range(X, n * eb), range(mean, stat), range(rstd, stat), range(weight, weight ? wb * channels : 0),
+                                   range(bias, bias ? wb * channels : 0)}) {
+            if (overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+        for (const Range& other : outs) {
+            if (&o != &other && overlap(o, other)) return SCRAM_ERR_ALIAS;
+        }
+    }
+    return scram::launch_group_norm_backward(c, mean, rstd, dX, dweight, dbias, workspace, stream) == hipSuccess ? SCRAM_OK
+                                                                                                                 : SCRAM_ERR_HIP;
 }
 
 const char* scram_status_string(int status)

@@ -1,0 +1,583 @@
+// Gradients of the attention over every key.
+//
+//   p_ij = softmax_j(scale q_i.k_j + bias), dp_ij = dO_i.v_j, D_i = sum_j p_ij dp_ij, ds_ij = p_ij (dp_ij - D_i)
+//   dQ_i = scale sum_j ds_ij k_j, dK_j = scale sum_i ds_ij q_i, dV_j = sum_i p_ij dO_i, dB_o = sum of ds_ij at offset o
+//
+// Bound by computing: five products of a pair's rows are what cannot be done
+// without, 10 d operations a pair.  Three kernels, each with one writer for
+// every result and sums of a fixed order:
+// - queries: a block holds 128 and passes over the keys twice.  The first pass
+//   gives the softmax's statistics and D (of fp32 weights: where one weight is
+//   nearly 1, dp - D is what is left of two nearly equal numbers, which a D
+//   from the rounded output would bury), the second dQ;
+// - keys: a block holds 128 and passes over the queries: dK and dV;
+// - offsets, with a bias: scores and ds once more, added up in registers over
+//   all pairs of tiles at one offset, whose diagonals are then one offset each.
+// The products with p and ds take them from the registers that formed them
+// (scram_dense.h).
+
+#include "scram_dense.h"
+
+namespace scram {
+namespace {
+
+constexpr int kRowsBlock = 128;  // queries or keys of a block
+
+struct DenseBackward : DenseParams {
+    const void* dO;
+    void* dQ;
+    void* dK;
+    void* dV;
+    void* dbias;       // nullable
+    float4* stats;     // [all query rows] row_stats()
+    float* part;       // key side: [splits][all keys][2][D]
+    float* diagonals;  // [bias rows][2 Hk - 1][2 x_tiles - 1][64]
+    int64_t all_keys;
+    int tiles;         // of a group's queries, or of a slice's keys
+    int splits;        // key side: runs of query tiles
+    int x_tiles, Hk, Wk, key_slices, S;
+};
+
+// A row's softmax for the other kernels: weights are exp2(x - x0) f for scores x in base 2, x0 the logarithm of their sum and
+// f 1.  Scores so large that adding the logarithm would lose it (a bias of the type's lowest values) keep them apart: x0 is
+// the maximum, f one over the sum.  The third value is D.
+__device__ __forceinline__ float4 row_stats(float top, float sum, float dsum)
+{
+    if (sum == 0.f) return make_float4(INFINITY, 1.f, 0.f, 0.f);  // no key: exp2(x - infinity) = 0
+    const bool apart = fabsf(top) > 4096.f;
+    return make_float4(apart ? top : top + __builtin_amdgcn_logf(sum), apart ? 1.f / sum : 1.f, dsum / sum, 0.f);
+}
+
+// Rows of the other side that a block stages at a time.
+template <typename T, int D>
+constexpr int kStaged = D * sizeof(T) > 256 ? 32 : 64;
+
+template <typename T, int D>
+constexpr size_t backward_lds()
+{
+    using R = DenseRow<T, D>;
+    return 2 * (kStaged<T, D> * R::kStride) + R::kSlack;
+}
+
+// The query side.
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(kBlock) void dense_query_kernel(DenseBackward p)
+{
+    using R = DenseRow<T, D>;
+    constexpr int kKeys = kStaged<T, D>, U = kKeys / 32;
+    extern __shared__ __align__(16) unsigned char lds[];
+    unsigned char* const k_tile = lds;
+    unsigned char* const v_tile = lds + kKeys * R::kStride;
+    int* const s_place = reinterpret_cast<int*>(lds + backward_lds<T, D>());
+    float* const s_bias = reinterpret_cast<float*>(s_place + kKeys);
+    __shared__ int s_end[4];
+
+    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
+    const int tile = static_cast<int>(b % static_cast<uint32_t>(p.tiles));
+    const int group = static_cast<int>(b / static_cast<uint32_t>(p.tiles));
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int slice_k = p.per_group == 1 ? group / p.share : group;
+    const int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
+    const int row = tile * kRowsBlock + wave * 32 + m;
+    const bool live = row < p.rows;
+    uint32_t head, q;
+    divmod(static_cast<uint32_t>(min(row, p.rows - 1)), p.div_nq, head, q);
+    const int slice = group * p.per_group + static_cast<int>(head);
+    const int begin = p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first;
+    const int at = begin + static_cast<int>(q);
+    const int end = live ? (p.causal ? min(length, at + 1) : length) : 0;
+    int last = length;
+    if (p.causal) {
+        int e = end;
+        for (int k = 32; k >= 1; k >>= 1) e = max(e, __shfl_xor(e, k));
+        if (lane == 0) s_end[wave] = e;
+        __syncthreads();
+        last = max(max(s_end[0], s_end[1]), max(s_end[2], s_end[3]));
+    }
+    const int all = (last + kKeys - 1) / kKeys;
+
+    const int64_t out_row = static_cast<int64_t>(group) * p.rows + row;
+    const int64_t from_row = live ? out_row : static_cast<int64_t>(group) * p.rows;
+    uint4 qf[R::kSteps], gf[R::kSteps];
+    load_operand<T, D>(p.Q, from_row, h, qf);
+    load_operand<T, D>(p.dO, from_row, h, gf);
+
+    DenseLoad<T, D, kKeys> kl, vl;
+    const int64_t k_row = static_cast<int64_t>(slice_k) * p.nk;
+    BiasWindow<T> win{};
+    int my_place = 0;
+    if constexpr (BIAS) my_place = BiasWindow<T>::place(p, at);
+    f32x16_t s[U], g[U];
+    // the tile's scores in base 2 (minus infinity: not seen) and dp
+    auto scores = [&](int t) {
+        const int k0 = t * kKeys;
+        kl.store(k_tile);
+        vl.store(v_tile);
+        if constexpr (BIAS) {
+            const int k1 = min(k0 + kKeys, p.nk) - 1;
+            const int q0 = tile * kRowsBlock, q1 = min(q0 + kRowsBlock, p.rows) - 1;
+            win.stage(p, slice % p.plane.rows, begin + q0, begin + q1, k0, k1, s_bias);
+            if (threadIdx.x < kKeys) s_place[threadIdx.x] = BiasWindow<T>::place(p, min(k0 + static_cast<int>(threadIdx.x), k1));
+        }
+        __syncthreads();
+        const int next = t + 1 < all ? t + 1 : 0;  // the second pass begins again
+        kl.load(p.K, k_row + next * static_cast<int64_t>(kKeys), last - next * kKeys);
+        vl.load(p.V, k_row + next * static_cast<int64_t>(kKeys), last - next * kKeys);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            s[u] = f32x16_t(0.f);
+            g[u] = f32x16_t(0.f);
+#pragma unroll
+            for (int c = 0; c < R::kSteps; ++c) {
+                s[u] = mma<T>(row_operand<T, D>(k_tile, 32 * u + tile_row<T>(m), h, c), qf[c], s[u]);
+                g[u] = mma<T>(row_operand<T, D>(v_tile, 32 * u + tile_row<T>(m), h, c), gf[c], g[u]);
+            }
+        }
+        const bool whole = __all(end >= k0 + kKeys);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int key = 32 * u + tile_slot<T>(i) + tile_half<T>() * h;
+                float x = s[u][i] * p.scale2;
+                if constexpr (BIAS) x = fmaf(s[u][i], p.scale2, s_bias[s_place[key] - my_place - win.base]);
+                if (!whole) x = k0 + key < end ? x : -INFINITY;
+                s[u][i] = x;
+            }
+    };
+
+    float top = -INFINITY, sum = 0.f, dsum = 0.f;
+    if (all > 0) {
+        kl.load(p.K, k_row, last);
+        vl.load(p.V, k_row, last);
+    }
+    for (int t = 0; t < all; ++t) {
+        scores(t);
+        float most = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, s[u][i]);
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float next = fmaxf(top, most), shift = next == -INFINITY ? 0.f : next;
+        const float keep = __builtin_amdgcn_exp2f(top - shift);
+        sum *= keep;
+        dsum *= keep;
+        top = next;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float e = __builtin_amdgcn_exp2f(s[u][i] - shift);
+                sum += e;
+                dsum = fmaf(e, g[u][i], dsum);
+            }
+        __syncthreads();
+    }
+    sum += __shfl_xor(sum, 32);
+    dsum += __shfl_xor(dsum, 32);
+    const float4 stats = row_stats(top, sum, dsum);
+    if (live && h == 0) p.stats[out_row] = stats;
+    // here the sum divides once, at the end
+    const float shift = top == -INFINITY ? 0.f : top, mean = stats.z;
+    const float factor = sum == 0.f ? 0.f : p.scale / sum;
+
+    f32x16_t o[R::kColumns];
+#pragma unroll
+    for (int c = 0; c < R::kColumns; ++c) o[c] = f32x16_t(0.f);
+    for (int t = 0; t < all; ++t) {
+        scores(t);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[u][i] = __builtin_amdgcn_exp2f(s[u][i] - shift) * (g[u][i] - mean);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < R::kRowSteps; ++r) {
+                const uint4 w = as_operand<T>(s[u], r);
+#pragma unroll
+                for (int c = 0; c < R::kColumns; ++c) o[c] = mma<T>(column_operand<T, D>(k_tile, 32 * u, r, c), w, o[c]);
+            }
+        __syncthreads();
+    }
+    if (!live) return;
+    T* const to = static_cast<T*>(p.dQ) + out_row * D;
+#pragma unroll
+    for (int c = 0; c < R::kColumns; ++c)
+#pragma unroll
+        for (int i = 0; i < (D < 32 ? 2 : 4); ++i) {
+            vec<T, 4> x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = from_float<T>(o[c][4 * i + j] * factor);
+            store_vec<T, 4>(to + 32 * c + 8 * i + 4 * h, x);
+        }
+}
+
+// The key side: a block's 128 keys against a run of the query tiles of the slices that read them.
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
+{
+    using R = DenseRow<T, D>;
+    constexpr int kRows = kStaged<T, D>, U = kRows / 32;
+    extern __shared__ __align__(16) unsigned char lds[];
+    unsigned char* const q_tile = lds;
+    unsigned char* const g_tile = lds + kRows * R::kStride;
+    int* const s_place = reinterpret_cast<int*>(lds + backward_lds<T, D>());
+    float* const s_bias = reinterpret_cast<float*>(s_place + kRows);
+    __shared__ __align__(16) float s_lse[kRows], s_mean[kRows], s_factor[kRows];
+
+    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
+    const int split = static_cast<int>(b % static_cast<uint32_t>(p.splits));
+    const int tile = static_cast<int>(b / static_cast<uint32_t>(p.splits) % static_cast<uint32_t>(p.tiles));
+    const int slice_k = static_cast<int>(b / static_cast<uint32_t>(p.splits) / static_cast<uint32_t>(p.tiles));
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    // the keys that count and that some query sees: no others are read
+    int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
+    if (p.causal) {
+        int reach = p.first + p.nq;
+        if (p.origin) {
+            reach = 0;
+            for (int s = 0; s < p.share; ++s)
+                reach = max(reach, min(max(p.origin[slice_k * static_cast<int64_t>(p.share) + s], 0), p.nk - p.nq) + p.nq);
+        }
+        length = min(length, reach);
+    }
+    const int k_first = tile * kRowsBlock, key = k_first + wave * 32 + m;
+    const bool seen = key < length;
+    const int64_t k_row = static_cast<int64_t>(slice_k) * p.nk;
+
+    uint4 kf[R::kSteps], vf[R::kSteps];
+#pragma unroll
+    for (int c = 0; c < R::kSteps; ++c) kf[c] = vf[c] = make_uint4(0u, 0u, 0u, 0u);
+    if (seen) {
+        load_operand<T, D>(p.K, k_row + key, h, kf);
+        load_operand<T, D>(p.V, k_row + key, h, vf);
+    }
+    f32x16_t dk[R::kColumns], dv[R::kColumns];
+#pragma unroll
+    for (int c = 0; c < R::kColumns; ++c) dk[c] = dv[c] = f32x16_t(0.f);
+    int my_place = 0;
+    if constexpr (BIAS) my_place = BiasWindow<T>::place(p, min(key, p.nk - 1));
+
+    const int per_slice = (p.nq + kRows - 1) / kRows, all = per_slice * p.share;
+    const int t0 = static_cast<int>(static_cast<int64_t>(all) * split / p.splits);
+    const int t1 = k_first < length ? static_cast<int>(static_cast<int64_t>(all) * (split + 1) / p.splits) : t0;
+    DenseLoad<T, D, kRows> ql, gl;
+    // the next tile of which a query sees a key of the block, from t on; its slice's first place
+    int begin = 0;
+    auto seek = [&](int t) {
+        for (; t < t1; ++t) {
+            const int slice = slice_k * p.share + t / per_slice, q0 = t % per_slice * kRows;
+            begin = p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first;
+            if (!p.causal || begin + min(q0 + kRows, p.nq) > k_first) break;
+        }
+        return t;
+    };
+    auto fetch = [&](int t) {
+        const int64_t row = (slice_k * static_cast<int64_t>(p.share) + t / per_slice) * p.nq + t % per_slice * kRows;
+        ql.load(p.Q, row, p.nq - t % per_slice * kRows);
+        gl.load(p.dO, row, p.nq - t % per_slice * kRows);
+    };
+    int t = seek(t0);
+    if (t < t1) fetch(t);
+    while (t < t1) {
+        const int slice = slice_k * p.share + t / per_slice, q0 = t % per_slice * kRows;
+        const int at0 = begin + q0;  // place of the tile's first query
+        ql.store(q_tile);
+        gl.store(g_tile);
+        bool apart = false;
+        if (threadIdx.x < kRows) {
+            const int q = q0 + static_cast<int>(threadIdx.x);
+            const float4 st = q < p.nq ? p.stats[static_cast<int64_t>(slice) * p.nq + q] : make_float4(INFINITY, 1.f, 0.f, 0.f);
+            s_lse[threadIdx.x] = st.x;
+            s_factor[threadIdx.x] = st.y;
+            s_mean[threadIdx.x] = st.z;
+            apart = st.y != 1.f;
+            if constexpr (BIAS) s_place[threadIdx.x] = BiasWindow<T>::place(p, begin + min(q, p.nq - 1));
+        }
+        BiasWindow<T> win{};
+        if constexpr (BIAS)
+            win.stage(p, slice % p.plane.rows, at0, begin + min(q0 + kRows, p.nq) - 1, k_first, min(k_first + kRowsBlock, p.nk) - 1,
+                      s_bias);
+        apart = __syncthreads_or(apart);
+        t = seek(t + 1);
+        if (t < t1) fetch(t);
+        // a query after which some key of the wave's comes
+        const bool masked = p.causal && at0 < k_first + wave * 32 + 31;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            f32x16_t s(0.f), g(0.f);
+#pragma unroll
+            for (int c = 0; c < R::kSteps; ++c) {
+                s = mma<T>(row_operand<T, D>(q_tile, 32 * u + tile_row<T>(m), h, c), kf[c], s);
+                g = mma<T>(row_operand<T, D>(g_tile, 32 * u + tile_row<T>(m), h, c), vf[c], g);
+            }
+            f32x16_t w;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int q = 32 * u + tile_slot<T>(i) + tile_half<T>() * h;
+                float x = s[i] * p.scale2;
+                if constexpr (BIAS) x = fmaf(s[i], p.scale2, s_bias[my_place - s_place[q] - win.base]);
+                if (masked) x = key <= at0 + q ? x : -INFINITY;
+                w[i] = __builtin_amdgcn_exp2f((seen ? x : -INFINITY) - s_lse[q]);
+                if (apart) w[i] *= s_factor[q];
+                s[i] = w[i] * (g[i] - s_mean[q]);
+            }
+#pragma unroll
+            for (int r = 0; r < R::kRowSteps; ++r) {
+                const uint4 a = as_operand<T>(w, r), c4 = as_operand<T>(s, r);
+#pragma unroll
+                for (int c = 0; c < R::kColumns; ++c) {
+                    dv[c] = mma<T>(column_operand<T, D>(g_tile, 32 * u, r, c), a, dv[c]);
+                    dk[c] = mma<T>(column_operand<T, D>(q_tile, 32 * u, r, c), c4, dk[c]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (key >= p.nk) return;
+    if (p.splits > 1) {
+        float* const to = p.part + (static_cast<int64_t>(split) * p.all_keys + k_row + key) * (2 * D);
+#pragma unroll
+        for (int c = 0; c < R::kColumns; ++c)
+#pragma unroll
+            for (int i = 0; i < (D < 32 ? 2 : 4); ++i) {
+                float* const at = to + 32 * c + 8 * i + 4 * h;
+                *reinterpret_cast<float4*>(at) = make_float4(dk[c][4 * i], dk[c][4 * i + 1], dk[c][4 * i + 2], dk[c][4 * i + 3]);
+                *reinterpret_cast<float4*>(at + D) = make_float4(dv[c][4 * i], dv[c][4 * i + 1], dv[c][4 * i + 2], dv[c][4 * i + 3]);
+            }
+        return;
+    }
+    T* const to_k = static_cast<T*>(p.dK) + (k_row + key) * D;
+    T* const to_v = static_cast<T*>(p.dV) + (k_row + key) * D;
+#pragma unroll
+    for (int c = 0; c < R::kColumns; ++c)
+#pragma unroll
+        for (int i = 0; i < (D < 32 ? 2 : 4); ++i) {
+            vec<T, 4> x, y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[j] = from_float<T>(dk[c][4 * i + j] * p.scale);
+                y[j] = from_float<T>(dv[c][4 * i + j]);
+            }
+            store_vec<T, 4>(to_k + 32 * c + 8 * i + 4 * h, x);
+            store_vec<T, 4>(to_v + 32 * c + 8 * i + 4 * h, y);
+        }
+}
+
+// Adds up the parts of the key side's splits: a thread takes four values of dK's or dV's row.
+template <typename T, int D>
+__global__ __launch_bounds__(kBlock) void dense_key_join_kernel(DenseBackward p)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x, row = i / (D / 2);
+    if (row >= p.all_keys) return;
+    const int c = static_cast<int>(i % (D / 2)) * 4;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < p.splits; ++s) {
+        const float4 y = *reinterpret_cast<const float4*>(p.part + (static_cast<int64_t>(s) * p.all_keys + row) * (2 * D) + c);
+        x[0] += y.x;
+        x[1] += y.y;
+        x[2] += y.z;
+        x[3] += y.w;
+    }
+    vec<T, 4> y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = from_float<T>(c < D ? x[j] * p.scale : x[j]);
+    store_vec<T, 4>((c < D ? static_cast<T*>(p.dK) + c : static_cast<T*>(p.dV) + c - D) + row * D, y);
+}
+
+// The offset side: one (dy, tiles of 32 columns apart) of a head.  A wave takes a quarter of the pairs of such tiles.
+template <typename T, int D>
+__global__ __launch_bounds__(kBlock) void dense_offset_kernel(DenseBackward p)
+{
+    using R = DenseRow<T, D>;
+    __shared__ float s_sum[32][33];
+    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
+    const int apart_all = 2 * p.x_tiles - 1, height = 2 * p.Hk - 1;
+    const int apart = static_cast<int>(b % static_cast<uint32_t>(apart_all)) - p.x_tiles + 1;
+    const int dy = static_cast<int>(b / static_cast<uint32_t>(apart_all) % static_cast<uint32_t>(height)) - p.Hk + 1;
+    const int head = static_cast<int>(b / static_cast<uint32_t>(apart_all) / static_cast<uint32_t>(height));
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int W = p.Wk, columns = p.x_tiles - abs(apart), column0 = apart < 0 ? -apart : 0;
+    const int rows = min(p.Hk, (p.nq - 1 + W - 1) / W + 1);  // most grid rows that a slice's queries touch
+    const int64_t pairs = static_cast<int64_t>(p.S / p.plane.rows) * rows * columns;
+    const T* const table = static_cast<const T*>(p.bias) + head * p.plane.size + (static_cast<int64_t>(dy) + p.Hk - 1) * p.plane.width + W - 1;
+    f32x16_t sum(0.f);
+    float bias[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int dx = 32 * apart + m - tile_slot<T>(i) - tile_half<T>() * h;
+        bias[i] = abs(dx) < W ? bias_base2(to_float(table[dx])) : 0.f;
+    }
+    for (int64_t i0 = wave; i0 < pairs; i0 += 4) {
+        const int column = static_cast<int>(i0 % columns) + column0;
+        const int slice = static_cast<int>(i0 / columns / rows) * p.plane.rows + head;
+        const int begin = p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first;
+        const int qy = begin / W + static_cast<int>(i0 / columns % rows), ky = qy + dy;
+        if (qy >= p.Hk || ky < 0 || ky >= p.Hk) continue;
+        const int slice_k = slice / p.share;
+        const int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
+        const int kx = 32 * (column + apart) + m, key = ky * W + kx;
+        const bool seen = kx < W && key < length;
+        // the left operand's query, and those of the result's registers
+        const int qx0 = 32 * column, q_mine = qy * W + qx0 + tile_row<T>(m) - begin;
+        const bool q_ok = qx0 + tile_row<T>(m) < W && q_mine >= 0 && q_mine < p.nq;
+        if (!__any(seen) || !__any(q_ok)) continue;
+        const int64_t q_row = static_cast<int64_t>(slice) * p.nq, k_row = static_cast<int64_t>(slice_k) * p.nk;
+        uint4 qf[R::kSteps], gf[R::kSteps], kf[R::kSteps], vf[R::kSteps];
+#pragma unroll
+        for (int c = 0; c < R::kSteps; ++c) qf[c] = gf[c] = kf[c] = vf[c] = make_uint4(0u, 0u, 0u, 0u);
+        if (q_ok) {
+            load_operand<T, D>(p.Q, q_row + q_mine, h, qf);
+            load_operand<T, D>(p.dO, q_row + q_mine, h, gf);
+        }
+        if (seen) {
+            load_operand<T, D>(p.K, k_row + key, h, kf);
+            load_operand<T, D>(p.V, k_row + key, h, vf);
+        }
+        f32x16_t s(0.f), g(0.f);
+#pragma unroll
+        for (int c = 0; c < R::kSteps; ++c) {
+            s = mma<T>(qf[c], kf[c], s);
+            g = mma<T>(gf[c], vf[c], g);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int qx = qx0 + tile_slot<T>(i) + tile_half<T>() * h, q = qy * W + qx - begin;
+            const bool on = qx < W && q >= 0 && q < p.nq && seen && (!p.causal || key <= q + begin);
+            const float4 st = on ? p.stats[q_row + q] : make_float4(INFINITY, 1.f, 0.f, 0.f);
+            const float x = on ? fmaf(s[i], p.scale2, bias[i]) : -INFINITY;
+            sum[i] = fmaf(__builtin_amdgcn_exp2f(x - st.x) * st.y, on ? g[i] - st.z : 0.f, sum[i]);
+        }
+    }
+    // the waves' sums one after another, then the diagonals
+    for (int k = 0; k < 4; ++k) {
+        if (wave == k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float& at = s_sum[tile_slot<T>(i) + tile_half<T>() * h][m];
+                at = k ? at + sum[i] : sum[i];
+            }
+        __syncthreads();
+    }
+    if (threadIdx.x < 63) {
+        const int t = static_cast<int>(threadIdx.x) - 31;  // column less row
+        float x = 0.f;
+        for (int r = max(0, -t); r < min(32, 32 - t); ++r) x += s_sum[r][r + t];
+        p.diagonals[static_cast<int64_t>(b) * 64 + threadIdx.x] = x;
+    }
+}
+
+// dbias of an offset: the diagonals of the (at most two) pairs of tiles that hold it.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void dense_offset_join_kernel(DenseBackward p)
+{
+    const int apart_all = 2 * p.x_tiles - 1;
+    const int64_t all = p.plane.rows * p.plane.size;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kBlock) {
+        const int64_t row = i / p.plane.width;  // of all heads' rows
+        const int dx = static_cast<int>(i % p.plane.width) - p.Wk + 1;
+        const int apart = dx >= 0 ? dx / 32 : -((31 - dx) / 32), t = dx - 32 * apart;  // 0 <= t < 32
+        const float* const from = p.diagonals + (row * apart_all + apart + p.x_tiles - 1) * 64;
+        float x = apart > -p.x_tiles ? from[31 + t] : 0.f;
+        if (t > 0 && apart + 1 < p.x_tiles) x += from[64 + t - 1];  // 31 + (t - 32)
+        static_cast<T*>(p.dbias)[i] = from_float<T>(x);
+    }
+}
+
+size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
+
+struct BackwardPlan {
+    DenseBackward p;
+    int64_t query_blocks, key_blocks, offset_blocks;
+    size_t stats, part, diagonals;  // bytes
+};
+
+BackwardPlan backward_plan(const DenseCall& c)
+{
+    BackwardPlan plan{};
+    DenseBackward& p = plan.p;
+    static_cast<DenseParams&>(p) = dense_params(c);
+    p.S = c.g.S;
+    p.Hk = c.g.Hk;
+    p.Wk = c.g.Wk;
+    p.key_slices = c.key_slices;
+    p.all_keys = int64_t(c.key_slices) * p.nk;
+    p.x_tiles = (c.g.Wk + 31) / 32;
+    plan.query_blocks = int64_t(p.groups) * ((p.rows + kRowsBlock - 1) / kRowsBlock);
+    const int64_t tiles = int64_t(c.key_slices) * ((p.nk + kRowsBlock - 1) / kRowsBlock);
+    // splits of the queries: fewer than two blocks per CU leave CUs idle, and a part is worth a block from four tiles on
+    const int64_t rows = int64_t(p.share) * ((p.nq + 63) / 64);
+    int64_t n = 512 / tiles;
+    if (n > rows / 4) n = rows / 4;
+    p.splits = n < 1 ? 1 : static_cast<int>(n);
+    plan.key_blocks = tiles * p.splits;
+    plan.stats = round256(size_t(c.g.S) * p.nq * sizeof(float4));
+    plan.part = p.splits > 1 ? round256(size_t(p.splits) * p.all_keys * 2 * c.g.d * sizeof(float)) : 0;
+    if (c.bias) {
+        plan.offset_blocks = int64_t(c.bias_rows) * (2 * int64_t(c.g.Hk) - 1) * (2 * p.x_tiles - 1);
+        plan.diagonals = round256(size_t(plan.offset_blocks) * 64 * sizeof(float));
+    }
+    return plan;
+}
+
+}  // namespace
+
+size_t dense_backward_workspace_bytes(const DenseCall& c)
+{
+    const BackwardPlan plan = backward_plan(c);
+    return plan.stats + plan.part + plan.diagonals;
+}
+
+uint64_t dense_backward_blocks(const DenseCall& c)
+{
+    const BackwardPlan plan = backward_plan(c);
+    uint64_t most = plan.query_blocks;
+    if (uint64_t(plan.key_blocks) > most) most = plan.key_blocks;
+    return uint64_t(plan.offset_blocks) > most ? plan.offset_blocks : most;
+}
+
+hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, void* dQ, void* dK, void* dV, void* dbias,
+                                 void* workspace, hipStream_t stream, hipEvent_t start, hipEvent_t stop)
+{
+    const BackwardPlan plan = backward_plan(c);
+    DenseBackward p = plan.p;
+    p.dO = dO;
+    p.dQ = dQ;
+    p.dK = dK;
+    p.dV = dV;
+    p.dbias = dbias;
+    unsigned char* const ws = static_cast<unsigned char*>(workspace);
+    p.stats = reinterpret_cast<float4*>(ws);
+    p.part = reinterpret_cast<float*>(ws + plan.stats);
+    p.diagonals = reinterpret_cast<float*>(ws + plan.stats + plan.part);
+    const int window = c.bias ? static_cast<int>(dense_bias_window(c.g.Hk, c.g.Wk)) : 0;
+    return dispatch_value(dtype, c.g.d, hipErrorInvalidValue, [&](auto type, auto width) {
+        using T = std::conditional_t<std::is_same<decltype(type), float>::value, float, uint16_t>;
+        constexpr int D = decltype(width)::value;
+        const size_t lds = backward_lds<T, D>() + (c.bias ? (kStaged<T, D> + window) * sizeof(float) : 0);
+        DenseBackward a = p;
+        a.tiles = static_cast<int>(plan.query_blocks / p.groups);
+        hipError_t e = c.bias ? launch_dense_kernel(dense_query_kernel<T, D, true>, plan.query_blocks, lds, stream, start, nullptr, a)
+                              : launch_dense_kernel(dense_query_kernel<T, D, false>, plan.query_blocks, lds, stream, start, nullptr, a);
+        if (e != hipSuccess) return e;
+        a.tiles = (p.nk + kRowsBlock - 1) / kRowsBlock;
+        hipEvent_t end = p.splits == 1 && !dbias ? stop : nullptr;
+        e = c.bias ? launch_dense_kernel(dense_key_kernel<T, D, true>, plan.key_blocks, lds, stream, nullptr, end, a)
+                   : launch_dense_kernel(dense_key_kernel<T, D, false>, plan.key_blocks, lds, stream, nullptr, end, a);
+        if (e != hipSuccess) return e;
+        if (p.splits > 1) {
+            e = launch_dense_kernel(dense_key_join_kernel<T, D>, (p.all_keys * (D / 2) + kBlock - 1) / kBlock, 0, stream, nullptr,
+                                    dbias ? nullptr : stop, a);
+            if (e != hipSuccess) return e;
+        }
+        if (!dbias) return hipSuccess;
+        e = launch_dense_kernel(dense_offset_kernel<T, D>, plan.offset_blocks, 0, stream, nullptr, nullptr, a);
+        if (e != hipSuccess) return e;
+        const int64_t blocks = (p.plane.rows * p.plane.size + kBlock - 1) / kBlock;
+        return launch_dense_kernel(dense_offset_join_kernel<T>, blocks < 8192 ? blocks : 8192, 0, stream, nullptr, stop, a);
+    });
+}
+
+}  // namespace scram

@@ -1,7 +1,8 @@
 // Internal interface between the C-ABI front end (scram_api.cpp) and the
 // kernels (scram_pm.hip, scram_attend.hip, scram_backward.hip,
-// scram_snis.hip, scram_diff.hip, scram_diff_backward.hip, scram_rotary.hip,
-// scram_norm.hip).  Arguments reaching these functions have been
+// scram_snis.hip, scram_diff.hip, scram_diff_backward.hip, scram_dense.hip,
+// scram_dense_backward.hip, scram_bias.hip, scram_rotary.hip, scram_norm.hip,
+// scram_group.hip).  Arguments reaching these functions have been
 // validated by the front end.
 #pragma once
 
@@ -83,6 +84,54 @@ hipError_t launch_diff_attend(int dtype, const DiffCall& c, void* out, hipStream
 size_t diff_backward_workspace_bytes(const Grid& g, int kappa);
 hipError_t launch_diff_backward(int dtype, const DiffCall& c, const void* dO, float* dQ, float* dK, float* dV, float* dlam,
                                 void* workspace, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
+
+// Attention over every key and its gradients (scram_dense_attend).
+struct DenseCall {
+    const void *Q, *K, *V;
+    const void* bias;        // [bias_rows, 2 Hk - 1, 2 Wk - 1] (null: none)
+    int bias_rows;
+    const int32_t* lengths;  // device [key_slices] (null: all keys)
+    Grid g;
+    int key_slices;
+    float scale;
+    bool causal;
+    int first;               // causal or with a bias: raster index of a slice's first query among its keys
+    const int32_t* origin;   // the same per slice, on the device (null: first)
+};
+constexpr int kBiasWindowMost = 12288;  // most places of a bias' plane that a block holds at once
+int64_t dense_bias_window(int Hk, int Wk);
+size_t dense_workspace_bytes(const DenseCall& c);
+uint64_t dense_blocks(const DenseCall& c);
+hipError_t launch_dense(int dtype, const DenseCall& c, void* out, void* workspace, hipStream_t stream, hipEvent_t start,
+                        hipEvent_t stop);
+size_t dense_backward_workspace_bytes(const DenseCall& c);
+uint64_t dense_backward_blocks(const DenseCall& c);
+hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, void* dQ, void* dK, void* dV, void* dbias,
+                                 void* workspace, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
+
+// The bias of every offset from a table by buckets of distance (scram_relative_bias).
+struct BiasCall {
+    int dtype, heads, H, W;
+    int edges[2];            // of the height and the width
+    const int* edge[2];      // on the host
+};
+hipError_t launch_relative_bias(const BiasCall& c, const void* table, void* bias, hipStream_t stream);
+size_t relative_bias_backward_workspace_bytes(const BiasCall& c);
+hipError_t launch_relative_bias_backward(const BiasCall& c, const void* dbias, void* dtable, void* workspace, hipStream_t stream);
+
+// Group norm of images, channels last, with an activation (scram_group_norm).
+struct GroupCall {
+    int64_t images, pixels;
+    int channels, groups;
+    int dtype, grad_dtype, weight_dtype, activation;
+    const void *X, *weight, *bias, *dY;  // weight, bias nullable
+    float eps;
+};
+size_t group_norm_workspace_bytes(const GroupCall& c);
+hipError_t launch_group_norm(const GroupCall& c, void* Y, float* mean, float* rstd, void* workspace, hipStream_t stream);
+size_t group_norm_backward_workspace_bytes(const GroupCall& c);
+hipError_t launch_group_norm_backward(const GroupCall& c, const float* mean, const float* rstd, void* dX, float* dweight,
+                                      float* dbias, void* workspace, hipStream_t stream);
 
 // Rotation of channel pairs by the position's angles (scram_rotary).
 struct RotaryCall {

@@ -1,4 +1,4 @@
-"""Operators on channel rows around the attention: rotary grid positions and layer norm, with their gradients.
+"""Operators on channel rows around the attention: rotary grid positions, layer norm and group norm, with their gradients.
 
 Argument marshalling only, as in :mod:`.binding`; rows of any width, no padding.
 """
@@ -191,3 +191,99 @@ def layer_norm_backward(dY, X, mean, rstd, weight=None, *, out=None, workspace=N
 def layer_norm_backward_workspace_bytes(rows: int, channels: int) -> int:
     """Bytes of device workspace ``layer_norm_backward`` needs."""
     return int(_b.lib().scram_layer_norm_backward_workspace_bytes(rows, channels))
+
+
+ACTIVATIONS = {None: 0, "silu": 1}
+
+
+def _group(X, groups, weight, bias, activation, out):
+    """Checks of a group norm's tensors: (images, pixels, channels, groups, dtype code, weights' dtype code, activation,
+    device index)."""
+    if X.dim() < 2:
+        raise ValueError(f"X must be [images, ..., channels], got {tuple(X.shape)}")
+    _, C, code, wcode, index = _norm_rows(X, weight, bias, out)
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {tuple(ACTIVATIONS)}, got {activation!r}")
+    groups = int(groups)
+    if groups < 1 or C % groups:
+        raise ValueError(f"{C} channels do not split into {groups} groups")
+    N = X.shape[0]
+    return N, X.numel() // (N * C) if N * C else 0, C, groups, code, wcode, ACTIVATIONS[activation], index
+
+
+def group_norm(X, groups: int, weight=None, bias=None, eps: float = 1e-5, *, activation=None, out=None, stats: bool = False,
+               workspace=None):
+    """Group norm of images, channels last, and an activation (``scram_group_norm``).
+
+    ``X`` ``[images, ..., channels]``, normalised over an image's pixels and each of ``groups`` groups of neighbouring
+    channels; ``weight``, ``bias``: [channels] in X's dtype or float32, or None; ``activation``: None or "silu".  Returns
+    the result in X's dtype, with ``stats`` ``(result, mean, rstd)``: fp32 ``[images, groups]``, for
+    :func:`group_norm_backward`.  ``out`` may be ``X``.
+    ``workspace``: optional uint8 device tensor of at least ``group_norm_workspace_bytes(...)`` bytes.
+    """
+    torch = _b._torch()
+    N, pixels, C, groups, code, wcode, act, index = _group(X, groups, weight, bias, activation, out)
+    dev = X.device
+    if out is None:
+        out = torch.empty_like(X)
+    else:
+        _b._plain("out", out, X.dim(), X.dtype, index)
+    mean = rstd = None
+    if stats:
+        mean = torch.empty((N, groups), dtype=torch.float32, device=dev)
+        rstd = torch.empty_like(mean)
+    if workspace is None:
+        workspace = torch.empty(max(group_norm_workspace_bytes(N, pixels, C, groups, dtype=X.dtype), 1), dtype=torch.uint8, device=dev)
+    else:
+        _b._workspace(workspace, 0, dev)
+    _b._call(_b.lib().scram_group_norm, "scram_group_norm", dev,
+             (X.data_ptr(), code, _b._ptr(weight), _b._ptr(bias), wcode, N, pixels, C, groups, float(eps), act, out.data_ptr(),
+              _b._ptr(mean), _b._ptr(rstd), workspace.data_ptr(), workspace.numel() * workspace.element_size()))
+    return (out, mean, rstd) if stats else out
+
+
+def group_norm_backward(dY, X, mean, rstd, weight=None, bias=None, *, activation=None, out=None, workspace=None):
+    """Gradients of :func:`group_norm` (``scram_group_norm_backward``): ``(dX, dweight, dbias)``.
+
+    ``dY`` is in X's dtype or float32 and dX in dY's (``out`` may be ``dY``); dweight and dbias are fp32 [channels], also
+    where the call had no weights.  ``mean``, ``rstd`` ``[images, groups]``: what the call gave with ``stats``.
+    ``workspace``: optional uint8 device tensor of at least ``group_norm_backward_workspace_bytes(...)`` bytes.
+    """
+    torch = _b._torch()
+    index = X.get_device()
+    _b._plain("mean", mean, 2, torch.float32, index)
+    N, pixels, C, groups, code, wcode, act, index = _group(X, mean.shape[1], weight, bias, activation, out)
+    kind, gkind, dev = X.dtype, dY.dtype, X.device
+    if gkind != kind and gkind != torch.float32:
+        raise TypeError("dY must be float32 or of X's dtype")
+    if _b._plain("dY", dY, X.dim(), gkind, index).shape != X.shape:
+        raise ValueError(f"dY must be {tuple(X.shape)}, got {tuple(dY.shape)}")
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if _b._plain(name, t, 2, torch.float32, index).shape != (N, groups):
+            raise ValueError(f"{name} must be {(N, groups)}, got {tuple(t.shape)}")
+    if out is None:
+        out = torch.empty_like(dY)
+    else:
+        _b._plain("out", out, X.dim(), gkind, index)
+    dweight = torch.empty(C, dtype=torch.float32, device=dev)
+    dbias = torch.empty_like(dweight)
+    if workspace is None:
+        workspace = torch.empty(max(group_norm_backward_workspace_bytes(N, pixels, C, groups, dtype=kind), 1), dtype=torch.uint8,
+                                device=dev)
+    else:
+        _b._workspace(workspace, 0, dev)
+    _b._call(_b.lib().scram_group_norm_backward, "scram_group_norm_backward", dev,
+             (dY.data_ptr(), _b._dtype_code_of(gkind), X.data_ptr(), code, mean.data_ptr(), rstd.data_ptr(), _b._ptr(weight),
+              _b._ptr(bias), wcode, N, pixels, C, groups, act, out.data_ptr(), dweight.data_ptr(), dbias.data_ptr(),
+              workspace.data_ptr(), workspace.numel() * workspace.element_size()))
+    return out, dweight, dbias
+
+
+def group_norm_workspace_bytes(images: int, pixels: int, channels: int, groups: int, *, dtype) -> int:
+    """Bytes of device workspace ``group_norm`` needs (``dtype``: torch dtype of X)."""
+    return int(_b.lib().scram_group_norm_workspace_bytes(images, pixels, channels, groups, _b._dtype_code_of(dtype)))
+
+
+def group_norm_backward_workspace_bytes(images: int, pixels: int, channels: int, groups: int, *, dtype) -> int:
+    """Bytes of device workspace ``group_norm_backward`` needs (``dtype``: torch dtype of X)."""
+    return int(_b.lib().scram_group_norm_backward_workspace_bytes(images, pixels, channels, groups, _b._dtype_code_of(dtype)))
