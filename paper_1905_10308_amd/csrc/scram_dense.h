@@ -66,6 +66,9 @@ struct DenseRow {
     static constexpr int kSlack = 64 * static_cast<int>(sizeof(T));  // bytes that transposed reads may pass the last row by
 };
 
+// The wave's place in its block, as a number that the compiler knows to be the same for all lanes.
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6); }
+
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
     typedef float f32x2_t __attribute__((ext_vector_type(2)));

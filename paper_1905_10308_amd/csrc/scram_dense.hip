@@ -51,7 +51,7 @@ __global__ __launch_bounds__(kBlock) void dense_kernel(DenseForward p)
     const int split = static_cast<int>(b % static_cast<uint32_t>(p.splits));
     const int tile = static_cast<int>(b / static_cast<uint32_t>(p.splits) % static_cast<uint32_t>(p.tiles));
     const int group = static_cast<int>(b / static_cast<uint32_t>(p.splits) / static_cast<uint32_t>(p.tiles));
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_index(), m = lane & 31, h = lane >> 5;
     const int slice_k = p.per_group == 1 ? group / p.share : group;
     const int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
 
@@ -120,7 +120,6 @@ __global__ __launch_bounds__(kBlock) void dense_kernel(DenseForward p)
                 s[u] = mma<T>(row_operand<T, D>(k_tile, 32 * u + tile_row<T>(m), h, c), qf[c], s[u]);
         }
         float most = -INFINITY;
-        const bool whole = __all(end >= k0 + kKeys);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -128,10 +127,18 @@ __global__ __launch_bounds__(kBlock) void dense_kernel(DenseForward p)
                 const int key = 32 * u + tile_slot<T>(i) + tile_half<T>() * h;
                 float x = s[u][i] * p.scale2;
                 if constexpr (BIAS) x = fmaf(s[u][i], p.scale2, s_bias[s_place[key] - my_place - win.base]);
-                if (!whole) x = k0 + key < end ? x : -INFINITY;
                 s[u][i] = x;
-                most = fmaxf(most, x);
             }
+        if (!__all(end >= k0 + kKeys))
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[u][i] = k0 + 32 * u + tile_slot<T>(i) + tile_half<T>() * h < end ? s[u][i] : -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, s[u][i]);
         most = fmaxf(most, __shfl_xor(most, 32));
         const float next = fmaxf(top, most);
         const float shift = next == -INFINITY ? 0.f : next;  // no key yet: every weight is 0

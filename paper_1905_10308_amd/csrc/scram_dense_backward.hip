@@ -36,6 +36,7 @@ struct DenseBackward : DenseParams {
     int tiles;         // of a group's queries, or of a slice's keys
     int splits;        // key side: runs of query tiles
     int x_tiles, Hk, Wk, key_slices, S;
+    int cuts;          // of a column's grid rows among waves
 };
 
 // A row's softmax for the other kernels: weights are exp2(x - x0) f for scores x in base 2, x0 the logarithm of their sum and
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(kBlock) void dense_query_kernel(DenseBackward p)
     const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
     const int tile = static_cast<int>(b % static_cast<uint32_t>(p.tiles));
     const int group = static_cast<int>(b / static_cast<uint32_t>(p.tiles));
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_index(), m = lane & 31, h = lane >> 5;
     const int slice_k = p.per_group == 1 ? group / p.share : group;
     const int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
     const int row = tile * kRowsBlock + wave * 32 + m;
@@ -133,7 +134,6 @@ __global__ __launch_bounds__(kBlock) void dense_query_kernel(DenseBackward p)
                 g[u] = mma<T>(row_operand<T, D>(v_tile, 32 * u + tile_row<T>(m), h, c), gf[c], g[u]);
             }
         }
-        const bool whole = __all(end >= k0 + kKeys);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -141,9 +141,14 @@ __global__ __launch_bounds__(kBlock) void dense_query_kernel(DenseBackward p)
                 const int key = 32 * u + tile_slot<T>(i) + tile_half<T>() * h;
                 float x = s[u][i] * p.scale2;
                 if constexpr (BIAS) x = fmaf(s[u][i], p.scale2, s_bias[s_place[key] - my_place - win.base]);
-                if (!whole) x = k0 + key < end ? x : -INFINITY;
                 s[u][i] = x;
             }
+        if (__all(end >= k0 + kKeys)) return;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                s[u][i] = k0 + 32 * u + tile_slot<T>(i) + tile_half<T>() * h < end ? s[u][i] : -INFINITY;
     };
 
     float top = -INFINITY, sum = 0.f, dsum = 0.f;
@@ -231,7 +236,7 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
     const int split = static_cast<int>(b % static_cast<uint32_t>(p.splits));
     const int tile = static_cast<int>(b / static_cast<uint32_t>(p.splits) % static_cast<uint32_t>(p.tiles));
     const int slice_k = static_cast<int>(b / static_cast<uint32_t>(p.splits) / static_cast<uint32_t>(p.tiles));
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_index(), m = lane & 31, h = lane >> 5;
     // the keys that count and that some query sees: no others are read
     int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
     if (p.causal) {
@@ -303,8 +308,8 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
         apart = __syncthreads_or(apart);
         t = seek(t + 1);
         if (t < t1) fetch(t);
-        // a query after which some key of the wave's comes
-        const bool masked = p.causal && at0 < k_first + wave * 32 + 31;
+        // a query after which some key of the wave's comes, or a key that is not seen
+        const bool masked = (p.causal && at0 < k_first + wave * 32 + 31) || k_first + wave * 32 + 32 > length;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             f32x16_t s(0.f), g(0.f);
@@ -313,17 +318,27 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
                 s = mma<T>(row_operand<T, D>(q_tile, 32 * u + tile_row<T>(m), h, c), kf[c], s);
                 g = mma<T>(row_operand<T, D>(g_tile, 32 * u + tile_row<T>(m), h, c), vf[c], g);
             }
-            f32x16_t w;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int q = 32 * u + tile_slot<T>(i) + tile_half<T>() * h;
                 float x = s[i] * p.scale2;
                 if constexpr (BIAS) x = fmaf(s[i], p.scale2, s_bias[my_place - s_place[q] - win.base]);
-                if (masked) x = key <= at0 + q ? x : -INFINITY;
-                w[i] = __builtin_amdgcn_exp2f((seen ? x : -INFINITY) - s_lse[q]);
-                if (apart) w[i] *= s_factor[q];
-                s[i] = w[i] * (g[i] - s_mean[q]);
+                s[i] = x;
             }
+            if (masked)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int q = 32 * u + tile_slot<T>(i) + tile_half<T>() * h;
+                    s[i] = seen && (!p.causal || key <= at0 + q) ? s[i] : -INFINITY;
+                }
+            f32x16_t w;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(s[i] - s_lse[32 * u + tile_slot<T>(i) + tile_half<T>() * h]);
+            if (apart)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] *= s_factor[32 * u + tile_slot<T>(i) + tile_half<T>() * h];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = w[i] * (g[i] - s_mean[32 * u + tile_slot<T>(i) + tile_half<T>() * h]);
 #pragma unroll
             for (int r = 0; r < R::kRowSteps; ++r) {
                 const uint4 a = as_operand<T>(w, r), c4 = as_operand<T>(s, r);
@@ -387,85 +402,178 @@ __global__ __launch_bounds__(kBlock) void dense_key_join_kernel(DenseBackward p)
     store_vec<T, 4>((c < D ? static_cast<T*>(p.dK) + c : static_cast<T*>(p.dV) + c - D) + row * D, y);
 }
 
-// The offset side: one (dy, tiles of 32 columns apart) of a head.  A wave takes a quarter of the pairs of such tiles.
+// Rows of offsets that a block of the offset side takes: with two, a tile of keys that a step has met is the other row's at
+// the next step, and stays in registers.
 template <typename T, int D>
-__global__ __launch_bounds__(kBlock) void dense_offset_kernel(DenseBackward p)
+constexpr int kOffsetRows = D * sizeof(T) > 256 ? 1 : 2;
+
+// 32 rows on their way through a wave's own part of LDS: read from memory as they lie there, a row by neighbouring lanes, and
+// from LDS as operands, a row by a lane (operands straight from memory touch 32 lines an instruction: 289 us where this takes
+// ROWS_US, 16 slices of 64 x 64, 64 channels).
+template <typename T, int D>
+struct WaveTile {
+    using R = DenseRow<T, D>;
+    static constexpr int kEach = R::kChunks / 2;
+    static constexpr int kBytes = 32 * R::kStride;
+    uint4 x[kEach];
+
+    // rows first .. last - 1 of the tile that begins at `row0`; the others are zeros
+    __device__ __forceinline__ void load(const void* rows, int64_t row0, int first, int last)
+    {
+        const unsigned char* const from = static_cast<const unsigned char*>(rows) + row0 * R::kBytes;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int c = i * 64 + static_cast<int>(threadIdx.x & 63), r = c / R::kChunks;
+            x[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (r >= first && r < last) x[i] = *reinterpret_cast<const uint4*>(from + 16 * c);
+        }
+    }
+    // the operands of row `row` for this lane
+    __device__ __forceinline__ void turn(unsigned char* tile, int row, uint4 (&y)[R::kSteps]) const
+    {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int c = i * 64 + static_cast<int>(threadIdx.x & 63);
+            *reinterpret_cast<uint4*>(tile + c / R::kChunks * R::kStride + 16 * (c % R::kChunks)) = x[i];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int s = 0; s < R::kSteps; ++s) y[s] = row_operand<T, D>(tile, row, (threadIdx.x & 63) >> 5, s);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+};
+
+// The offset side: offsets dy0 .. of rows, and tiles of 32 columns `apart`, of one head.  A wave goes down the grid rows of a
+// column of tiles (of every fourth column and slice); a tile's scores are formed transposed, so that a query's statistics are
+// its lane's, and what a pair of tiles leaves is added up in registers by the place in the tile.
+template <typename T, int D>
+__global__ __launch_bounds__(kBlock, 2) void dense_offset_kernel(DenseBackward p)
 {
     using R = DenseRow<T, D>;
+    constexpr int N = kOffsetRows<T, D>;
     __shared__ float s_sum[32][33];
+    __shared__ __align__(16) float s_bias[N][4][64][4];  // by register and lane
+    __shared__ __align__(16) unsigned char s_turn[4][WaveTile<T, D>::kBytes];
     const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
-    const int apart_all = 2 * p.x_tiles - 1, height = 2 * p.Hk - 1;
+    const int apart_all = 2 * p.x_tiles - 1, height = 2 * p.Hk - 1, groups = (height + N - 1) / N;
     const int apart = static_cast<int>(b % static_cast<uint32_t>(apart_all)) - p.x_tiles + 1;
-    const int dy = static_cast<int>(b / static_cast<uint32_t>(apart_all) % static_cast<uint32_t>(height)) - p.Hk + 1;
-    const int head = static_cast<int>(b / static_cast<uint32_t>(apart_all) / static_cast<uint32_t>(height));
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int dy0 = static_cast<int>(b / static_cast<uint32_t>(apart_all) % static_cast<uint32_t>(groups)) * N - p.Hk + 1;
+    const int head = static_cast<int>(b / static_cast<uint32_t>(apart_all) / static_cast<uint32_t>(groups));
+    const int lane = threadIdx.x & 63, wave = wave_index(), m = lane & 31, h = lane >> 5;
     const int W = p.Wk, columns = p.x_tiles - abs(apart), column0 = apart < 0 ? -apart : 0;
-    const int rows = min(p.Hk, (p.nq - 1 + W - 1) / W + 1);  // most grid rows that a slice's queries touch
-    const int64_t pairs = static_cast<int64_t>(p.S / p.plane.rows) * rows * columns;
-    const T* const table = static_cast<const T*>(p.bias) + head * p.plane.size + (static_cast<int64_t>(dy) + p.Hk - 1) * p.plane.width + W - 1;
-    f32x16_t sum(0.f);
-    float bias[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int dx = 32 * apart + m - tile_slot<T>(i) - tile_half<T>() * h;
-        bias[i] = abs(dx) < W ? bias_base2(to_float(table[dx])) : 0.f;
+    for (int i = threadIdx.x; i < N * 1024; i += kBlock) {
+        const int e = i & 3, l = (i >> 2) & 63, r = 4 * ((i >> 8) & 3) + e, j = i >> 10;
+        const int dx = 32 * apart + tile_slot<T>(r) + tile_half<T>() * (l >> 5) - (l & 31), dy = dy0 + j;
+        const T* const table = static_cast<const T*>(p.bias) + head * p.plane.size;
+        s_bias[j][(i >> 8) & 3][l][e] =
+            abs(dx) < W && dy < p.Hk
+                ? bias_base2(to_float(table[(static_cast<int64_t>(dy) + p.Hk - 1) * p.plane.width + W - 1 + dx])) : 0.f;
     }
-    for (int64_t i0 = wave; i0 < pairs; i0 += 4) {
-        const int column = static_cast<int>(i0 % columns) + column0;
-        const int slice = static_cast<int>(i0 / columns / rows) * p.plane.rows + head;
+    __syncthreads();
+    f32x16_t sum[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum[j] = f32x16_t(0.f);
+    const int64_t strips = static_cast<int64_t>(p.S / p.plane.rows) * columns * p.cuts;
+    for (int64_t strip = wave; strip < strips; strip += 4) {
+        const int cut = static_cast<int>(strip % p.cuts), column = static_cast<int>(strip / p.cuts % columns) + column0;
+        const int slice = static_cast<int>(strip / p.cuts / columns) * p.plane.rows + head, slice_k = slice / p.share;
         const int begin = p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first;
-        const int qy = begin / W + static_cast<int>(i0 / columns % rows), ky = qy + dy;
-        if (qy >= p.Hk || ky < 0 || ky >= p.Hk) continue;
-        const int slice_k = slice / p.share;
         const int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
-        const int kx = 32 * (column + apart) + m, key = ky * W + kx;
-        const bool seen = kx < W && key < length;
-        // the left operand's query, and those of the result's registers
-        const int qx0 = 32 * column, q_mine = qy * W + qx0 + tile_row<T>(m) - begin;
-        const bool q_ok = qx0 + tile_row<T>(m) < W && q_mine >= 0 && q_mine < p.nq;
-        if (!__any(seen) || !__any(q_ok)) continue;
         const int64_t q_row = static_cast<int64_t>(slice) * p.nq, k_row = static_cast<int64_t>(slice_k) * p.nk;
-        uint4 qf[R::kSteps], gf[R::kSteps], kf[R::kSteps], vf[R::kSteps];
+        const int qx0 = 32 * column, qx = qx0 + m, kx0 = 32 * (column + apart);
+        const bool x_whole = qx0 + 32 <= W && kx0 + 32 <= W;
+        uint4 kf[N][R::kSteps], vf[N][R::kSteps];
+        auto keys = [&](int ky, uint4 (&k)[R::kSteps], uint4 (&v)[R::kSteps]) {
+            const int key = ky * W + kx0;
+            const int last = ky >= 0 && ky < p.Hk ? min(min(32, W - kx0), length - key) : 0;
+            WaveTile<T, D> kl, vl;
+            kl.load(p.K, k_row + key, 0, last);
+            vl.load(p.V, k_row + key, 0, last);
+            kl.turn(s_turn[wave], tile_row<T>(m), k);
+            vl.turn(s_turn[wave], tile_row<T>(m), v);
+        };
+        const int low = max(begin / W, -(dy0 + N - 1)), high = min((begin + p.nq - 1) / W, p.Hk - 1 - dy0);
+        const int from = low + (high - low + 1) * cut / p.cuts, to = low + (high - low + 1) * (cut + 1) / p.cuts - 1;
+        // grid row qy of the queries against rows qy + dy0 + j; those of j are in place (at + j) % N
+        auto step = [&](int qy, auto at) {
+            constexpr int kAt = decltype(at)::value;
+            const int q = qy * W + qx - begin;
+            const bool q_ok = qx < W && q >= 0 && q < p.nq;
+            const float4 st = q_ok ? p.stats[q_row + q] : make_float4(INFINITY, 1.f, 0.f, 0.f);
+            uint4 qf[R::kSteps], gf[R::kSteps];
+            {
+                const int q0 = qy * W + qx0 - begin;
+                WaveTile<T, D> ql, gl;
+                ql.load(p.Q, q_row + q0, -q0, min(min(32, W - qx0), p.nq - q0));
+                gl.load(p.dO, q_row + q0, -q0, min(min(32, W - qx0), p.nq - q0));
+                ql.turn(s_turn[wave], m, qf);
+                gl.turn(s_turn[wave], m, gf);
+            }
+            keys(qy + dy0 + N - 1, kf[(kAt + N - 1) % N], vf[(kAt + N - 1) % N]);
 #pragma unroll
-        for (int c = 0; c < R::kSteps; ++c) qf[c] = gf[c] = kf[c] = vf[c] = make_uint4(0u, 0u, 0u, 0u);
-        if (q_ok) {
-            load_operand<T, D>(p.Q, q_row + q_mine, h, qf);
-            load_operand<T, D>(p.dO, q_row + q_mine, h, gf);
-        }
-        if (seen) {
-            load_operand<T, D>(p.K, k_row + key, h, kf);
-            load_operand<T, D>(p.V, k_row + key, h, vf);
-        }
-        f32x16_t s(0.f), g(0.f);
+            for (int j = 0; j < N; ++j) {
+                const int ky = qy + dy0 + j, dy = dy0 + j;
+                if (ky < 0 || ky >= p.Hk || ky * W + kx0 >= length) continue;
+                if (p.causal && (dy > 0 || (dy == 0 && apart > 0))) continue;
+                f32x16_t s(0.f), g(0.f);
 #pragma unroll
-        for (int c = 0; c < R::kSteps; ++c) {
-            s = mma<T>(qf[c], kf[c], s);
-            g = mma<T>(gf[c], vf[c], g);
-        }
+                for (int c = 0; c < R::kSteps; ++c) {
+                    s = mma<T>(kf[(kAt + j) % N][c], qf[c], s);
+                    g = mma<T>(vf[(kAt + j) % N][c], gf[c], g);
+                }
+                const bool whole = x_whole && ky * W + kx0 + 32 <= length && !(p.causal && dy == 0 && apart == 0) && __all(q_ok);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int qx = qx0 + tile_slot<T>(i) + tile_half<T>() * h, q = qy * W + qx - begin;
-            const bool on = qx < W && q >= 0 && q < p.nq && seen && (!p.causal || key <= q + begin);
-            const float4 st = on ? p.stats[q_row + q] : make_float4(INFINITY, 1.f, 0.f, 0.f);
-            const float x = on ? fmaf(s[i], p.scale2, bias[i]) : -INFINITY;
-            sum[i] = fmaf(__builtin_amdgcn_exp2f(x - st.x) * st.y, on ? g[i] - st.z : 0.f, sum[i]);
+                for (int r = 0; r < 4; ++r) {
+                    const float4 bias = *reinterpret_cast<const float4*>(s_bias[j][r][lane]);
+                    s[4 * r] = fmaf(s[4 * r], p.scale2, bias.x);
+                    s[4 * r + 1] = fmaf(s[4 * r + 1], p.scale2, bias.y);
+                    s[4 * r + 2] = fmaf(s[4 * r + 2], p.scale2, bias.z);
+                    s[4 * r + 3] = fmaf(s[4 * r + 3], p.scale2, bias.w);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) g[i] -= st.z;
+                if (!whole)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int x1 = kx0 + tile_slot<T>(i) + tile_half<T>() * h, key = ky * W + x1;
+                        const bool on = q_ok && x1 < W && key < length && (!p.causal || key <= q + begin);
+                        s[i] = on ? s[i] : -INFINITY;
+                        g[i] = on ? g[i] : 0.f;
+                    }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[j][i] = fmaf(__builtin_amdgcn_exp2f(s[i] - st.x) * st.y, g[i], sum[j][i]);
+            }
+        };
+        if (low > high || from > to) continue;
+#pragma unroll
+        for (int j = 0; j < N - 1; ++j) keys(from + dy0 + j, kf[j], vf[j]);
+        for (int qy = from; qy <= to; qy += N) {
+            step(qy, std::integral_constant<int, 0>{});
+            if (N > 1 && qy + 1 <= to) step(qy + 1, std::integral_constant<int, N - 1>{});
         }
     }
     // the waves' sums one after another, then the diagonals
-    for (int k = 0; k < 4; ++k) {
-        if (wave == k)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float& at = s_sum[tile_slot<T>(i) + tile_half<T>() * h][m];
-                at = k ? at + sum[i] : sum[i];
-            }
+    for (int j = 0; j < N; ++j) {
+        for (int k = 0; k < 4; ++k) {
+            if (wave == k)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float& at = s_sum[m][tile_slot<T>(i) + tile_half<T>() * h];
+                    at = k ? at + sum[j][i] : sum[j][i];
+                }
+            __syncthreads();
+        }
+        if (threadIdx.x < 63 && dy0 + j < p.Hk) {
+            const int t = static_cast<int>(threadIdx.x) - 31;  // the key's column less the query's
+            float x = 0.f;
+            for (int r = max(0, -t); r < min(32, 32 - t); ++r) x += s_sum[r][r + t];
+            const int64_t row = static_cast<int64_t>(head) * height + dy0 + j + p.Hk - 1;
+            p.diagonals[(row * apart_all + apart + p.x_tiles - 1) * 64 + threadIdx.x] = x;
+        }
         __syncthreads();
-    }
-    if (threadIdx.x < 63) {
-        const int t = static_cast<int>(threadIdx.x) - 31;  // column less row
-        float x = 0.f;
-        for (int r = max(0, -t); r < min(32, 32 - t); ++r) x += s_sum[r][r + t];
-        p.diagonals[static_cast<int64_t>(b) * 64 + threadIdx.x] = x;
     }
 }
 
@@ -516,7 +624,10 @@ BackwardPlan backward_plan(const DenseCall& c)
     plan.stats = round256(size_t(c.g.S) * p.nq * sizeof(float4));
     plan.part = p.splits > 1 ? round256(size_t(p.splits) * p.all_keys * 2 * c.g.d * sizeof(float)) : 0;
     if (c.bias) {
-        plan.offset_blocks = int64_t(c.bias_rows) * (2 * int64_t(c.g.Hk) - 1) * (2 * p.x_tiles - 1);
+        // four runs of grid rows for the waves of a block at least
+        const int64_t columns = int64_t(c.g.S / c.bias_rows) * (p.x_tiles > 1 ? p.x_tiles - 1 : 1);
+        p.cuts = columns >= 4 || c.g.Hk < 8 ? 1 : 4;
+        plan.offset_blocks = int64_t(c.bias_rows) * (2 * int64_t(c.g.Hk) - 1) * (2 * p.x_tiles - 1);  // at most
         plan.diagonals = round256(size_t(plan.offset_blocks) * 64 * sizeof(float));
     }
     return plan;
@@ -573,7 +684,8 @@ hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, 
             if (e != hipSuccess) return e;
         }
         if (!dbias) return hipSuccess;
-        e = launch_dense_kernel(dense_offset_kernel<T, D>, plan.offset_blocks, 0, stream, nullptr, nullptr, a);
+        const int64_t offsets = int64_t(p.plane.rows) * ((2 * p.Hk - 1 + kOffsetRows<T, D> - 1) / kOffsetRows<T, D>) * (2 * p.x_tiles - 1);
+        e = launch_dense_kernel(dense_offset_kernel<T, D>, offsets, 0, stream, nullptr, nullptr, a);
         if (e != hipSuccess) return e;
         const int64_t blocks = (p.plane.rows * p.plane.size + kBlock - 1) / kBlock;
         return launch_dense_kernel(dense_offset_join_kernel<T>, blocks < 8192 ? blocks : 8192, 0, stream, nullptr, stop, a);
