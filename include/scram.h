@@ -629,7 +629,8 @@ enum { SCRAM_ACT_NONE = 0, SCRAM_ACT_SILU = 1 };
  *             SCRAM_F32 (NULL: ones, zeros)
  *   eps       >= 0, finite
  *   mean, rstd  nullable (both) fp32 [images, groups]: mu and r, for the gradient
- *   workspace scram_group_norm_workspace_bytes(...) bytes, 256-byte aligned
+ *   workspace scram_group_norm_workspace_bytes(...) bytes, 256-byte aligned;
+ *             may be NULL where that is 0
  * images * pixels * channels < 2^40, images * groups < 2^31.  Outputs and the
  * workspace overlap nothing else.  Returns a status code.
  */

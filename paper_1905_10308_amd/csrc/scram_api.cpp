@@ -765,13 +765,13 @@ int scram_group_norm(const void* X, int dtype, const void* weight, const void* b
     int rc = check_group(images, pixels, channels, groups, dtype, weight_dtype, activation);
     if (rc) return rc;
     if (!(eps >= 0.f) || !isfinite(eps)) return SCRAM_ERR_SHAPE;
-    if (!workspace) return SCRAM_ERR_WORKSPACE;
     const size_t eb = elem_bytes(dtype), wb = elem_bytes(weight_dtype);
-    if (!aligned(X, eb) || !aligned(Y, eb) || !aligned(weight, wb) || !aligned(bias, wb) || !aligned(mean, 4) || !aligned(rstd, 4) ||
-        !aligned(workspace, 256))
-        return SCRAM_ERR_ALIGN;
     const scram::GroupCall c{images, pixels, channels, groups, dtype, dtype, weight_dtype, activation, X, weight, bias, nullptr, eps};
     const size_t need = scram::group_norm_workspace_bytes(c);
+    if (need && !workspace) return SCRAM_ERR_WORKSPACE;
+    if (!aligned(X, eb) || !aligned(Y, eb) || !aligned(weight, wb) || !aligned(bias, wb) || !aligned(mean, 4) || !aligned(rstd, 4) ||
+        (need && !aligned(workspace, 256)))
+        return SCRAM_ERR_ALIGN;
     if (workspace_bytes < need) return SCRAM_ERR_WORKSPACE;
     const size_t n = size_t(images) * pixels * channels, stat = mean ? 4 * size_t(images) * groups : 0;
     const Range outs[] = {range(Y, n * eb), range(mean, stat), range(rstd, stat), range(workspace, need)};

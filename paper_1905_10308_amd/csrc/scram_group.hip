@@ -586,7 +586,7 @@ __global__ __launch_bounds__(kBlock) void group_small_kernel(GroupParams p)
         sum = block_sum(sum, s_part);
         const float d = sum.x / n, mean = near + d;  // (what the first sum's rounding left out)
         const float rstd = 1.f / sqrtf(fmaxf(sum.y / n - d * d, 0.f) + p.eps);
-        if (threadIdx.x == 0) {
+        if (threadIdx.x == 0 && p.mean) {
             p.mean[u] = mean;
             p.rstd[u] = rstd;
         }
@@ -704,6 +704,7 @@ size_t group_parts_bytes(const GroupParams& p, int each)
 
 size_t group_norm_workspace_bytes(const GroupCall& c)
 {
+    if (group_small(c)) return 0;
     const GroupParams p = group_params(c);
     return group_parts_bytes(p, 3) + round256(8 * size_t(p.images) * p.groups);
 }
@@ -713,8 +714,12 @@ hipError_t launch_group_norm(const GroupCall& c, void* Y, float* mean, float* rs
     GroupParams p = group_params(c);
     p.out = Y;
     p.parts = static_cast<float*>(workspace);
-    p.mean = mean ? mean : reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + group_parts_bytes(p, 3));
-    p.rstd = rstd ? rstd : p.mean + p.images * p.groups;
+    p.mean = mean;
+    p.rstd = rstd;
+    if (!mean && !group_small(c)) {
+        p.mean = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + group_parts_bytes(p, 3));
+        p.rstd = p.mean + p.images * p.groups;
+    }
     const dim3 grid(group_grid(p.images * p.columns * p.blocks)), joins(group_grid(p.images * p.groups)), block(kBlock);
     auto run = [&](auto type) {
         using T = decltype(type);
@@ -736,6 +741,7 @@ hipError_t launch_group_norm(const GroupCall& c, void* Y, float* mean, float* rs
 size_t group_norm_backward_workspace_bytes(const GroupCall& c)
 {
     const GroupParams p = group_params(c);
+    if (group_small(c)) return round256(8 * size_t(p.images) * p.C);
     return group_parts_bytes(p, 2) + round256(8 * size_t(p.images) * p.C) + round256(8 * size_t(p.images) * p.groups);
 }
 
@@ -751,7 +757,7 @@ hipError_t launch_group_norm_backward(const GroupCall& c, const float* mean, con
     p.rstd_in = rstd;
     unsigned char* const at = static_cast<unsigned char*>(workspace);
     p.parts = reinterpret_cast<float*>(at);
-    p.sums = reinterpret_cast<float*>(at + group_parts_bytes(p, 2));
+    p.sums = reinterpret_cast<float*>(at + (group_small(c) ? 0 : group_parts_bytes(p, 2)));
     p.means = reinterpret_cast<float*>(at + group_parts_bytes(p, 2) + round256(8 * size_t(p.images) * p.C));
     const dim3 grid(group_grid(p.images * p.columns * p.blocks)), joins(group_grid(p.images * p.groups)), block(kBlock);
     auto run = [&](auto type, auto grad) {

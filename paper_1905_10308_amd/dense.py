@@ -146,17 +146,17 @@ def bias_edges(count: int, furthest: int):
 
 
 @functools.lru_cache(maxsize=256)
-def _edges(axis):
-    if len(axis) > BIAS_MAX_EDGES:
-        raise ValueError(f"at most {BIAS_MAX_EDGES} edges an axis, got {len(axis)}")
-    if any(b <= a for a, b in zip((0,) + axis, axis)):
-        raise ValueError(f"edges must rise from 1 on, got {axis}")
-    return (ctypes.c_int * max(len(axis), 1))(*axis)
-
-
-def _both(edges):
-    y, x = edges
-    return tuple(_b._int32("edge", e) for e in y), tuple(_b._int32("edge", e) for e in x)
+def _axes(y, x):
+    """The host arrays of two axes' edges, as the library's calls take them: (edges, count, edges, count)."""
+    got = []
+    for axis in (y, x):
+        axis = tuple(_b._int32("edge", e) for e in axis)
+        if len(axis) > BIAS_MAX_EDGES:
+            raise ValueError(f"at most {BIAS_MAX_EDGES} edges an axis, got {len(axis)}")
+        if any(b <= a for a, b in zip((0,) + axis, axis)):
+            raise ValueError(f"edges must rise from 1 on, got {axis}")
+        got += [(ctypes.c_int * max(len(axis), 1))(*axis), len(axis)]
+    return tuple(got)
 
 
 def relative_bias(table, H: int, W: int, *, edges=None, out=None):
@@ -167,7 +167,6 @@ def relative_bias(table, H: int, W: int, *, edges=None, out=None):
     ``bias_edges(my, H - 1), bias_edges(mx, W - 1)``.  Returns ``[heads, 2 H - 1, 2 W - 1]`` in the table's dtype, for
     :func:`dense_attend`.
     """
-    torch = _b._torch()
     _b._plain("table", table, 3, table.dtype, table.get_device())
     code, (heads, ny, nx) = _b._dtype_code(table), table.shape
     if ny % 2 == 0 or nx % 2 == 0:
@@ -175,17 +174,17 @@ def relative_bias(table, H: int, W: int, *, edges=None, out=None):
     H, W = _b._int32("H", H), _b._int32("W", W)
     if H < 1 or W < 1:
         raise ValueError(f"a grid of {H} x {W}")
-    y, x = _both(edges) if edges is not None else (bias_edges(ny // 2, H - 1), bias_edges(nx // 2, W - 1))
-    if (2 * len(y) + 1, 2 * len(x) + 1) != (ny, nx):
-        raise ValueError(f"{len(y)} and {len(x)} edges need a table of {2 * len(y) + 1} x {2 * len(x) + 1} a head, got {ny} x {nx}")
-    ey, ex = _edges(y), _edges(x)
+    y, x = edges if edges is not None else (bias_edges(ny // 2, H - 1), bias_edges(nx // 2, W - 1))
+    axes = _axes(tuple(y), tuple(x))
+    if (2 * axes[1] + 1, 2 * axes[3] + 1) != (ny, nx):
+        raise ValueError(f"{axes[1]} and {axes[3]} edges need a table of {2 * axes[1] + 1} x {2 * axes[3] + 1} a head, got {ny} x {nx}")
     shape = (heads, 2 * H - 1, 2 * W - 1)
     if out is None:
-        out = torch.empty(shape, dtype=table.dtype, device=table.device)
+        out = table.new_empty(shape)
     elif _b._plain("out", out, 3, table.dtype, table.get_device()).shape != shape:
         raise ValueError(f"out must be {shape}, got {tuple(out.shape)}")
     _b._call(_b.lib().scram_relative_bias, "scram_relative_bias", table.device,
-             (table.data_ptr(), code, heads, H, W, ey, len(y), ex, len(x), out.data_ptr()))
+             (table.data_ptr(), code, heads, H, W, *axes, out.data_ptr()))
     return out
 
 
@@ -199,20 +198,20 @@ def relative_bias_backward(dbias, *, edges, workspace=None):
     code, (heads, hh, ww), dev = _b._dtype_code(dbias), dbias.shape, dbias.device
     if hh % 2 == 0 or ww % 2 == 0:
         raise ValueError(f"dbias must be [heads, 2 H - 1, 2 W - 1], got {tuple(dbias.shape)}")
-    y, x = _both(edges)
-    ey, ex = _edges(y), _edges(x)
+    axes = _axes(*map(tuple, edges))
     H, W = (hh + 1) // 2, (ww + 1) // 2
-    dtable = torch.empty((heads, 2 * len(y) + 1, 2 * len(x) + 1), dtype=dbias.dtype, device=dev)
+    dtable = dbias.new_empty((heads, 2 * axes[1] + 1, 2 * axes[3] + 1))
     if workspace is None:
-        workspace = torch.empty(max(relative_bias_backward_workspace_bytes(heads, H, W, len(x)), 1), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(max(relative_bias_backward_workspace_bytes(heads, H, W, axes[3]), 1), dtype=torch.uint8, device=dev)
     else:
         _b._workspace(workspace, 0, dev)
     _b._call(_b.lib().scram_relative_bias_backward, "scram_relative_bias_backward", dev,
-             (dbias.data_ptr(), code, heads, H, W, ey, len(y), ex, len(x), dtable.data_ptr(), workspace.data_ptr(),
+             (dbias.data_ptr(), code, heads, H, W, *axes, dtable.data_ptr(), workspace.data_ptr(),
               workspace.numel() * workspace.element_size()))
     return dtable
 
 
+@functools.lru_cache(maxsize=256)
 def relative_bias_backward_workspace_bytes(heads: int, H: int, W: int, mx: int) -> int:
     """Bytes of device workspace ``relative_bias_backward`` needs (``mx``: edges of the width)."""
     return int(_b.lib().scram_relative_bias_backward_workspace_bytes(heads, H, W, mx))

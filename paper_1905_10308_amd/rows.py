@@ -211,6 +211,12 @@ def _group(X, groups, weight, bias, activation, out):
     return N, X.numel() // (N * C) if N * C else 0, C, groups, code, wcode, ACTIVATIONS[activation], index
 
 
+@functools.lru_cache(maxsize=1024)
+def _group_bytes(backward, *sizes):
+    L = _b.lib()
+    return int((L.scram_group_norm_backward_workspace_bytes if backward else L.scram_group_norm_workspace_bytes)(*sizes))
+
+
 def group_norm(X, groups: int, weight=None, bias=None, eps: float = 1e-5, *, activation=None, out=None, stats: bool = False,
                workspace=None):
     """Group norm of images, channels last, and an activation (``scram_group_norm``).
@@ -230,15 +236,16 @@ def group_norm(X, groups: int, weight=None, bias=None, eps: float = 1e-5, *, act
         _b._plain("out", out, X.dim(), X.dtype, index)
     mean = rstd = None
     if stats:
-        mean = torch.empty((N, groups), dtype=torch.float32, device=dev)
-        rstd = torch.empty_like(mean)
+        mean, rstd = torch.empty((2, N, groups), dtype=torch.float32, device=dev)
     if workspace is None:
-        workspace = torch.empty(max(group_norm_workspace_bytes(N, pixels, C, groups, dtype=X.dtype), 1), dtype=torch.uint8, device=dev)
+        size = _group_bytes(False, N, pixels, C, groups, code)
+        if size:
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
     else:
-        _b._workspace(workspace, 0, dev)
+        size = _b._workspace(workspace, 0, dev).numel() * workspace.element_size()
     _b._call(_b.lib().scram_group_norm, "scram_group_norm", dev,
              (X.data_ptr(), code, _b._ptr(weight), _b._ptr(bias), wcode, N, pixels, C, groups, float(eps), act, out.data_ptr(),
-              _b._ptr(mean), _b._ptr(rstd), workspace.data_ptr(), workspace.numel() * workspace.element_size()))
+              _b._ptr(mean), _b._ptr(rstd), _b._ptr(workspace), size))
     return (out, mean, rstd) if stats else out
 
 
@@ -265,11 +272,9 @@ def group_norm_backward(dY, X, mean, rstd, weight=None, bias=None, *, activation
         out = torch.empty_like(dY)
     else:
         _b._plain("out", out, X.dim(), gkind, index)
-    dweight = torch.empty(C, dtype=torch.float32, device=dev)
-    dbias = torch.empty_like(dweight)
+    dweight, dbias = torch.empty((2, C), dtype=torch.float32, device=dev)
     if workspace is None:
-        workspace = torch.empty(max(group_norm_backward_workspace_bytes(N, pixels, C, groups, dtype=kind), 1), dtype=torch.uint8,
-                                device=dev)
+        workspace = torch.empty(max(_group_bytes(True, N, pixels, C, groups, code), 1), dtype=torch.uint8, device=dev)
     else:
         _b._workspace(workspace, 0, dev)
     _b._call(_b.lib().scram_group_norm_backward, "scram_group_norm_backward", dev,
@@ -281,9 +286,9 @@ def group_norm_backward(dY, X, mean, rstd, weight=None, bias=None, *, activation
 
 def group_norm_workspace_bytes(images: int, pixels: int, channels: int, groups: int, *, dtype) -> int:
     """Bytes of device workspace ``group_norm`` needs (``dtype``: torch dtype of X)."""
-    return int(_b.lib().scram_group_norm_workspace_bytes(images, pixels, channels, groups, _b._dtype_code_of(dtype)))
+    return _group_bytes(False, images, pixels, channels, groups, _b._dtype_code_of(dtype))
 
 
 def group_norm_backward_workspace_bytes(images: int, pixels: int, channels: int, groups: int, *, dtype) -> int:
     """Bytes of device workspace ``group_norm_backward`` needs (``dtype``: torch dtype of X)."""
-    return int(_b.lib().scram_group_norm_backward_workspace_bytes(images, pixels, channels, groups, _b._dtype_code_of(dtype)))
+    return _group_bytes(True, images, pixels, channels, groups, _b._dtype_code_of(dtype))

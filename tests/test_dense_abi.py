@@ -115,7 +115,7 @@ def test_relative_bias_backward_rejects(L, kw, code):
 
 
 def group(L, backward=False, **kw):
-    a = dict(X=A[0], dtype=BF16, w=A[1], b=A[2], wtype=BF16, N=2, P=30, C=64, G=8, eps=1e-5, act=1, Y=A[3], mean=A[4], rstd=A[5], dY=A[6],
+    a = dict(X=A[0], dtype=BF16, w=A[1], b=A[2], wtype=BF16, N=2, P=3000, C=64, G=8, eps=1e-5, act=1, Y=A[3], mean=A[4], rstd=A[5], dY=A[6],
              gtype=F32, dX=A[7], dw=A[8], db=A[9], ws=A[10], ws_bytes=1 << 24)
     a.update(kw)
     size = (a["N"], a["P"], a["C"], a["G"])

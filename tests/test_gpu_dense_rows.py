@@ -204,10 +204,10 @@ def test_extremes(scram):
 
 
 def test_group_norm_graph_and_refusals(scram):
-    x, w, b, dy = image((2, 12, 12, 40), 5, "bf16", 4)
+    x, w, b, dy = image((2, 30, 40, 40), 5, "bf16", 4)
     dy = dy.bfloat16()
-    n = max(scram.group_norm_workspace_bytes(2, 144, 40, 5, dtype=torch.bfloat16),
-            scram.group_norm_backward_workspace_bytes(2, 144, 40, 5, dtype=torch.bfloat16))
+    n = max(scram.group_norm_workspace_bytes(2, 1200, 40, 5, dtype=torch.bfloat16),
+            scram.group_norm_backward_workspace_bytes(2, 1200, 40, 5, dtype=torch.bfloat16))
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
 
     def call():
@@ -220,7 +220,7 @@ def test_group_norm_graph_and_refusals(scram):
     with torch.cuda.graph(graph):
         held = call()
     for seed in range(5, 8):
-        x.copy_(image((2, 12, 12, 40), 5, "bf16", seed)[0])
+        x.copy_(image((2, 30, 40, 40), 5, "bf16", seed)[0])
         graph.replay()
         got = [t.clone() for t in held]
         assert all(torch.equal(a, c) for a, c in zip(got, call()))
