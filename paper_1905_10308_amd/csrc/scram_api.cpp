@@ -629,7 +629,7 @@ int scram_layer_norm_backward(const void* dY, int grad_dtype, const void* X, int
 size_t scram_dense_attend_workspace_bytes(int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dtype, int biased)
 {
     if (check_grid(S, Hq, Wq, Hk, Wk) || key_slices < 1 || S % key_slices || check_type(dtype, d)) return 0;
-    return scram::dense_workspace_bytes(dense_call(nullptr, nullptr, nullptr, biased ? "" : nullptr, 1, nullptr, S, key_slices, Hq, Wq,
+    return scram::dense_workspace_bytes(dtype, dense_call(nullptr, nullptr, nullptr, biased ? "" : nullptr, 1, nullptr, S, key_slices, Hq, Wq,
                                                    Hk, Wk, d, 1.f, 0, 0, nullptr));
 }
 
@@ -643,8 +643,8 @@ int scram_dense_attend(const void* Q, const void* K, const void* V, int dtype, c
         dense_call(Q, K, V, bias, bias_rows, lengths, S, key_slices, Hq, Wq, Hk, Wk, d, scale, flags, first, origin);
     int rc = check_dense(dtype, call, dv, flags);
     if (rc) return rc;
-    if (scram::dense_blocks(call) > kMaxBlocks) return SCRAM_ERR_SHAPE;
-    const size_t eb = elem_bytes(dtype), need = scram::dense_workspace_bytes(call);
+    if (scram::dense_blocks(dtype, call) > kMaxBlocks) return SCRAM_ERR_SHAPE;
+    const size_t eb = elem_bytes(dtype), need = scram::dense_workspace_bytes(dtype, call);
     if (need && !workspace) return SCRAM_ERR_WORKSPACE;
     if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(bias, eb) || !aligned(lengths, 4) ||
         !aligned(origin, 4) || (need && !aligned(workspace, 256)))

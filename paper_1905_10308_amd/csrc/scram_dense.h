@@ -181,6 +181,36 @@ struct DenseLoad {
     }
 };
 
+// The same for a block of THREADS threads; the rows from `live` (> 0) on are row live - 1 again, whose products count nowhere.
+template <typename T, int D, int N, int THREADS>
+struct DenseStage {
+    using R = DenseRow<T, D>;
+    static constexpr int kTotal = N * R::kChunks;
+    static constexpr int kEach = (kTotal + THREADS - 1) / THREADS;
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    words x[kEach];
+
+    __device__ __forceinline__ void load(const void* rows, int64_t row0, int live)
+    {
+        const unsigned char* const from = static_cast<const unsigned char*>(rows) + row0 * R::kBytes;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int c = i * THREADS + static_cast<int>(threadIdx.x);
+            const uint32_t at = min(c / R::kChunks, live - 1) * R::kBytes + 16 * (c % R::kChunks);
+            x[i] = *reinterpret_cast<const words*>(from + at);
+        }
+    }
+    __device__ __forceinline__ void store(unsigned char* tile) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int c = i * THREADS + static_cast<int>(threadIdx.x);
+            if (kTotal % THREADS == 0 || c < kTotal)
+                *reinterpret_cast<words*>(tile + c / R::kChunks * R::kStride + 16 * (c % R::kChunks)) = x[i];
+        }
+    }
+};
+
 // A row of D elements as the right operand of products over its channels.
 template <typename T, int D>
 __device__ __forceinline__ void load_operand(const void* rows, int64_t row, int h, uint4 (&x)[DenseRow<T, D>::kSteps])
@@ -218,21 +248,76 @@ struct BiasWindow {
     }
 };
 
+// Place of a raster index on the bias' plane, as of an offset from index 0.
+__device__ __forceinline__ int bias_place(const DenseParams& p, int at)
+{
+    uint32_t y, x;
+    divmod(static_cast<uint32_t>(at), p.div_wk, y, x);
+    return static_cast<int>(y) * p.plane.width + static_cast<int>(x);
+}
+
+__device__ __forceinline__ int bias_place_or(bool biased, const DenseParams& p, int at) { return biased ? bias_place(p, at) : 0; }
+
+// A window of the bias' plane on its way to LDS, by a block's THREADS threads: queries q0 .. q1 against keys k0 .. k1.  Places
+// rise with the raster index, so that they lie between those of the runs' ends: the window's start is place(k0) - place(q1),
+// and a pair's index its place less that.
+template <typename T, int THREADS>
+struct BiasStage {
+    float x[2];
+    const T* from;
+    int n;
+
+    __device__ __forceinline__ void load(const DenseParams& p, int head, int q0, int q1, int k0, int k1)
+    {
+        const int base = bias_place(p, k0) - bias_place(p, q1);
+        from = static_cast<const T*>(p.bias) + head * p.plane.size + p.plane.origin + base;
+        n = bias_place(p, k1) - bias_place(p, q0) - base + 1;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int i = static_cast<int>(threadIdx.x) + j * THREADS;
+            x[j] = i < n ? to_float(from[i]) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void store(float* window) const
+    {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int i = static_cast<int>(threadIdx.x) + j * THREADS;
+            if (i < n) window[i] = bias_base2(x[j]);
+        }
+        for (int i = static_cast<int>(threadIdx.x) + 2 * THREADS; i < n; i += THREADS) window[i] = bias_base2(to_float(from[i]));
+    }
+};
+
+__device__ __forceinline__ float bias_at(const float* window, int bytes)
+{
+    return *reinterpret_cast<const float*>(reinterpret_cast<const unsigned char*>(window) + bytes);
+}
+
+// Most places between the ends of a run of q queries against one of k keys.
+inline int64_t bias_window(int q, int k, int Hk, int Wk)
+{
+    if (Hk == 1) return q + k;
+    // n positions over rows that are 2 Wk - 1 places apart
+    auto span = [&](int64_t n) { return n + (Wk - 1) * ((n - 1) / Wk + 1); };
+    return span(q) + span(k);
+}
+
 // Launch of kBlock threads with LDS of a size known at the launch.
-template <typename P>
+template <int THREADS = kBlock, typename P>
 hipError_t launch_dense_kernel(void (*kernel)(P), uint64_t blocks, size_t lds, hipStream_t st, hipEvent_t start, hipEvent_t stop,
                                const P& p)
 {
-    if (blocks == 0 || blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
+    if (blocks == 0 || blocks > 0xFFFFFFFFull / THREADS) return hipErrorInvalidConfiguration;
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  static_cast<int>(lds));
         if (e != hipSuccess) return e;
     }
     if (start || stop)
-        hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), lds, st, start, stop, 0, p);
+        hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(THREADS), lds, st, start, stop, 0, p);
     else
-        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), lds, st, p);
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(THREADS), lds, st, p);
     return hipGetLastError();
 }
 
