@@ -669,7 +669,7 @@ size_t scram_dense_attend_backward_workspace_bytes(int S, int key_slices, int Hq
 {
     if (check_grid(S, Hq, Wq, Hk, Wk) || key_slices < 1 || S % key_slices || check_type(dtype, d)) return 0;
     if (bias_rows < 0 || (bias_rows && S % bias_rows)) return 0;
-    return scram::dense_backward_workspace_bytes(dense_call(nullptr, nullptr, nullptr, bias_rows ? "" : nullptr, bias_rows, nullptr, S,
+    return scram::dense_backward_workspace_bytes(dtype, dense_call(nullptr, nullptr, nullptr, bias_rows ? "" : nullptr, bias_rows, nullptr, S,
                                                             key_slices, Hq, Wq, Hk, Wk, d, 1.f, 0, 0, nullptr));
 }
 
@@ -685,9 +685,9 @@ int scram_dense_attend_backward(const void* Q, const void* K, const void* V, int
         dense_call(Q, K, V, bias, bias_rows, lengths, S, key_slices, Hq, Wq, Hk, Wk, d, scale, flags, first, origin);
     int rc = check_dense(dtype, call, dv, flags);
     if (rc) return rc;
-    if (scram::dense_backward_blocks(call) > kMaxBlocks) return SCRAM_ERR_SHAPE;
+    if (scram::dense_backward_blocks(dtype, call) > kMaxBlocks) return SCRAM_ERR_SHAPE;
     if (!workspace) return SCRAM_ERR_WORKSPACE;
-    const size_t eb = elem_bytes(dtype), need = scram::dense_backward_workspace_bytes(call);
+    const size_t eb = elem_bytes(dtype), need = scram::dense_backward_workspace_bytes(dtype, call);
     if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(dO, 16) || !aligned(bias, eb) || !aligned(lengths, 4) ||
         !aligned(origin, 4) || !aligned(dQ, 16) || !aligned(dK, 16) || !aligned(dV, 16) || !aligned(dbias, eb) ||
         !aligned(workspace, 256))

@@ -153,35 +153,8 @@ __device__ __forceinline__ uint4 column_operand(const unsigned char* tile, int r
     }
 }
 
-// N rows of a tile on their way from memory to LDS, in the registers of a block of kBlock threads; rows from `live` on are zeros.
-template <typename T, int D, int N>
-struct DenseLoad {
-    using R = DenseRow<T, D>;
-    static constexpr int kTotal = N * R::kChunks;
-    static constexpr int kEach = (kTotal + kBlock - 1) / kBlock;
-    uint4 x[kEach];
-
-    __device__ __forceinline__ void load(const void* rows, int64_t row0, int live)
-    {
-        const unsigned char* const from = static_cast<const unsigned char*>(rows) + row0 * R::kBytes;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int c = i * kBlock + static_cast<int>(threadIdx.x);
-            x[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (c / R::kChunks < live && c < kTotal) x[i] = *reinterpret_cast<const uint4*>(from + 16 * c);
-        }
-    }
-    __device__ __forceinline__ void store(unsigned char* tile) const
-    {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int c = i * kBlock + static_cast<int>(threadIdx.x);
-            if (c < kTotal) *reinterpret_cast<uint4*>(tile + c / R::kChunks * R::kStride + 16 * (c % R::kChunks)) = x[i];
-        }
-    }
-};
-
-// The same for a block of THREADS threads; the rows from `live` (> 0) on are row live - 1 again, whose products count nowhere.
+// N rows of a tile on their way from memory to LDS, in the registers of a block of THREADS threads; the rows from `live` (> 0)
+// on are row live - 1 again, whose products count nowhere.
 template <typename T, int D, int N, int THREADS>
 struct DenseStage {
     using R = DenseRow<T, D>;
@@ -226,28 +199,6 @@ __device__ __forceinline__ float bias_base2(float b)
     return fabsf(b) <= kMost ? fminf(fmaxf(b * kLog2e, -kMost), kMost) : b;
 }
 
-// A block's window of the bias plane in LDS: the places of a run of queries against a run of keys.  Places rise with the
-// raster index, so that they lie between those of the runs' ends.
-template <typename T>
-struct BiasWindow {
-    int base;  // place(key) - place(query) - base is the index
-
-    static __device__ __forceinline__ int place(const DenseParams& p, int at)
-    {
-        uint32_t y, x;
-        divmod(static_cast<uint32_t>(at), p.div_wk, y, x);
-        return static_cast<int>(y) * p.plane.width + static_cast<int>(x);
-    }
-    // queries q0 .. q1, keys k0 .. k1
-    __device__ __forceinline__ void stage(const DenseParams& p, int head, int q0, int q1, int k0, int k1, float* window)
-    {
-        const T* const table = static_cast<const T*>(p.bias) + head * p.plane.size + p.plane.origin;
-        base = place(p, k0) - place(p, q1);
-        const int n = place(p, k1) - place(p, q0) - base + 1;
-        for (int i = threadIdx.x; i < n; i += kBlock) window[i] = bias_base2(to_float(table[base + i]));
-    }
-};
-
 // Place of a raster index on the bias' plane, as of an offset from index 0.
 __device__ __forceinline__ int bias_place(const DenseParams& p, int at)
 {
@@ -258,34 +209,34 @@ __device__ __forceinline__ int bias_place(const DenseParams& p, int at)
 
 __device__ __forceinline__ int bias_place_or(bool biased, const DenseParams& p, int at) { return biased ? bias_place(p, at) : 0; }
 
-// A window of the bias' plane on its way to LDS, by a block's THREADS threads: queries q0 .. q1 against keys k0 .. k1.  Places
+// A window of the bias' plane on its way to LDS, by a block's threads or a share of them: queries q0 .. q1 against keys k0 .. k1.  Places
 // rise with the raster index, so that they lie between those of the runs' ends: the window's start is place(k0) - place(q1),
 // and a pair's index its place less that.
-template <typename T, int THREADS>
+template <typename T>
 struct BiasStage {
     float x[2];
     const T* from;
     int n;
 
-    __device__ __forceinline__ void load(const DenseParams& p, int head, int q0, int q1, int k0, int k1)
+    __device__ __forceinline__ void load(const DenseParams& p, int head, int q0, int q1, int k0, int k1, int thread, int threads)
     {
         const int base = bias_place(p, k0) - bias_place(p, q1);
         from = static_cast<const T*>(p.bias) + head * p.plane.size + p.plane.origin + base;
         n = bias_place(p, k1) - bias_place(p, q0) - base + 1;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int i = static_cast<int>(threadIdx.x) + j * THREADS;
+            const int i = thread + j * threads;
             x[j] = i < n ? to_float(from[i]) : 0.f;
         }
     }
-    __device__ __forceinline__ void store(float* window) const
+    __device__ __forceinline__ void store(float* window, int thread, int threads) const
     {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int i = static_cast<int>(threadIdx.x) + j * THREADS;
+            const int i = thread + j * threads;
             if (i < n) window[i] = bias_base2(x[j]);
         }
-        for (int i = static_cast<int>(threadIdx.x) + 2 * THREADS; i < n; i += THREADS) window[i] = bias_base2(to_float(from[i]));
+        for (int i = thread + 2 * threads; i < n; i += threads) window[i] = bias_base2(to_float(from[i]));
     }
 };
 
@@ -301,6 +252,297 @@ inline int64_t bias_window(int q, int k, int Hk, int Wk)
     // n positions over rows that are 2 Wk - 1 places apart
     auto span = [&](int64_t n) { return n + (Wk - 1) * ((n - 1) / Wk + 1); };
     return span(q) + span(k);
+}
+
+// ---------------------------------------------------------------------------
+// Blocks that hold queries and pass over keys (the forward pass, and the query side of the gradients)
+// ---------------------------------------------------------------------------
+
+constexpr int kQueryThreads = 512;
+
+struct DenseQueries : DenseParams {
+    int64_t all_rows;
+    int tiles, splits;  // of a group's rows; of the keys over blocks
+    int window;         // floats of LDS for the bias, of each slice in a tile
+    int window_shift;   // log2 of the shares of a block's threads that stage them
+    int buffers;        // steps whose rows fit in LDS: with two, the next one's are stored while this one's are read
+    int runs;           // whether the keys of a lane's vectors (tile_half of them) lie in one grid row
+};
+
+// Keys of a wave in a block's step: 64, 32 where two steps' rows would not fit in LDS.
+constexpr int wave_keys(int row_bytes, int kw) { return kw * row_bytes <= 512 ? 64 : 32; }
+template <typename T, int D, int KW>
+constexpr int kWaveKeys = wave_keys(D * sizeof(T), KW);
+
+// Bytes of a step's rows in LDS.
+template <typename T, int D, int KW>
+constexpr size_t kTileBytes = 2 * (KW * kWaveKeys<T, D, KW> * DenseRow<T, D>::kStride);
+
+// Bytes of LDS before the bias': the staged rows, and after them what the waves of the same queries join.
+template <typename T, int D, int KW>
+__host__ __device__ constexpr size_t query_lds(int buffers)
+{
+    using R = DenseRow<T, D>;
+    const size_t tiles = buffers * kTileBytes<T, D, KW> + R::kSlack;
+    constexpr size_t join = 8 * 64 * sizeof(float) * (16 * R::kColumns + 2);
+    return tiles > join ? tiles : join;
+}
+
+// s scale2 + bias for a 32 x 32 tile: places are those of the rows of the tile (4 a place), mine the lane's, so that a row's
+// value lies SIGN (its place - mine) bytes into the window.
+template <typename T, int SIGN>
+__device__ __forceinline__ void add_bias(f32x16_t& s, float scale2, const float* window, const int* places, int mine, int h, bool runs)
+{
+    constexpr int N = tile_half<T>();
+    if (runs) {  // a vector's rows lie side by side
+#pragma unroll
+        for (int g = 0; g < 16; g += N) {
+            const int at = SIGN * (places[tile_slot<T>(g) + N * h] - mine);
+#pragma unroll
+            for (int j = 0; j < N; ++j) s[g + j] = fmaf(s[g + j], scale2, bias_at(window, at + 4 * SIGN * j));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale2, bias_at(window, SIGN * (places[tile_slot<T>(i) + N * h] - mine)));
+    }
+}
+
+// A block's rows of queries and its passes over the keys.  Its eight waves share the rows (32 each) and the keys: KW of them
+// take different keys of the same rows.
+template <typename T, int D, bool BIAS, int KW>
+struct QueryBlock {
+    using R = DenseRow<T, D>;
+    static constexpr int kRows = 32 * 8 / KW, kEach = kWaveKeys<T, D, KW>, kKeys = KW * kEach;
+
+    const DenseQueries& p;
+    unsigned char* lds;
+    int* s_places;
+    int bias_floats;  // of a step: places of its keys, windows
+    int lane, m, h, wave, qw, kw;
+    int split, tile, group, slice_k, row;
+    bool live;
+    uint32_t head;
+    int end, least, most_keys;  // first key behind those that the lane's query sees; of the wave's queries the fewest and most
+    int last, t0, t1;           // the block's keys, its steps
+    int64_t out_row;
+    float scale2;
+    int my_at, my_end, my_place;
+    int q0, q1, my_window, my_thread, my_threads;
+    DenseStage<T, D, kKeys, kQueryThreads> kl, vl;
+    BiasStage<T> bl;
+
+    __device__ __forceinline__ int begin_of(int slice) const { return p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first; }
+
+    __device__ __forceinline__ QueryBlock(const DenseQueries& params, unsigned char* memory) : p(params), lds(memory)
+    {
+        s_places = reinterpret_cast<int*>(lds + query_lds<T, D, KW>(p.buffers));
+        bias_floats = kKeys + p.per_group * p.window;
+        const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
+        split = static_cast<int>(b % static_cast<uint32_t>(p.splits));
+        tile = static_cast<int>(b / static_cast<uint32_t>(p.splits) % static_cast<uint32_t>(p.tiles));
+        if (p.causal) tile = p.tiles - 1 - tile;  // those of many keys first
+        group = static_cast<int>(b / static_cast<uint32_t>(p.splits) / static_cast<uint32_t>(p.tiles));
+        lane = threadIdx.x & 63;
+        m = lane & 31;
+        h = lane >> 5;
+        wave = wave_index();
+        qw = wave % (8 / KW);
+        kw = wave / (8 / KW);
+        slice_k = p.per_group == 1 ? group / p.share : group;
+        const int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
+        row = tile * kRows + qw * 32 + m;
+        live = row < p.rows;
+        out_row = static_cast<int64_t>(group) * p.rows + row;
+        uint32_t q;
+        divmod(static_cast<uint32_t>(min(row, p.rows - 1)), p.div_nq, head, q);
+        const int begin = begin_of(group * p.per_group + static_cast<int>(head)), at = begin + static_cast<int>(q);
+        end = live ? (p.causal ? min(length, at + 1) : length) : 0;
+        least = live ? end : p.nk;
+        most_keys = end;
+        for (int k = 16; k >= 1; k >>= 1) {
+            least = min(least, __shfl_xor(least, k));
+            most_keys = max(most_keys, __shfl_xor(most_keys, k));
+        }
+        least = __builtin_amdgcn_readfirstlane(least);
+        most_keys = __builtin_amdgcn_readfirstlane(most_keys);
+        last = length;
+        if (p.causal) {
+            __shared__ int s_end[8];
+            if (lane == 0) s_end[wave] = most_keys;
+            __syncthreads();
+            last = s_end[0];
+            for (int w = 1; w < 8 / KW; ++w) last = max(last, s_end[w]);
+        }
+        const int all = (last + kKeys - 1) / kKeys;
+        t0 = static_cast<int>(static_cast<int64_t>(all) * split / p.splits);
+        t1 = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / p.splits);
+        scale2 = p.scale2;
+        if constexpr (BIAS) {
+            // a tile of several slices (whole ones then) has a window for each, which a share of the threads stages
+            q0 = p.per_group == 1 ? tile * kRows : 0;
+            q1 = min(q0 + kRows, p.nq) - 1;
+            my_threads = kQueryThreads >> p.window_shift;
+            my_window = static_cast<int>(threadIdx.x) / my_threads;
+            my_thread = static_cast<int>(threadIdx.x) % my_threads;
+            // the place of a step's first key less that of the slice's last query is its window's start
+            my_at = bias_place(p, at);
+            my_end = bias_place(p, begin + q1) + (p.per_group > 1 ? static_cast<int>(head) * p.window : 0);
+        }
+    }
+
+    __device__ __forceinline__ int64_t from_row() const { return live ? out_row : static_cast<int64_t>(group) * p.rows; }
+
+    // Scores largest where the rows' products are: a negative scale is taken into the queries.
+    __device__ __forceinline__ void positive_scale(uint4 (&qf)[R::kSteps])
+    {
+        if (scale2 < 0.f) {
+            scale2 = -scale2;
+            constexpr uint32_t kSign = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+#pragma unroll
+            for (int c = 0; c < R::kSteps; ++c) qf[c] = make_uint4(qf[c].x ^ kSign, qf[c].y ^ kSign, qf[c].z ^ kSign, qf[c].w ^ kSign);
+        }
+        if (scale2 == 0.f) scale2 = 1e-37f;  // (a key that is not seen has a score of minus infinity, and a weight of 0 by it)
+    }
+
+    __device__ __forceinline__ void fetch(int t)
+    {
+        const int k0 = t * kKeys;
+        const int64_t k_row = static_cast<int64_t>(slice_k) * p.nk + k0;
+        kl.load(p.K, k_row, last - k0);
+        vl.load(p.V, k_row, last - k0);
+        if constexpr (BIAS) {
+            if (my_window < p.per_group) {
+                const int slice = group * p.per_group + my_window, begin = begin_of(slice);
+                bl.load(p, slice % p.plane.rows, begin + q0, begin + q1, k0, min(k0 + kKeys, p.nk) - 1, my_thread, my_threads);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(int t)
+    {
+        const int at = p.buffers > 1 ? t & 1 : 0;
+        unsigned char* const tiles = lds + at * kTileBytes<T, D, KW>;
+        kl.store(tiles);
+        vl.store(tiles + kKeys * R::kStride);
+        if constexpr (BIAS) {
+            int* const places = s_places + at * bias_floats;
+            if (my_window < p.per_group)
+                bl.store(reinterpret_cast<float*>(places + kKeys) + my_window * p.window, my_thread, my_threads);
+            const int k0 = t * kKeys, k1 = min(k0 + kKeys, p.nk) - 1;
+            if (threadIdx.x < kKeys) places[threadIdx.x] = 4 * bias_place(p, min(k0 + static_cast<int>(threadIdx.x), k1));
+        }
+    }
+
+    // One pass: step(rows, places, k0, from) for every 32 keys of the wave's, keys k0 .. of the slice, staged at rows from ..
+    template <typename F>
+    __device__ __forceinline__ void pass(F&& step)
+    {
+        if (t0 < t1) {
+            fetch(t0);
+            store(t0);
+        }
+        __syncthreads();
+        for (int t = t0; t < t1; ++t) {
+            const int k0 = t * kKeys + kw * kEach, at = p.buffers > 1 ? t & 1 : 0;
+            if (t + 1 < t1) fetch(t + 1);
+            if constexpr (BIAS) my_place = 4 * (my_at + bias_place(p, t * kKeys) - my_end);
+            const int steps = min(kEach, most_keys - k0);
+#pragma unroll 1
+            for (int u = 0; u < steps; u += 32) step(lds + at * kTileBytes<T, D, KW>, s_places + at * bias_floats, k0 + u, kw * kEach + u);
+            if (p.buffers == 1) __syncthreads();
+            if (t + 1 < t1) store(t + 1);
+            __syncthreads();
+        }
+    }
+
+    // Transposed products of the staged keys (rows from .. of the tile at `rows`) with a lane's row.
+    __device__ __forceinline__ f32x16_t products(const unsigned char* rows, int from, const uint4 (&x)[R::kSteps]) const
+    {
+        f32x16_t s(0.f);
+#pragma unroll
+        for (int c = 0; c < R::kSteps; ++c) s = mma<T>(row_operand<T, D>(rows, from + tile_row<T>(m), h, c), x[c], s);
+        return s;
+    }
+    // The scores of products s in base 2 (RAW: before the scale), minus infinity where a key is not seen.
+    template <bool RAW>
+    __device__ __forceinline__ void scores(f32x16_t& s, const int* places, int k0, int from) const
+    {
+        if constexpr (BIAS)
+            add_bias<T, 1>(s, scale2, reinterpret_cast<const float*>(places + kKeys), places + from, my_place, h, p.runs);
+        else if constexpr (!RAW)
+            s *= scale2;
+        if (k0 + 32 > least) {
+            asm volatile("");  // (not for every step, by selects)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = k0 + tile_slot<T>(i) + tile_half<T>() * h < end ? s[i] : -INFINITY;
+        }
+    }
+};
+
+// How a call's queries are dealt to blocks: the waves that share a block's keys, splits of the keys.  split: whether blocks may
+// share a tile's keys.
+struct QueryPlan {
+    int key_waves;
+    int64_t blocks;
+};
+
+constexpr int kMostSplits = 256;
+
+inline QueryPlan query_plan(const DenseCall& c, int elem_bytes, bool split, DenseQueries& p)
+{
+    const int bytes = c.g.d * elem_bytes;
+    auto room = [&](int kw, int slices, int buffers) {
+        const int64_t keys = kw * wave_keys(bytes, kw), rows = 256 / kw;
+        const int64_t windows = c.bias ? slices * bias_window(int(rows), int(keys), c.g.Hk, c.g.Wk) + keys : 0;
+        return buffers * (2 * keys * (bytes + 16) + 4 * windows) + 6144 <= 160 * 1024;
+    };
+    // a tile that holds the queries of all slices of a key slice, each with a window
+    const bool together = c.bias && p.share > 1 && int64_t(p.share) * p.nq <= 32 && p.share <= 16 && bytes <= 256 && room(8, p.share, 1);
+    if (!c.bias || together) {
+        p.per_group = p.share;
+        p.groups = c.g.S / p.share;
+        p.rows = p.nq * p.share;
+    }
+    auto blocks = [&](int kw) { return int64_t(p.groups) * ((p.rows + 256 / kw - 1) / (256 / kw)); };
+    int kw = 8;
+    if (p.rows > 32 && blocks(4) >= 256) kw = 4;
+    if (p.rows > 64 && blocks(2) >= 256) kw = 2;
+    if (bytes > 256 && kw == 8) kw = 4;
+    if (!room(kw, together ? p.share : 1, 1)) kw = 2;
+    p.buffers = room(kw, together ? p.share : 1, 2) ? 2 : 1;
+    p.tiles = (p.rows + 256 / kw - 1) / (256 / kw);
+    const int keys = kw * wave_keys(bytes, kw);
+    if (c.bias) p.window = int(bias_window(256 / kw, keys, c.g.Hk, c.g.Wk));
+    while ((1 << p.window_shift) < p.per_group && c.bias) ++p.window_shift;
+    p.runs = c.g.Wk % (elem_bytes == 2 ? 8 : 4) == 0;
+    // fewer blocks than CUs leave CUs idle
+    const int64_t steps = (p.nk + keys - 1) / keys;
+    int64_t n = split ? 256 / blocks(kw) : 1;
+    if (n > steps) n = steps;
+    if (n > kMostSplits) n = kMostSplits;
+    p.splits = n < 1 ? 1 : int(n);
+    p.all_rows = int64_t(p.groups) * p.rows;
+    return QueryPlan{kw, blocks(kw) * p.splits};
+}
+
+// Bytes of LDS of a block of queries.
+template <typename T, int D, bool BIAS, int KW>
+size_t query_block_lds(const DenseQueries& p)
+{
+    constexpr int keys = KW * kWaveKeys<T, D, KW>;
+    return query_lds<T, D, KW>(p.buffers) + (BIAS ? p.buffers * (keys + size_t(p.per_group) * p.window) * sizeof(float) + 64 : 0);
+}
+
+// f(BIAS, KW) of a plan
+template <typename T, int D, typename F>
+hipError_t query_dispatch(bool biased, int key_waves, F&& f)
+{
+    auto with = [&](auto b) {
+        if (key_waves == 2) return f(b, std::integral_constant<int, 2>{});
+        if constexpr (D * sizeof(T) <= 256)
+            if (key_waves == 8) return f(b, std::integral_constant<int, 8>{});
+        return f(b, std::integral_constant<int, 4>{});
+    };
+    return biased ? with(std::true_type{}) : with(std::false_type{});
 }
 
 // Launch of kBlock threads with LDS of a size known at the launch.

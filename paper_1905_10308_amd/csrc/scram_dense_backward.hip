@@ -21,9 +21,9 @@
 namespace scram {
 namespace {
 
-constexpr int kRowsBlock = 128;  // queries or keys of a block
+constexpr int kKeysBlock = 128;  // keys of a block of the key side
 
-struct DenseBackward : DenseParams {
+struct DenseBackward : DenseQueries {
     const void* dO;
     void* dQ;
     void* dK;
@@ -33,8 +33,9 @@ struct DenseBackward : DenseParams {
     float* part;       // key side: [splits][all keys][2][D]
     float* diagonals;  // [bias rows][2 Hk - 1][2 x_tiles - 1][64]
     int64_t all_keys;
-    int tiles;         // of a group's queries, or of a slice's keys
-    int splits;        // key side: runs of query tiles
+    int key_tiles;     // of a slice's keys
+    int key_splits;    // runs of query tiles
+    int key_window;    // floats of LDS for the key side's bias
     int x_tiles, Hk, Wk, key_slices, S;
     int cuts;          // of a column's grid rows among waves
 };
@@ -49,174 +50,116 @@ __device__ __forceinline__ float4 row_stats(float top, float sum, float dsum)
     return make_float4(apart ? top : top + __builtin_amdgcn_logf(sum), apart ? 1.f / sum : 1.f, dsum / sum, 0.f);
 }
 
-// Rows of the other side that a block stages at a time.
-template <typename T, int D>
-constexpr int kStaged = D * sizeof(T) > 256 ? 32 : 64;
-
-template <typename T, int D>
-constexpr size_t backward_lds()
+// The query side: two passes over the keys.
+template <typename T, int D, bool BIAS, int KW>
+__global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBackward p)
 {
     using R = DenseRow<T, D>;
-    return 2 * (kStaged<T, D> * R::kStride) + R::kSlack;
-}
-
-// The query side.
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(kBlock) void dense_query_kernel(DenseBackward p)
-{
-    using R = DenseRow<T, D>;
-    constexpr int kKeys = kStaged<T, D>, U = kKeys / 32;
+    constexpr bool kFold = sizeof(T) == 2 && !BIAS;  // as in the forward pass; the first pass keeps a certain key's weight at 1
     extern __shared__ __align__(16) unsigned char lds[];
-    unsigned char* const k_tile = lds;
-    unsigned char* const v_tile = lds + kKeys * R::kStride;
-    int* const s_place = reinterpret_cast<int*>(lds + backward_lds<T, D>());
-    float* const s_bias = reinterpret_cast<float*>(s_place + kKeys);
-    __shared__ int s_end[4];
-
-    const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
-    const int tile = static_cast<int>(b % static_cast<uint32_t>(p.tiles));
-    const int group = static_cast<int>(b / static_cast<uint32_t>(p.tiles));
-    const int lane = threadIdx.x & 63, wave = wave_index(), m = lane & 31, h = lane >> 5;
-    const int slice_k = p.per_group == 1 ? group / p.share : group;
-    const int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
-    const int row = tile * kRowsBlock + wave * 32 + m;
-    const bool live = row < p.rows;
-    uint32_t head, q;
-    divmod(static_cast<uint32_t>(min(row, p.rows - 1)), p.div_nq, head, q);
-    const int slice = group * p.per_group + static_cast<int>(head);
-    const int begin = p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first;
-    const int at = begin + static_cast<int>(q);
-    const int end = live ? (p.causal ? min(length, at + 1) : length) : 0;
-    int last = length;
-    if (p.causal) {
-        int e = end;
-        for (int k = 32; k >= 1; k >>= 1) e = max(e, __shfl_xor(e, k));
-        if (lane == 0) s_end[wave] = e;
-        __syncthreads();
-        last = max(max(s_end[0], s_end[1]), max(s_end[2], s_end[3]));
-    }
-    const int all = (last + kKeys - 1) / kKeys;
-
-    const int64_t out_row = static_cast<int64_t>(group) * p.rows + row;
-    const int64_t from_row = live ? out_row : static_cast<int64_t>(group) * p.rows;
+    __shared__ float s_join[3][8][32];
+    QueryBlock<T, D, BIAS, KW> q(p, lds);
+    const int lane = q.lane, m = q.m, h = q.h, wave = q.wave, qw = q.qw, kw = q.kw;
+    const int64_t out_row = q.out_row;
     uint4 qf[R::kSteps], gf[R::kSteps];
-    load_operand<T, D>(p.Q, from_row, h, qf);
-    load_operand<T, D>(p.dO, from_row, h, gf);
+    load_operand<T, D>(p.Q, q.from_row(), h, qf);
+    load_operand<T, D>(p.dO, q.from_row(), h, gf);
+    if constexpr (kFold) q.positive_scale(qf);
 
-    DenseLoad<T, D, kKeys> kl, vl;
-    const int64_t k_row = static_cast<int64_t>(slice_k) * p.nk;
-    BiasWindow<T> win{};
-    int my_place = 0;
-    if constexpr (BIAS) my_place = BiasWindow<T>::place(p, at);
-    f32x16_t s[U], g[U];
-    // the tile's scores in base 2 (minus infinity: not seen) and dp
-    auto scores = [&](int t) {
-        const int k0 = t * kKeys;
-        kl.store(k_tile);
-        vl.store(v_tile);
-        if constexpr (BIAS) {
-            const int k1 = min(k0 + kKeys, p.nk) - 1;
-            const int q0 = tile * kRowsBlock, q1 = min(q0 + kRowsBlock, p.rows) - 1;
-            win.stage(p, slice % p.plane.rows, begin + q0, begin + q1, k0, k1, s_bias);
-            if (threadIdx.x < kKeys) s_place[threadIdx.x] = BiasWindow<T>::place(p, min(k0 + static_cast<int>(threadIdx.x), k1));
-        }
-        __syncthreads();
-        const int next = t + 1 < all ? t + 1 : 0;  // the second pass begins again
-        kl.load(p.K, k_row + next * static_cast<int64_t>(kKeys), last - next * kKeys);
-        vl.load(p.V, k_row + next * static_cast<int64_t>(kKeys), last - next * kKeys);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            s[u] = f32x16_t(0.f);
-            g[u] = f32x16_t(0.f);
-#pragma unroll
-            for (int c = 0; c < R::kSteps; ++c) {
-                s[u] = mma<T>(row_operand<T, D>(k_tile, 32 * u + tile_row<T>(m), h, c), qf[c], s[u]);
-                g[u] = mma<T>(row_operand<T, D>(v_tile, 32 * u + tile_row<T>(m), h, c), gf[c], g[u]);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int key = 32 * u + tile_slot<T>(i) + tile_half<T>() * h;
-                float x = s[u][i] * p.scale2;
-                if constexpr (BIAS) x = fmaf(s[u][i], p.scale2, s_bias[s_place[key] - my_place - win.base]);
-                s[u][i] = x;
-            }
-        if (__all(end >= k0 + kKeys)) return;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[u][i] = k0 + 32 * u + tile_slot<T>(i) + tile_half<T>() * h < end ? s[u][i] : -INFINITY;
-    };
-
+    // a lane's maximum, sum, and sum of dp: of its half of the keys
     float top = -INFINITY, sum = 0.f, dsum = 0.f;
-    if (all > 0) {
-        kl.load(p.K, k_row, last);
-        vl.load(p.V, k_row, last);
-    }
-    for (int t = 0; t < all; ++t) {
-        scores(t);
-        float most = -INFINITY;
+    q.pass([&](const unsigned char* rows, const int* places, int k0, int from) {
+        f32x16_t s = q.products(rows, from, qf);
+        const f32x16_t g = q.products(rows + q.kKeys * R::kStride, from, gf);
+        q.template scores<false>(s, places, k0, from);
+        float most = top;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) most = fmaxf(most, s[u][i]);
-        most = fmaxf(most, __shfl_xor(most, 32));
-        const float next = fmaxf(top, most), shift = next == -INFINITY ? 0.f : next;
-        const float keep = __builtin_amdgcn_exp2f(top - shift);
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i]);
+        const float shift = most == -INFINITY ? 0.f : most, keep = __builtin_amdgcn_exp2f(top - shift);
         sum *= keep;
         dsum *= keep;
-        top = next;
+        top = most;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(s[u][i] - shift);
-                sum += e;
-                dsum = fmaf(e, g[u][i], dsum);
-            }
-        __syncthreads();
+        for (int i = 0; i < 16; ++i) {
+            const float e = __builtin_amdgcn_exp2f(s[i] - shift);
+            sum += e;
+            dsum = fmaf(e, g[i], dsum);
+        }
+    });
+    auto join = [&](float t, float a, float b) {
+        const float most = fmaxf(top, t), shift = most == -INFINITY ? 0.f : most;
+        const float x = __builtin_amdgcn_exp2f(top - shift), y = __builtin_amdgcn_exp2f(t - shift);
+        sum = sum * x + a * y;
+        dsum = dsum * x + b * y;
+        top = most;
+    };
+    join(__shfl_xor(top, 32), __shfl_xor(sum, 32), __shfl_xor(dsum, 32));
+    if (h == 0) {
+        s_join[0][wave][m] = top;
+        s_join[1][wave][m] = sum;
+        s_join[2][wave][m] = dsum;
     }
-    sum += __shfl_xor(sum, 32);
-    dsum += __shfl_xor(dsum, 32);
+    __syncthreads();
+    top = -INFINITY;
+    sum = dsum = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) join(s_join[0][k * (8 / KW) + qw][m], s_join[1][k * (8 / KW) + qw][m], s_join[2][k * (8 / KW) + qw][m]);
     const float4 stats = row_stats(top, sum, dsum);
-    if (live && h == 0) p.stats[out_row] = stats;
+    if (q.live && h == 0 && kw == 0) p.stats[out_row] = stats;
     // here the sum divides once, at the end
-    const float shift = top == -INFINITY ? 0.f : top, mean = stats.z;
+    const float shift = top == -INFINITY ? 0.f : top, mean = stats.z, scale2 = q.scale2;
     const float factor = sum == 0.f ? 0.f : p.scale / sum;
 
     f32x16_t o[R::kColumns];
 #pragma unroll
     for (int c = 0; c < R::kColumns; ++c) o[c] = f32x16_t(0.f);
-    for (int t = 0; t < all; ++t) {
-        scores(t);
+    q.pass([&](const unsigned char* rows, const int* places, int k0, int from) {
+        f32x16_t s = q.products(rows, from, qf);
+        const f32x16_t g = q.products(rows + q.kKeys * R::kStride, from, gf);
+        q.template scores<kFold>(s, places, k0, from);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int i = 0; i < 16; ++i)
+            s[i] = __builtin_amdgcn_exp2f(kFold ? fmaf(s[i], scale2, -shift) : s[i] - shift) * (g[i] - mean);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[u][i] = __builtin_amdgcn_exp2f(s[u][i] - shift) * (g[u][i] - mean);
+        for (int r = 0; r < R::kRowSteps; ++r) {
+            const uint4 w = as_operand<T>(s, r);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int r = 0; r < R::kRowSteps; ++r) {
-                const uint4 w = as_operand<T>(s[u], r);
-#pragma unroll
-                for (int c = 0; c < R::kColumns; ++c) o[c] = mma<T>(column_operand<T, D>(k_tile, 32 * u, r, c), w, o[c]);
-            }
-        __syncthreads();
-    }
-    if (!live) return;
-    T* const to = static_cast<T*>(p.dQ) + out_row * D;
+            for (int c = 0; c < R::kColumns; ++c) o[c] = mma<T>(column_operand<T, D>(rows, from, r, c), w, o[c]);
+        }
+    });
+    // the waves of the same queries: each joins a share of the channels
+    constexpr int kPart = 64 * 16 * R::kColumns;
+    float* const joined = reinterpret_cast<float*>(lds);
 #pragma unroll
     for (int c = 0; c < R::kColumns; ++c)
 #pragma unroll
-        for (int i = 0; i < (D < 32 ? 2 : 4); ++i) {
-            vec<T, 4> x;
+        for (int i = 0; i < 16; ++i) joined[wave * kPart + 64 * (16 * c + i) + lane] = o[c][i];
+    __syncthreads();
+    if (!q.live) return;
+    constexpr int kQuads = D < 32 ? 2 : 4 * R::kColumns;
+    for (int g = kw; g < kQuads; g += KW) {
+        vec<T, 4> y;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = from_float<T>(o[c][4 * i + j] * factor);
-            store_vec<T, 4>(to + 32 * c + 8 * i + 4 * h, x);
+        for (int j = 0; j < 4; ++j) {
+            float x = 0.f;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) x += joined[(k * (8 / KW) + qw) * kPart + 64 * (4 * g + j) + lane];
+            y[j] = from_float<T>(x * factor);
         }
+        store_vec<T, 4>(static_cast<T*>(p.dQ) + out_row * D + 8 * g + 4 * h, y);
+    }
+}
+
+// Rows of queries that a block of the key side stages at a time, and whether two such steps fit in LDS.
+template <typename T, int D>
+constexpr int kStaged = D * sizeof(T) > 256 ? 32 : 64;
+template <typename T, int D>
+constexpr size_t kKeyTile = 2 * (kStaged<T, D> * DenseRow<T, D>::kStride);
+
+template <typename T, int D>
+size_t key_lds(const DenseBackward& p, bool biased)
+{
+    return 2 * kKeyTile<T, D> + DenseRow<T, D>::kSlack + 2 * sizeof(float) * (3 * kStaged<T, D> + (biased ? kStaged<T, D> + p.key_window : 0)) + 64;
 }
 
 // The key side: a block's 128 keys against a run of the query tiles of the slices that read them.
@@ -226,29 +169,24 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
     using R = DenseRow<T, D>;
     constexpr int kRows = kStaged<T, D>, U = kRows / 32;
     extern __shared__ __align__(16) unsigned char lds[];
-    unsigned char* const q_tile = lds;
-    unsigned char* const g_tile = lds + kRows * R::kStride;
-    int* const s_place = reinterpret_cast<int*>(lds + backward_lds<T, D>());
-    float* const s_bias = reinterpret_cast<float*>(s_place + kRows);
-    __shared__ __align__(16) float s_lse[kRows], s_mean[kRows], s_factor[kRows];
+    // of each of two steps: logarithms, factors and means of the queries' softmax, their places, the bias' window
+    float* const s_stats = reinterpret_cast<float*>(lds + 2 * kKeyTile<T, D> + R::kSlack);
+    const int stats_floats = 3 * kRows + (BIAS ? kRows + p.key_window : 0);
 
     const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
-    const int split = static_cast<int>(b % static_cast<uint32_t>(p.splits));
-    const int tile = static_cast<int>(b / static_cast<uint32_t>(p.splits) % static_cast<uint32_t>(p.tiles));
-    const int slice_k = static_cast<int>(b / static_cast<uint32_t>(p.splits) / static_cast<uint32_t>(p.tiles));
+    const int split = static_cast<int>(b % static_cast<uint32_t>(p.key_splits));
+    const int tile = static_cast<int>(b / static_cast<uint32_t>(p.key_splits) % static_cast<uint32_t>(p.key_tiles));
+    const int slice_k = static_cast<int>(b / static_cast<uint32_t>(p.key_splits) / static_cast<uint32_t>(p.key_tiles));
     const int lane = threadIdx.x & 63, wave = wave_index(), m = lane & 31, h = lane >> 5;
     // the keys that count and that some query sees: no others are read
     int length = p.lengths ? min(max(p.lengths[slice_k], 0), p.nk) : p.nk;
+    auto begin_of = [&](int slice) { return p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first; };
     if (p.causal) {
-        int reach = p.first + p.nq;
-        if (p.origin) {
-            reach = 0;
-            for (int s = 0; s < p.share; ++s)
-                reach = max(reach, min(max(p.origin[slice_k * static_cast<int64_t>(p.share) + s], 0), p.nk - p.nq) + p.nq);
-        }
+        int reach = 0;
+        for (int s = 0; s < (p.origin ? p.share : 1); ++s) reach = max(reach, begin_of(slice_k * p.share + s) + p.nq);
         length = min(length, reach);
     }
-    const int k_first = tile * kRowsBlock, key = k_first + wave * 32 + m;
+    const int k_first = tile * kKeysBlock, k_wave = k_first + wave * 32, key = k_wave + m;
     const bool seen = key < length;
     const int64_t k_row = static_cast<int64_t>(slice_k) * p.nk;
 
@@ -262,105 +200,134 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
     f32x16_t dk[R::kColumns], dv[R::kColumns];
 #pragma unroll
     for (int c = 0; c < R::kColumns; ++c) dk[c] = dv[c] = f32x16_t(0.f);
-    int my_place = 0;
-    if constexpr (BIAS) my_place = BiasWindow<T>::place(p, min(key, p.nk - 1));
+    const int k_last = min(k_first + kKeysBlock, p.nk) - 1;
+    int key_place = 0, first_place = 0;
+    if constexpr (BIAS) {
+        key_place = bias_place(p, min(key, p.nk - 1));
+        first_place = bias_place(p, k_first);
+    }
 
     const int per_slice = (p.nq + kRows - 1) / kRows, all = per_slice * p.share;
-    const int t0 = static_cast<int>(static_cast<int64_t>(all) * split / p.splits);
-    const int t1 = k_first < length ? static_cast<int>(static_cast<int64_t>(all) * (split + 1) / p.splits) : t0;
-    DenseLoad<T, D, kRows> ql, gl;
-    // the next tile of which a query sees a key of the block, from t on; its slice's first place
-    int begin = 0;
+    const int t0 = static_cast<int>(static_cast<int64_t>(all) * split / p.key_splits);
+    const int t1 = k_first < length ? static_cast<int>(static_cast<int64_t>(all) * (split + 1) / p.key_splits) : t0;
+    // the next tile of which a query sees a key of the block, from t on
     auto seek = [&](int t) {
-        for (; t < t1; ++t) {
-            const int slice = slice_k * p.share + t / per_slice, q0 = t % per_slice * kRows;
-            begin = p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first;
-            if (!p.causal || begin + min(q0 + kRows, p.nq) > k_first) break;
-        }
+        if (p.causal)
+            for (; t < t1; ++t) {
+                const int q0 = t % per_slice * kRows;
+                if (begin_of(slice_k * p.share + t / per_slice) + min(q0 + kRows, p.nq) > k_first) break;
+            }
         return t;
     };
+    DenseStage<T, D, kRows, kBlock> ql, gl;
+    BiasStage<T> bl;
+    float4 st = make_float4(INFINITY, 1.f, 0.f, 0.f);
+    int next_at = 0, next_end = 0, next_place = 0;  // of the fetched tile: place of its first query; places on the bias' plane
     auto fetch = [&](int t) {
-        const int64_t row = (slice_k * static_cast<int64_t>(p.share) + t / per_slice) * p.nq + t % per_slice * kRows;
-        ql.load(p.Q, row, p.nq - t % per_slice * kRows);
-        gl.load(p.dO, row, p.nq - t % per_slice * kRows);
-    };
-    int t = seek(t0);
-    if (t < t1) fetch(t);
-    while (t < t1) {
-        const int slice = slice_k * p.share + t / per_slice, q0 = t % per_slice * kRows;
-        const int at0 = begin + q0;  // place of the tile's first query
-        ql.store(q_tile);
-        gl.store(g_tile);
-        bool apart = false;
-        if (threadIdx.x < kRows) {
-            const int q = q0 + static_cast<int>(threadIdx.x);
-            const float4 st = q < p.nq ? p.stats[static_cast<int64_t>(slice) * p.nq + q] : make_float4(INFINITY, 1.f, 0.f, 0.f);
-            s_lse[threadIdx.x] = st.x;
-            s_factor[threadIdx.x] = st.y;
-            s_mean[threadIdx.x] = st.z;
-            apart = st.y != 1.f;
-            if constexpr (BIAS) s_place[threadIdx.x] = BiasWindow<T>::place(p, begin + min(q, p.nq - 1));
+        const int slice = slice_k * p.share + t / per_slice, q0 = t % per_slice * kRows, begin = begin_of(slice);
+        const int64_t row = static_cast<int64_t>(slice) * p.nq + q0;
+        ql.load(p.Q, row, p.nq - q0);
+        gl.load(p.dO, row, p.nq - q0);
+        const int q = static_cast<int>(threadIdx.x);
+        st = make_float4(INFINITY, 1.f, 0.f, 0.f);
+        if (q < kRows && q0 + q < p.nq) st = p.stats[row + q];
+        next_at = begin + q0;
+        if constexpr (BIAS) {
+            const int q1 = begin + min(q0 + kRows, p.nq) - 1;
+            bl.load(p, slice % p.plane.rows, begin + q0, q1, k_first, k_last, q, kBlock);
+            next_end = bias_place(p, q1);
+            if (q < kRows) next_place = 4 * bias_place(p, min(begin + q0 + q, q1));
         }
-        BiasWindow<T> win{};
-        if constexpr (BIAS)
-            win.stage(p, slice % p.plane.rows, at0, begin + min(q0 + kRows, p.nq) - 1, k_first, min(k_first + kRowsBlock, p.nk) - 1,
-                      s_bias);
-        apart = __syncthreads_or(apart);
+    };
+    bool apart = false;
+    auto store = [&](int at) {
+        ql.store(lds + at * kKeyTile<T, D>);
+        gl.store(lds + at * kKeyTile<T, D> + kRows * R::kStride);
+        float* const stats = s_stats + at * stats_floats;
+        const int q = static_cast<int>(threadIdx.x);
+        if (q < kRows) {
+            stats[q] = st.x;
+            stats[kRows + q] = st.y;
+            stats[2 * kRows + q] = st.z;
+            if constexpr (BIAS) reinterpret_cast<int*>(stats)[3 * kRows + q] = next_place;
+        }
+        if constexpr (BIAS) bl.store(stats + 4 * kRows, q, kBlock);
+        return st.y != 1.f;
+    };
+    int t = seek(t0), at = 0;
+    if (t < t1) {
+        fetch(t);
+        apart = store(0);
+    }
+    apart = __syncthreads_or(apart);
+    while (t < t1) {
+        const int at0 = next_at;  // place of the tile's first query
+        // 4 (place of the key, less the window's start)
+        const int my_place = 4 * (key_place - (first_place - next_end));
+        const unsigned char* const q_tile = lds + at * kKeyTile<T, D>;
+        const unsigned char* const g_tile = q_tile + kRows * R::kStride;
+        const float* const stats = s_stats + at * stats_floats;
         t = seek(t + 1);
         if (t < t1) fetch(t);
         // a query after which some key of the wave's comes, or a key that is not seen
-        const bool masked = (p.causal && at0 < k_first + wave * 32 + 31) || k_first + wave * 32 + 32 > length;
-#pragma unroll
+        const bool masked = (p.causal && at0 < k_wave + 31) || k_wave + 32 > length;
+#pragma unroll 1
         for (int u = 0; u < U; ++u) {
+            if (p.causal && at0 + 32 * u + 31 < k_wave) continue;  // before the wave's keys
             f32x16_t s(0.f), g(0.f);
 #pragma unroll
             for (int c = 0; c < R::kSteps; ++c) {
                 s = mma<T>(row_operand<T, D>(q_tile, 32 * u + tile_row<T>(m), h, c), kf[c], s);
                 g = mma<T>(row_operand<T, D>(g_tile, 32 * u + tile_row<T>(m), h, c), vf[c], g);
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int q = 32 * u + tile_slot<T>(i) + tile_half<T>() * h;
-                float x = s[i] * p.scale2;
-                if constexpr (BIAS) x = fmaf(s[i], p.scale2, s_bias[my_place - s_place[q] - win.base]);
-                s[i] = x;
-            }
-            if (masked)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int q = 32 * u + tile_slot<T>(i) + tile_half<T>() * h;
-                    s[i] = seen && (!p.causal || key <= at0 + q) ? s[i] : -INFINITY;
-                }
+            const int row0 = 32 * u + tile_half<T>() * h;
             f32x16_t w;
+            if constexpr (BIAS) {
+                add_bias<T, -1>(s, p.scale2, stats + 4 * kRows, reinterpret_cast<const int*>(stats) + 3 * kRows + 32 * u, my_place, h, p.runs);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(s[i] - s_lse[32 * u + tile_slot<T>(i) + tile_half<T>() * h]);
-            if (apart)
+                for (int i = 0; i < 16; ++i) w[i] = s[i] - stats[row0 + tile_slot<T>(i)];
+            } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] *= s_factor[32 * u + tile_slot<T>(i) + tile_half<T>() * h];
+                for (int i = 0; i < 16; ++i) w[i] = fmaf(s[i], p.scale2, -stats[row0 + tile_slot<T>(i)]);
+            }
+            if (masked) {
+                asm volatile("");  // (not for every tile, by selects)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = w[i] * (g[i] - s_mean[32 * u + tile_slot<T>(i) + tile_half<T>() * h]);
+                for (int i = 0; i < 16; ++i) w[i] = seen && (!p.causal || key <= at0 + row0 + tile_slot<T>(i)) ? w[i] : -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(w[i]);
+            if (apart) {
+                asm volatile("");
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] *= stats[kRows + row0 + tile_slot<T>(i)];
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = w[i] * (g[i] - stats[2 * kRows + row0 + tile_slot<T>(i)]);
 #pragma unroll
             for (int r = 0; r < R::kRowSteps; ++r) {
-                const uint4 a = as_operand<T>(w, r), c4 = as_operand<T>(s, r);
+                const uint4 a = as_operand<T>(w, r), d = as_operand<T>(s, r);
 #pragma unroll
                 for (int c = 0; c < R::kColumns; ++c) {
                     dv[c] = mma<T>(column_operand<T, D>(g_tile, 32 * u, r, c), a, dv[c]);
-                    dk[c] = mma<T>(column_operand<T, D>(q_tile, 32 * u, r, c), c4, dk[c]);
+                    dk[c] = mma<T>(column_operand<T, D>(q_tile, 32 * u, r, c), d, dk[c]);
                 }
             }
         }
-        __syncthreads();
+        at ^= 1;
+        apart = t < t1 ? store(at) : false;
+        apart = __syncthreads_or(apart);
     }
     if (key >= p.nk) return;
-    if (p.splits > 1) {
+    if (p.key_splits > 1) {
         float* const to = p.part + (static_cast<int64_t>(split) * p.all_keys + k_row + key) * (2 * D);
 #pragma unroll
         for (int c = 0; c < R::kColumns; ++c)
 #pragma unroll
             for (int i = 0; i < (D < 32 ? 2 : 4); ++i) {
-                float* const at = to + 32 * c + 8 * i + 4 * h;
-                *reinterpret_cast<float4*>(at) = make_float4(dk[c][4 * i], dk[c][4 * i + 1], dk[c][4 * i + 2], dk[c][4 * i + 3]);
-                *reinterpret_cast<float4*>(at + D) = make_float4(dv[c][4 * i], dv[c][4 * i + 1], dv[c][4 * i + 2], dv[c][4 * i + 3]);
+                float* const x = to + 32 * c + 8 * i + 4 * h;
+                *reinterpret_cast<float4*>(x) = make_float4(dk[c][4 * i], dk[c][4 * i + 1], dk[c][4 * i + 2], dk[c][4 * i + 3]);
+                *reinterpret_cast<float4*>(x + D) = make_float4(dv[c][4 * i], dv[c][4 * i + 1], dv[c][4 * i + 2], dv[c][4 * i + 3]);
             }
         return;
     }
@@ -389,7 +356,7 @@ __global__ __launch_bounds__(kBlock) void dense_key_join_kernel(DenseBackward p)
     if (row >= p.all_keys) return;
     const int c = static_cast<int>(i % (D / 2)) * 4;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < p.splits; ++s) {
+    for (int s = 0; s < p.key_splits; ++s) {
         const float4 y = *reinterpret_cast<const float4*>(p.part + (static_cast<int64_t>(s) * p.all_keys + row) * (2 * D) + c);
         x[0] += y.x;
         x[1] += y.y;
@@ -598,32 +565,35 @@ size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 
 struct BackwardPlan {
     DenseBackward p;
-    int64_t query_blocks, key_blocks, offset_blocks;
+    QueryPlan queries;
+    int64_t key_blocks, offset_blocks;
     size_t stats, part, diagonals;  // bytes
 };
 
-BackwardPlan backward_plan(const DenseCall& c)
+BackwardPlan backward_plan(const DenseCall& c, int elem_bytes)
 {
     BackwardPlan plan{};
     DenseBackward& p = plan.p;
     static_cast<DenseParams&>(p) = dense_params(c);
+    plan.queries = query_plan(c, elem_bytes, false, p);
     p.S = c.g.S;
     p.Hk = c.g.Hk;
     p.Wk = c.g.Wk;
     p.key_slices = c.key_slices;
     p.all_keys = int64_t(c.key_slices) * p.nk;
-    p.x_tiles = (c.g.Wk + 31) / 32;
-    plan.query_blocks = int64_t(p.groups) * ((p.rows + kRowsBlock - 1) / kRowsBlock);
-    const int64_t tiles = int64_t(c.key_slices) * ((p.nk + kRowsBlock - 1) / kRowsBlock);
+    p.key_tiles = (p.nk + kKeysBlock - 1) / kKeysBlock;
+    if (c.bias) p.key_window = int(bias_window(64, kKeysBlock, c.g.Hk, c.g.Wk));
+    const int64_t tiles = int64_t(c.key_slices) * p.key_tiles;
     // splits of the queries: fewer than two blocks per CU leave CUs idle, and a part is worth a block from four tiles on
     const int64_t rows = int64_t(p.share) * ((p.nq + 63) / 64);
     int64_t n = 512 / tiles;
     if (n > rows / 4) n = rows / 4;
-    p.splits = n < 1 ? 1 : static_cast<int>(n);
-    plan.key_blocks = tiles * p.splits;
+    p.key_splits = n < 1 ? 1 : int(n);
+    plan.key_blocks = tiles * p.key_splits;
     plan.stats = round256(size_t(c.g.S) * p.nq * sizeof(float4));
-    plan.part = p.splits > 1 ? round256(size_t(p.splits) * p.all_keys * 2 * c.g.d * sizeof(float)) : 0;
+    plan.part = p.key_splits > 1 ? round256(size_t(p.key_splits) * p.all_keys * 2 * c.g.d * sizeof(float)) : 0;
     if (c.bias) {
+        p.x_tiles = (c.g.Wk + 31) / 32;
         // four runs of grid rows for the waves of a block at least
         const int64_t columns = int64_t(c.g.S / c.bias_rows) * (p.x_tiles > 1 ? p.x_tiles - 1 : 1);
         p.cuts = columns >= 4 || c.g.Hk < 8 ? 1 : 4;
@@ -633,18 +603,20 @@ BackwardPlan backward_plan(const DenseCall& c)
     return plan;
 }
 
+int elem_bytes_of(int dtype) { return dtype == SCRAM_BF16 ? 2 : 4; }
+
 }  // namespace
 
-size_t dense_backward_workspace_bytes(const DenseCall& c)
+size_t dense_backward_workspace_bytes(int dtype, const DenseCall& c)
 {
-    const BackwardPlan plan = backward_plan(c);
+    const BackwardPlan plan = backward_plan(c, elem_bytes_of(dtype));
     return plan.stats + plan.part + plan.diagonals;
 }
 
-uint64_t dense_backward_blocks(const DenseCall& c)
+uint64_t dense_backward_blocks(int dtype, const DenseCall& c)
 {
-    const BackwardPlan plan = backward_plan(c);
-    uint64_t most = plan.query_blocks;
+    const BackwardPlan plan = backward_plan(c, elem_bytes_of(dtype));
+    uint64_t most = 2 * uint64_t(plan.queries.blocks);
     if (uint64_t(plan.key_blocks) > most) most = plan.key_blocks;
     return uint64_t(plan.offset_blocks) > most ? plan.offset_blocks : most;
 }
@@ -652,8 +624,8 @@ uint64_t dense_backward_blocks(const DenseCall& c)
 hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, void* dQ, void* dK, void* dV, void* dbias,
                                  void* workspace, hipStream_t stream, hipEvent_t start, hipEvent_t stop)
 {
-    const BackwardPlan plan = backward_plan(c);
-    DenseBackward p = plan.p;
+    BackwardPlan plan = backward_plan(c, elem_bytes_of(dtype));
+    DenseBackward& p = plan.p;
     p.dO = dO;
     p.dQ = dQ;
     p.dK = dK;
@@ -663,32 +635,32 @@ hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, 
     p.stats = reinterpret_cast<float4*>(ws);
     p.part = reinterpret_cast<float*>(ws + plan.stats);
     p.diagonals = reinterpret_cast<float*>(ws + plan.stats + plan.part);
-    const int window = c.bias ? static_cast<int>(dense_bias_window(c.g.Hk, c.g.Wk)) : 0;
     return dispatch_value(dtype, c.g.d, hipErrorInvalidValue, [&](auto type, auto width) {
         using T = std::conditional_t<std::is_same<decltype(type), float>::value, float, uint16_t>;
         constexpr int D = decltype(width)::value;
-        const size_t lds = backward_lds<T, D>() + (c.bias ? (kStaged<T, D> + window) * sizeof(float) : 0);
-        DenseBackward a = p;
-        a.tiles = static_cast<int>(plan.query_blocks / p.groups);
-        hipError_t e = c.bias ? launch_dense_kernel(dense_query_kernel<T, D, true>, plan.query_blocks, lds, stream, start, nullptr, a)
-                              : launch_dense_kernel(dense_query_kernel<T, D, false>, plan.query_blocks, lds, stream, start, nullptr, a);
+        hipError_t e = query_dispatch<T, D>(c.bias, plan.queries.key_waves, [&](auto biased, auto key_waves) {
+            constexpr int KW = decltype(key_waves)::value;
+            constexpr bool kBiased = decltype(biased)::value;
+            return launch_dense_kernel<kQueryThreads>(dense_query_kernel<T, D, kBiased, KW>, plan.queries.blocks,
+                                                      query_block_lds<T, D, kBiased, KW>(p), stream, start, nullptr, p);
+        });
         if (e != hipSuccess) return e;
-        a.tiles = (p.nk + kRowsBlock - 1) / kRowsBlock;
-        hipEvent_t end = p.splits == 1 && !dbias ? stop : nullptr;
-        e = c.bias ? launch_dense_kernel(dense_key_kernel<T, D, true>, plan.key_blocks, lds, stream, nullptr, end, a)
-                   : launch_dense_kernel(dense_key_kernel<T, D, false>, plan.key_blocks, lds, stream, nullptr, end, a);
+        const hipEvent_t end = p.key_splits == 1 && !dbias ? stop : nullptr;
+        const size_t lds = key_lds<T, D>(p, c.bias);
+        e = c.bias ? launch_dense_kernel(dense_key_kernel<T, D, true>, plan.key_blocks, lds, stream, nullptr, end, p)
+                   : launch_dense_kernel(dense_key_kernel<T, D, false>, plan.key_blocks, lds, stream, nullptr, end, p);
         if (e != hipSuccess) return e;
-        if (p.splits > 1) {
+        if (p.key_splits > 1) {
             e = launch_dense_kernel(dense_key_join_kernel<T, D>, (p.all_keys * (D / 2) + kBlock - 1) / kBlock, 0, stream, nullptr,
-                                    dbias ? nullptr : stop, a);
+                                    dbias ? nullptr : stop, p);
             if (e != hipSuccess) return e;
         }
         if (!dbias) return hipSuccess;
         const int64_t offsets = int64_t(p.plane.rows) * ((2 * p.Hk - 1 + kOffsetRows<T, D> - 1) / kOffsetRows<T, D>) * (2 * p.x_tiles - 1);
-        e = launch_dense_kernel(dense_offset_kernel<T, D>, offsets, 0, stream, nullptr, nullptr, a);
+        e = launch_dense_kernel(dense_offset_kernel<T, D>, offsets, 0, stream, nullptr, nullptr, p);
         if (e != hipSuccess) return e;
         const int64_t blocks = (p.plane.rows * p.plane.size + kBlock - 1) / kBlock;
-        return launch_dense_kernel(dense_offset_join_kernel<T>, blocks < 8192 ? blocks : 8192, 0, stream, nullptr, stop, a);
+        return launch_dense_kernel(dense_offset_join_kernel<T>, blocks < 8192 ? blocks : 8192, 0, stream, nullptr, stop, p);
     });
 }
 

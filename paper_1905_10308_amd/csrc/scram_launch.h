@@ -98,14 +98,14 @@ struct DenseCall {
     int first;               // causal or with a bias: raster index of a slice's first query among its keys
     const int32_t* origin;   // the same per slice, on the device (null: first)
 };
-constexpr int kBiasWindowMost = 12288;  // most places of a bias' plane that a block holds at once
+constexpr int kBiasWindowMost = 10240;  // most places of a bias' plane that a block holds at once
 int64_t dense_bias_window(int Hk, int Wk);
 size_t dense_workspace_bytes(int dtype, const DenseCall& c);
 uint64_t dense_blocks(int dtype, const DenseCall& c);
 hipError_t launch_dense(int dtype, const DenseCall& c, void* out, void* workspace, hipStream_t stream, hipEvent_t start,
                         hipEvent_t stop);
-size_t dense_backward_workspace_bytes(const DenseCall& c);
-uint64_t dense_backward_blocks(const DenseCall& c);
+size_t dense_backward_workspace_bytes(int dtype, const DenseCall& c);
+uint64_t dense_backward_blocks(int dtype, const DenseCall& c);
 hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, void* dQ, void* dK, void* dV, void* dbias,
                                  void* workspace, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
 
