@@ -53,17 +53,25 @@ struct DenseParams {
     float scale, scale2;     // the softmax's temperature, and in base 2
 };
 
-// Rows of D elements of T in LDS, kPad bytes apart.
+// Rows of D elements of T.  In LDS they lie side by side, each row's 16-byte chunks in an order of its own (chunk c of row r at
+// place c ^ order(r)), so that sixteen rows' chunks c, and four rows' chunks 4 k .. 4 k + 3, lie in different banks.
 template <typename T, int D>
 struct DenseRow {
     static constexpr int kBytes = D * static_cast<int>(sizeof(T));
-    static constexpr int kStride = kBytes + 16;             // 16 lanes' vectors of 16 bytes then lie in different banks
     static constexpr int kChunks = kBytes / 16;
     static constexpr int kSteps = kBytes / 32;              // steps of a product's inner index over the channels
     static constexpr int kInner = 32 / static_cast<int>(sizeof(T));  // that a step takes: 16 (bf16) or 8
     static constexpr int kRowSteps = 32 / kInner;           // steps of a product whose inner index runs over a tile's 32 rows
     static constexpr int kColumns = D < 32 ? 1 : D / 32;    // tiles of 32 channels (of 16: half of one)
-    static constexpr int kSlack = 64 * static_cast<int>(sizeof(T));  // bytes that transposed reads may pass the last row by
+
+    static __device__ __forceinline__ int order(int r)
+    {
+        if constexpr (kChunks == 2) return (r >> 3) & 1;
+        if constexpr (kChunks == 4) return (r >> 2) & 3;
+        if constexpr (kChunks == 8) return ((r & 2) << 1) | ((r >> 2) & 3);
+        return ((r & 3) << 2) | ((r >> 2) & 3);
+    }
+    static __device__ __forceinline__ int place(int r, int c) { return r * kBytes + 16 * (c ^ order(r)); }
 };
 
 // The wave's place in its block, as a number that the compiler knows to be the same for all lanes.
@@ -125,63 +133,68 @@ __device__ __forceinline__ uint4 as_operand(const f32x16_t& x, int s)
 template <typename T, int D>
 __device__ __forceinline__ uint4 row_operand(const unsigned char* tile, int row, int h, int s)
 {
-    return *reinterpret_cast<const uint4*>(tile + row * DenseRow<T, D>::kStride + 32 * s + 16 * h);
+    return *reinterpret_cast<const uint4*>(tile + DenseRow<T, D>::place(row, 2 * s + h));
 }
 
-// Left operand of a product whose inner index runs over staged rows (row0 on, step s of 32 of them) and whose rows are channels
-// 32 o .. 32 o + 31.  bf16: the transposing load hands lane i of each 16 the element e of the 8 bytes that lane 4 e + i / 4
-// addresses.
+// Left operand of a product whose inner index runs over staged rows (row0 on, a multiple of 32; step s of 32 of them) and whose
+// rows are channels 32 o .. 32 o + 31 (of 16 channels: each twice).  bf16: the transposing load hands lane i of each 16 the
+// element e of the 8 bytes that lane 4 e + i / 4 addresses.
 template <typename T, int D>
 __device__ __forceinline__ uint4 column_operand(const unsigned char* tile, int row0, int s, int o)
 {
     using R = DenseRow<T, D>;
     const int lane = threadIdx.x & 63, h = lane >> 5;
     if constexpr (sizeof(T) == 2) {
-        const int i = lane & 15;
-        const unsigned char* const at =
-            tile + (row0 + 16 * s + 8 * h + (i >> 2)) * R::kStride + 64 * o + 2 * (lane & 16) + 8 * (i & 3);
+        const int i = lane & 15, r = 8 * h + (i >> 2);
+        const int c = 4 * o + (D < 32 ? 0 : (lane & 16) >> 3) + ((i & 2) >> 1);
+        const unsigned char* const at = tile + (row0 + 16 * s) * R::kBytes + 8 * (i & 1);
         using lds_v4 = __attribute__((address_space(3))) bf16x4_t*;
-        const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(at));
-        const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(at + 4 * R::kStride));
+        const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(at + R::place(r, c)));
+        const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(at + R::place(r + 4, c)));
         return __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
+        const int c = 8 * o + ((lane & (D < 32 ? 15 : 31)) >> 2), r = 8 * (s & 1) + 4 * h;
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            w[j] = *reinterpret_cast<const uint32_t*>(tile + (row0 + 8 * s + 4 * h + j) * R::kStride + 128 * o + 4 * (lane & 31));
+            w[j] = *reinterpret_cast<const uint32_t*>(tile + (row0 + 8 * (s & ~1)) * R::kBytes + R::place(r + j, c) + 4 * (lane & 3));
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
-// N rows of a tile on their way from memory to LDS, in the registers of a block of THREADS threads; the rows from `live` (> 0)
-// on are row live - 1 again, whose products count nowhere.
+// N rows of a tile on their way from memory to LDS, past the registers of a block of THREADS threads: a wave's load writes its
+// lanes' 16 bytes one after another from the place in m0 on, so the order of a row's chunks is that in which lanes fetch them.
+// The rows from `live` (> 0) on are row live - 1 again, whose products count nowhere.  Issued in assembly, since for the
+// builtin the compiler would wait for the rows on their way before it reads any others; wait() waits for them, and for the
+// other waves' a barrier.  (m0 has no other use in these kernels.)
 template <typename T, int D, int N, int THREADS>
 struct DenseStage {
     using R = DenseRow<T, D>;
-    static constexpr int kTotal = N * R::kChunks;
-    static constexpr int kEach = (kTotal + THREADS - 1) / THREADS;
-    typedef uint32_t words __attribute__((ext_vector_type(4)));
-    words x[kEach];
+    static constexpr int kTotal = N * R::kBytes / 1024;  // loads of a wave
+    static constexpr int kWaves = THREADS / 64, kEach = (kTotal + kWaves - 1) / kWaves;
+    static_assert(N * R::kBytes % 1024 == 0, "whole loads");
 
-    __device__ __forceinline__ void load(const void* rows, int64_t row0, int live)
+    static __device__ __forceinline__ uint32_t offset(int load, int live)
+    {
+        const int i = load * 64 + static_cast<int>(threadIdx.x & 63), r = i / R::kChunks;
+        return min(r, live - 1) * R::kBytes + 16 * ((i % R::kChunks) ^ R::order(r));
+    }
+    static __device__ __forceinline__ void load(const void* rows, int64_t row0, int live, unsigned char* tile)
     {
         const unsigned char* const from = static_cast<const unsigned char*>(rows) + row0 * R::kBytes;
+        const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)(tile)));
+        const int wave = wave_index();
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int c = i * THREADS + static_cast<int>(threadIdx.x);
-            const uint32_t at = min(c / R::kChunks, live - 1) * R::kBytes + 16 * (c % R::kChunks);
-            x[i] = *reinterpret_cast<const words*>(from + at);
+        for (int j = 0; j < kEach; ++j) {
+            const int load = j * kWaves + wave;
+            if (kTotal % kWaves == 0 || load < kTotal)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                             :
+                             : "s"(to + 1024u * load), "v"(offset(load, live)), "s"(from)
+                             : "memory");
         }
     }
-    __device__ __forceinline__ void store(unsigned char* tile) const
-    {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int c = i * THREADS + static_cast<int>(threadIdx.x);
-            if (kTotal % THREADS == 0 || c < kTotal)
-                *reinterpret_cast<words*>(tile + c / R::kChunks * R::kStride + 16 * (c % R::kChunks)) = x[i];
-        }
-    }
+    static __device__ __forceinline__ void wait() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 };
 
 // A row of D elements as the right operand of products over its channels.
@@ -276,14 +289,14 @@ constexpr int kWaveKeys = wave_keys(D * sizeof(T), KW);
 
 // Bytes of a step's rows in LDS.
 template <typename T, int D, int KW>
-constexpr size_t kTileBytes = 2 * (KW * kWaveKeys<T, D, KW> * DenseRow<T, D>::kStride);
+constexpr size_t kTileBytes = 2 * (KW * kWaveKeys<T, D, KW> * DenseRow<T, D>::kBytes);
 
 // Bytes of LDS before the bias': the staged rows, and after them what the waves of the same queries join.
 template <typename T, int D, int KW>
 __host__ __device__ constexpr size_t query_lds(int buffers)
 {
     using R = DenseRow<T, D>;
-    const size_t tiles = buffers * kTileBytes<T, D, KW> + R::kSlack;
+    const size_t tiles = buffers * kTileBytes<T, D, KW>;
     constexpr size_t join = 8 * 64 * sizeof(float) * (16 * R::kColumns + 2);
     return tiles > join ? tiles : join;
 }
@@ -328,7 +341,7 @@ struct QueryBlock {
     float scale2;
     int my_at, my_end, my_place;
     int q0, q1, my_window, my_thread, my_threads;
-    DenseStage<T, D, kKeys, kQueryThreads> kl, vl;
+    using Stage = DenseStage<T, D, kKeys, kQueryThreads>;
     BiasStage<T> bl;
 
     __device__ __forceinline__ int begin_of(int slice) const { return p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first; }
@@ -404,27 +417,29 @@ struct QueryBlock {
         if (scale2 == 0.f) scale2 = 1e-37f;  // (a key that is not seen has a score of minus infinity, and a weight of 0 by it)
     }
 
+    // The rows of step t, on their way to their buffer.
     __device__ __forceinline__ void fetch(int t)
     {
         const int k0 = t * kKeys;
         const int64_t k_row = static_cast<int64_t>(slice_k) * p.nk + k0;
-        kl.load(p.K, k_row, last - k0);
-        vl.load(p.V, k_row, last - k0);
+        unsigned char* const tiles = lds + (p.buffers > 1 ? t & 1 : 0) * kTileBytes<T, D, KW>;
+        Stage::load(p.K, k_row, last - k0, tiles);
+        Stage::load(p.V, k_row, last - k0, tiles + kKeys * R::kBytes);
+    }
+    // The bias of step t: from memory, and to LDS.
+    __device__ __forceinline__ void fetch_bias(int t)
+    {
         if constexpr (BIAS) {
             if (my_window < p.per_group) {
-                const int slice = group * p.per_group + my_window, begin = begin_of(slice);
+                const int slice = group * p.per_group + my_window, begin = begin_of(slice), k0 = t * kKeys;
                 bl.load(p, slice % p.plane.rows, begin + q0, begin + q1, k0, min(k0 + kKeys, p.nk) - 1, my_thread, my_threads);
             }
         }
     }
-    __device__ __forceinline__ void store(int t)
+    __device__ __forceinline__ void store_bias(int t)
     {
-        const int at = p.buffers > 1 ? t & 1 : 0;
-        unsigned char* const tiles = lds + at * kTileBytes<T, D, KW>;
-        kl.store(tiles);
-        vl.store(tiles + kKeys * R::kStride);
         if constexpr (BIAS) {
-            int* const places = s_places + at * bias_floats;
+            int* const places = s_places + (p.buffers > 1 ? t & 1 : 0) * bias_floats;
             if (my_window < p.per_group)
                 bl.store(reinterpret_cast<float*>(places + kKeys) + my_window * p.window, my_thread, my_threads);
             const int k0 = t * kKeys, k1 = min(k0 + kKeys, p.nk) - 1;
@@ -438,18 +453,26 @@ struct QueryBlock {
     {
         if (t0 < t1) {
             fetch(t0);
-            store(t0);
+            fetch_bias(t0);
+            store_bias(t0);
         }
+        Stage::wait();
         __syncthreads();
         for (int t = t0; t < t1; ++t) {
             const int k0 = t * kKeys + kw * kEach, at = p.buffers > 1 ? t & 1 : 0;
-            if (t + 1 < t1) fetch(t + 1);
+            const bool more = t + 1 < t1;
+            if (more && p.buffers > 1) fetch(t + 1);
+            if (more) fetch_bias(t + 1);
             if constexpr (BIAS) my_place = 4 * (my_at + bias_place(p, t * kKeys) - my_end);
             const int steps = min(kEach, most_keys - k0);
 #pragma unroll 1
             for (int u = 0; u < steps; u += 32) step(lds + at * kTileBytes<T, D, KW>, s_places + at * bias_floats, k0 + u, kw * kEach + u);
-            if (p.buffers == 1) __syncthreads();
-            if (t + 1 < t1) store(t + 1);
+            if (p.buffers == 1) {
+                __syncthreads();
+                if (more) fetch(t + 1);
+            }
+            if (more) store_bias(t + 1);
+            Stage::wait();
             __syncthreads();
         }
     }
@@ -459,7 +482,7 @@ struct QueryBlock {
     {
         f32x16_t s(0.f);
 #pragma unroll
-        for (int c = 0; c < R::kSteps; ++c) s = mma<T>(row_operand<T, D>(rows, from + tile_row<T>(m), h, c), x[c], s);
+        for (int c = 0; c < R::kSteps; ++c) s = mma<T>(row_operand<T, D>(rows + from * R::kBytes, tile_row<T>(m), h, c), x[c], s);
         return s;
     }
     // The scores of products s in base 2 (RAW: before the scale), minus infinity where a key is not seen.
@@ -493,7 +516,7 @@ inline QueryPlan query_plan(const DenseCall& c, int elem_bytes, bool split, Dens
     auto room = [&](int kw, int slices, int buffers) {
         const int64_t keys = kw * wave_keys(bytes, kw), rows = 256 / kw;
         const int64_t windows = c.bias ? slices * bias_window(int(rows), int(keys), c.g.Hk, c.g.Wk) + keys : 0;
-        return buffers * (2 * keys * (bytes + 16) + 4 * windows) + 6144 <= 160 * 1024;
+        return buffers * (2 * keys * bytes + 4 * windows) + 6144 <= 160 * 1024;
     };
     // a tile that holds the queries of all slices of a key slice, each with a window
     const bool together = c.bias && p.share > 1 && int64_t(p.share) * p.nq <= 32 && p.share <= 16 && bytes <= 256 && room(8, p.share, 1);

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && D * 
                 const uint4 w = as_operand<T>(s, r);
 #pragma unroll
                 for (int c = 0; c < R::kColumns; ++c)
-                    o[c] = mma<T>(column_operand<T, D>(rows + q.kKeys * R::kStride, from, r, c), w, o[c]);
+                    o[c] = mma<T>(column_operand<T, D>(rows + q.kKeys * R::kBytes, from, r, c), w, o[c]);
             }
         });
         if (pass == 1) break;

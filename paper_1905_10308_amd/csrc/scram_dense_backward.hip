@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBack
     float top = -INFINITY, sum = 0.f, dsum = 0.f;
     q.pass([&](const unsigned char* rows, const int* places, int k0, int from) {
         f32x16_t s = q.products(rows, from, qf);
-        const f32x16_t g = q.products(rows + q.kKeys * R::kStride, from, gf);
+        const f32x16_t g = q.products(rows + q.kKeys * R::kBytes, from, gf);
         q.template scores<false>(s, places, k0, from);
         float most = top;
 #pragma unroll
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBack
     for (int c = 0; c < R::kColumns; ++c) o[c] = f32x16_t(0.f);
     q.pass([&](const unsigned char* rows, const int* places, int k0, int from) {
         f32x16_t s = q.products(rows, from, qf);
-        const f32x16_t g = q.products(rows + q.kKeys * R::kStride, from, gf);
+        const f32x16_t g = q.products(rows + q.kKeys * R::kBytes, from, gf);
         q.template scores<kFold>(s, places, k0, from);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -154,12 +154,12 @@ __global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBack
 template <typename T, int D>
 constexpr int kStaged = D * sizeof(T) > 256 ? 32 : 64;
 template <typename T, int D>
-constexpr size_t kKeyTile = 2 * (kStaged<T, D> * DenseRow<T, D>::kStride);
+constexpr size_t kKeyTile = 2 * (kStaged<T, D> * DenseRow<T, D>::kBytes);
 
 template <typename T, int D>
 size_t key_lds(const DenseBackward& p, bool biased)
 {
-    return 2 * kKeyTile<T, D> + DenseRow<T, D>::kSlack + 2 * sizeof(float) * (3 * kStaged<T, D> + (biased ? kStaged<T, D> + p.key_window : 0)) + 64;
+    return 2 * kKeyTile<T, D> + 2 * sizeof(float) * (3 * kStaged<T, D> + (biased ? kStaged<T, D> + p.key_window : 0)) + 64;
 }
 
 // The key side: a block's 128 keys against a run of the query tiles of the slices that read them.
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
     constexpr int kRows = kStaged<T, D>, U = kRows / 32;
     extern __shared__ __align__(16) unsigned char lds[];
     // of each of two steps: logarithms, factors and means of the queries' softmax, their places, the bias' window
-    float* const s_stats = reinterpret_cast<float*>(lds + 2 * kKeyTile<T, D> + R::kSlack);
+    float* const s_stats = reinterpret_cast<float*>(lds + 2 * kKeyTile<T, D>);
     const int stats_floats = 3 * kRows + (BIAS ? kRows + p.key_window : 0);
 
     const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
@@ -219,15 +219,15 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
             }
         return t;
     };
-    DenseStage<T, D, kRows, kBlock> ql, gl;
+    using Stage = DenseStage<T, D, kRows, kBlock>;
     BiasStage<T> bl;
     float4 st = make_float4(INFINITY, 1.f, 0.f, 0.f);
     int next_at = 0, next_end = 0, next_place = 0;  // of the fetched tile: place of its first query; places on the bias' plane
-    auto fetch = [&](int t) {
+    auto fetch = [&](int t, int at) {
         const int slice = slice_k * p.share + t / per_slice, q0 = t % per_slice * kRows, begin = begin_of(slice);
         const int64_t row = static_cast<int64_t>(slice) * p.nq + q0;
-        ql.load(p.Q, row, p.nq - q0);
-        gl.load(p.dO, row, p.nq - q0);
+        Stage::load(p.Q, row, p.nq - q0, lds + at * kKeyTile<T, D>);
+        Stage::load(p.dO, row, p.nq - q0, lds + at * kKeyTile<T, D> + kRows * R::kBytes);
         const int q = static_cast<int>(threadIdx.x);
         st = make_float4(INFINITY, 1.f, 0.f, 0.f);
         if (q < kRows && q0 + q < p.nq) st = p.stats[row + q];
@@ -241,8 +241,6 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
     };
     bool apart = false;
     auto store = [&](int at) {
-        ql.store(lds + at * kKeyTile<T, D>);
-        gl.store(lds + at * kKeyTile<T, D> + kRows * R::kStride);
         float* const stats = s_stats + at * stats_floats;
         const int q = static_cast<int>(threadIdx.x);
         if (q < kRows) {
@@ -256,19 +254,20 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
     };
     int t = seek(t0), at = 0;
     if (t < t1) {
-        fetch(t);
+        fetch(t, 0);
         apart = store(0);
     }
+    Stage::wait();
     apart = __syncthreads_or(apart);
     while (t < t1) {
         const int at0 = next_at;  // place of the tile's first query
         // 4 (place of the key, less the window's start)
         const int my_place = 4 * (key_place - (first_place - next_end));
         const unsigned char* const q_tile = lds + at * kKeyTile<T, D>;
-        const unsigned char* const g_tile = q_tile + kRows * R::kStride;
+        const unsigned char* const g_tile = q_tile + kRows * R::kBytes;
         const float* const stats = s_stats + at * stats_floats;
         t = seek(t + 1);
-        if (t < t1) fetch(t);
+        if (t < t1) fetch(t, at ^ 1);
         // a query after which some key of the wave's comes, or a key that is not seen
         const bool masked = (p.causal && at0 < k_wave + 31) || k_wave + 32 > length;
 #pragma unroll 1
@@ -277,8 +276,8 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
             f32x16_t s(0.f), g(0.f);
 #pragma unroll
             for (int c = 0; c < R::kSteps; ++c) {
-                s = mma<T>(row_operand<T, D>(q_tile, 32 * u + tile_row<T>(m), h, c), kf[c], s);
-                g = mma<T>(row_operand<T, D>(g_tile, 32 * u + tile_row<T>(m), h, c), vf[c], g);
+                s = mma<T>(row_operand<T, D>(q_tile + 32 * u * R::kBytes, tile_row<T>(m), h, c), kf[c], s);
+                g = mma<T>(row_operand<T, D>(g_tile + 32 * u * R::kBytes, tile_row<T>(m), h, c), vf[c], g);
             }
             const int row0 = 32 * u + tile_half<T>() * h;
             f32x16_t w;
@@ -316,6 +315,7 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
         }
         at ^= 1;
         apart = t < t1 ? store(at) : false;
+        Stage::wait();
         apart = __syncthreads_or(apart);
     }
     if (key >= p.nk) return;
@@ -381,18 +381,18 @@ template <typename T, int D>
 struct WaveTile {
     using R = DenseRow<T, D>;
     static constexpr int kEach = R::kChunks / 2;
-    static constexpr int kBytes = 32 * R::kStride;
-    uint4 x[kEach];
+    static constexpr int kBytes = 32 * R::kBytes;
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    words x[kEach];
 
-    // rows first .. last - 1 of the tile that begins at `row0`; the others are zeros
+    // rows first .. last - 1 (one at least) of the tile that begins at `row0`; those before and after them are its ends again
     __device__ __forceinline__ void load(const void* rows, int64_t row0, int first, int last)
     {
         const unsigned char* const from = static_cast<const unsigned char*>(rows) + row0 * R::kBytes;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int c = i * 64 + static_cast<int>(threadIdx.x & 63), r = c / R::kChunks;
-            x[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r >= first && r < last) x[i] = *reinterpret_cast<const uint4*>(from + 16 * c);
+            const int c = i * 64 + static_cast<int>(threadIdx.x & 63);
+            x[i] = *reinterpret_cast<const words*>(from + min(max(c / R::kChunks, first), last - 1) * R::kBytes + 16 * (c % R::kChunks));
         }
     }
     // the operands of row `row` for this lane
@@ -402,7 +402,7 @@ struct WaveTile {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int c = i * 64 + static_cast<int>(threadIdx.x & 63);
-            *reinterpret_cast<uint4*>(tile + c / R::kChunks * R::kStride + 16 * (c % R::kChunks)) = x[i];
+            *reinterpret_cast<words*>(tile + R::place(c / R::kChunks, c % R::kChunks)) = x[i];
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -455,6 +455,7 @@ __global__ __launch_bounds__(kBlock, 2) void dense_offset_kernel(DenseBackward p
         auto keys = [&](int ky, uint4 (&k)[R::kSteps], uint4 (&v)[R::kSteps]) {
             const int key = ky * W + kx0;
             const int last = ky >= 0 && ky < p.Hk ? min(min(32, W - kx0), length - key) : 0;
+            if (last <= 0) return;  // (a row that no pair is taken with)
             WaveTile<T, D> kl, vl;
             kl.load(p.K, k_row + key, 0, last);
             vl.load(p.V, k_row + key, 0, last);
@@ -468,17 +469,19 @@ __global__ __launch_bounds__(kBlock, 2) void dense_offset_kernel(DenseBackward p
             constexpr int kAt = decltype(at)::value;
             const int q = qy * W + qx - begin;
             const bool q_ok = qx < W && q >= 0 && q < p.nq;
+            keys(qy + dy0 + N - 1, kf[(kAt + N - 1) % N], vf[(kAt + N - 1) % N]);
+            const int q0 = qy * W + qx0 - begin, q_first = max(0, -q0), q_last = min(min(32, W - qx0), p.nq - q0);
+            if (q_first >= q_last) return;  // none of the run's queries
             const float4 st = q_ok ? p.stats[q_row + q] : make_float4(INFINITY, 1.f, 0.f, 0.f);
+            const bool apart_sums = __any(st.y != 1.f);
             uint4 qf[R::kSteps], gf[R::kSteps];
             {
-                const int q0 = qy * W + qx0 - begin;
                 WaveTile<T, D> ql, gl;
-                ql.load(p.Q, q_row + q0, -q0, min(min(32, W - qx0), p.nq - q0));
-                gl.load(p.dO, q_row + q0, -q0, min(min(32, W - qx0), p.nq - q0));
+                ql.load(p.Q, q_row + q0, q_first, q_last);
+                gl.load(p.dO, q_row + q0, q_first, q_last);
                 ql.turn(s_turn[wave], m, qf);
                 gl.turn(s_turn[wave], m, gf);
             }
-            keys(qy + dy0 + N - 1, kf[(kAt + N - 1) % N], vf[(kAt + N - 1) % N]);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const int ky = qy + dy0 + j, dy = dy0 + j;
@@ -510,7 +513,14 @@ __global__ __launch_bounds__(kBlock, 2) void dense_offset_kernel(DenseBackward p
                         g[i] = on ? g[i] : 0.f;
                     }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum[j][i] = fmaf(__builtin_amdgcn_exp2f(s[i] - st.x) * st.y, g[i], sum[j][i]);
+                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] - st.x);
+                if (apart_sums) {
+                    asm volatile("");
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] *= st.y;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[j][i] = fmaf(s[i], g[i], sum[j][i]);
             }
         };
         if (low > high || from > to) continue;
