@@ -136,31 +136,60 @@ __device__ __forceinline__ uint4 row_operand(const unsigned char* tile, int row,
     return *reinterpret_cast<const uint4*>(tile + DenseRow<T, D>::place(row, 2 * s + h));
 }
 
-// Left operand of a product whose inner index runs over staged rows (row0 on, a multiple of 32; step s of 32 of them) and whose
-// rows are channels 32 o .. 32 o + 31 (of 16 channels: each twice).  bf16: the transposing load hands lane i of each 16 the
-// element e of the 8 bytes that lane 4 e + i / 4 addresses.
+using lds_bytes = __attribute__((address_space(3))) const unsigned char*;
+
+// A lane's places in 32 staged rows, kept for all the tiles that it reads: `at` is the bytes of a tile behind the first.
 template <typename T, int D>
-__device__ __forceinline__ uint4 column_operand(const unsigned char* tile, int row0, int s, int o)
-{
+struct TileReader {
     using R = DenseRow<T, D>;
-    const int lane = threadIdx.x & 63, h = lane >> 5;
-    if constexpr (sizeof(T) == 2) {
-        const int i = lane & 15, r = 8 * h + (i >> 2);
-        const int c = 4 * o + (D < 32 ? 0 : (lane & 16) >> 3) + ((i & 2) >> 1);
-        const unsigned char* const at = tile + (row0 + 16 * s) * R::kBytes + 8 * (i & 1);
-        using lds_v4 = __attribute__((address_space(3))) bf16x4_t*;
-        const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(at + R::place(r, c)));
-        const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(at + R::place(r + 4, c)));
-        return __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    } else {
-        const int c = 8 * o + ((lane & (D < 32 ? 15 : 31)) >> 2), r = 8 * (s & 1) + 4 * h;
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            w[j] = *reinterpret_cast<const uint32_t*>(tile + (row0 + 8 * (s & ~1)) * R::kBytes + R::place(r + j, c) + 4 * (lane & 3));
-        return make_uint4(w[0], w[1], w[2], w[3]);
+    using words = uint32_t __attribute__((ext_vector_type(4)));
+    lds_bytes base;
+    int row_x, column_x;  // places of a lane's first chunks in a tile; those of the others follow by exclusive or
+
+    __device__ __forceinline__ void set(const unsigned char* tile)
+    {
+        const int lane = threadIdx.x & 63, m = lane & 31, h = lane >> 5, i = lane & 15;
+        base = (lds_bytes)tile;
+        row_x = R::place(tile_row<T>(m), h);
+        column_x = R::place(8 * h + (i >> 2), (D < 32 ? 0 : (lane & 16) >> 3) + ((i & 2) >> 1)) + 8 * (i & 1);
     }
-}
+    // Keeps the compiler from holding every chunk's place in a register of its own throughout a loop, which spills.
+    __device__ __forceinline__ void renew()
+    {
+        asm volatile("" : "+v"(row_x));
+        if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(column_x));
+    }
+    // Left operand of products over the channels, step s: rows in the order of tile_row.
+    __device__ __forceinline__ uint4 row(int s, int at) const
+    {
+        using lds_words = __attribute__((address_space(3))) const words*;
+        return __builtin_bit_cast(uint4, *(lds_words)(base + (row_x ^ 32 * s) + at));
+    }
+    // Left operand of a product whose inner index runs over the rows (step s of 32 of them) and whose rows are channels 32 o ..
+    // 32 o + 31 (of 16 channels: each twice).  bf16: the transposing load hands lane i of each 16 the element e of the 8 bytes
+    // that lane 4 e + i / 4 addresses.
+    __device__ __forceinline__ uint4 column(int s, int o, int at) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            using lds_v4 = __attribute__((address_space(3))) bf16x4_t*;
+            constexpr int kFourDown = R::kChunks > 2 ? 16 : 0;  // how the order differs four rows further down
+            const lds_bytes from = base + (at + 16 * s * R::kBytes);
+            const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(from + (column_x ^ 64 * o)));
+            const bf16x4_t hi =
+                __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(from + ((column_x ^ 64 * o ^ kFourDown) + 4 * R::kBytes)));
+            return __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            using lds_word = __attribute__((address_space(3))) const uint32_t*;
+            const int lane = threadIdx.x & 63, h = lane >> 5;
+            const int c = 8 * o + ((lane & (D < 32 ? 15 : 31)) >> 2), r = 8 * (s & 1) + 4 * h;
+            const lds_bytes from = base + at + 8 * (s & ~1) * R::kBytes + 4 * (lane & 3);
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = *(lds_word)(from + R::place(r + j, c));
+            return make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+};
 
 // N rows of a tile on their way from memory to LDS, past the registers of a block of THREADS threads: a wave's load writes its
 // lanes' 16 bytes one after another from the place in m0 on, so the order of a row's chunks is that in which lanes fetch them.
@@ -182,7 +211,7 @@ struct DenseStage {
     static __device__ __forceinline__ void load(const void* rows, int64_t row0, int live, unsigned char* tile)
     {
         const unsigned char* const from = static_cast<const unsigned char*>(rows) + row0 * R::kBytes;
-        const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)(tile)));
+        const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_bytes)tile));
         const int wave = wave_index();
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
@@ -343,6 +372,8 @@ struct QueryBlock {
     int q0, q1, my_window, my_thread, my_threads;
     using Stage = DenseStage<T, D, kKeys, kQueryThreads>;
     BiasStage<T> bl;
+    TileReader<T, D> reader;  // of the wave's keys
+    static constexpr int kValues = kKeys * R::kBytes;  // bytes from a step's keys to its values
 
     __device__ __forceinline__ int begin_of(int slice) const { return p.origin ? min(max(p.origin[slice], 0), p.nk - p.nq) : p.first; }
 
@@ -390,6 +421,7 @@ struct QueryBlock {
         t0 = static_cast<int>(static_cast<int64_t>(all) * split / p.splits);
         t1 = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / p.splits);
         scale2 = p.scale2;
+        reader.set(lds + kw * kEach * R::kBytes);
         if constexpr (BIAS) {
             // a tile of several slices (whole ones then) has a window for each, which a share of the threads stages
             q0 = p.per_group == 1 ? tile * kRows : 0;
@@ -422,10 +454,11 @@ struct QueryBlock {
     {
         const int k0 = t * kKeys;
         const int64_t k_row = static_cast<int64_t>(slice_k) * p.nk + k0;
-        unsigned char* const tiles = lds + (p.buffers > 1 ? t & 1 : 0) * kTileBytes<T, D, KW>;
+        unsigned char* const tiles = lds + buffer(t) * kTileBytes<T, D, KW>;
         Stage::load(p.K, k_row, last - k0, tiles);
-        Stage::load(p.V, k_row, last - k0, tiles + kKeys * R::kBytes);
+        Stage::load(p.V, k_row, last - k0, tiles + kValues);
     }
+    __device__ __forceinline__ int buffer(int t) const { return p.buffers > 1 ? (t - t0) & 1 : 0; }
     // The bias of step t: from memory, and to LDS.
     __device__ __forceinline__ void fetch_bias(int t)
     {
@@ -439,7 +472,7 @@ struct QueryBlock {
     __device__ __forceinline__ void store_bias(int t)
     {
         if constexpr (BIAS) {
-            int* const places = s_places + (p.buffers > 1 ? t & 1 : 0) * bias_floats;
+            int* const places = s_places + buffer(t) * bias_floats;
             if (my_window < p.per_group)
                 bl.store(reinterpret_cast<float*>(places + kKeys) + my_window * p.window, my_thread, my_threads);
             const int k0 = t * kKeys, k1 = min(k0 + kKeys, p.nk) - 1;
@@ -447,10 +480,12 @@ struct QueryBlock {
         }
     }
 
-    // One pass: step(rows, places, k0, from) for every 32 keys of the wave's, keys k0 .. of the slice, staged at rows from ..
+    // One pass: step(at, places, from, k0) for every 32 keys of the wave's, keys k0 .. of the slice, staged `at` bytes behind what
+    // `reader` begins at, a constant; `places` are those of the step's keys, of which these are from ..
     template <typename F>
     __device__ __forceinline__ void pass(F&& step)
     {
+        const lds_bytes first_base = reader.base;
         if (t0 < t1) {
             fetch(t0);
             fetch_bias(t0);
@@ -459,14 +494,20 @@ struct QueryBlock {
         Stage::wait();
         __syncthreads();
         for (int t = t0; t < t1; ++t) {
-            const int k0 = t * kKeys + kw * kEach, at = p.buffers > 1 ? t & 1 : 0;
+            const int k0 = t * kKeys + kw * kEach;
             const bool more = t + 1 < t1;
             if (more && p.buffers > 1) fetch(t + 1);
             if (more) fetch_bias(t + 1);
             if constexpr (BIAS) my_place = 4 * (my_at + bias_place(p, t * kKeys) - my_end);
-            const int steps = min(kEach, most_keys - k0);
-#pragma unroll 1
-            for (int u = 0; u < steps; u += 32) step(lds + at * kTileBytes<T, D, KW>, s_places + at * bias_floats, k0 + u, kw * kEach + u);
+            const int* const places = s_places + buffer(t) * bias_floats;
+            reader.base = first_base + buffer(t) * static_cast<int>(kTileBytes<T, D, KW>);
+            reader.renew();
+            if (k0 < most_keys) step(std::integral_constant<int, 0>{}, places, kw * kEach, k0);
+            if constexpr (kEach == 64) {
+                __builtin_amdgcn_sched_barrier(0);  // (both at once would need more registers)
+                reader.renew();
+                if (k0 + 32 < most_keys) step(std::integral_constant<int, 32 * R::kBytes>{}, places, kw * kEach + 32, k0 + 32);
+            }
             if (p.buffers == 1) {
                 __syncthreads();
                 if (more) fetch(t + 1);
@@ -475,19 +516,20 @@ struct QueryBlock {
             Stage::wait();
             __syncthreads();
         }
+        reader.base = first_base;
     }
 
-    // Transposed products of the staged keys (rows from .. of the tile at `rows`) with a lane's row.
-    __device__ __forceinline__ f32x16_t products(const unsigned char* rows, int from, const uint4 (&x)[R::kSteps]) const
+    // Transposed products of 32 staged rows with a lane's row.
+    __device__ __forceinline__ f32x16_t products(int at, const uint4 (&x)[R::kSteps]) const
     {
         f32x16_t s(0.f);
 #pragma unroll
-        for (int c = 0; c < R::kSteps; ++c) s = mma<T>(row_operand<T, D>(rows + from * R::kBytes, tile_row<T>(m), h, c), x[c], s);
+        for (int c = 0; c < R::kSteps; ++c) s = mma<T>(reader.row(c, at), x[c], s);
         return s;
     }
-    // The scores of products s in base 2 (RAW: before the scale), minus infinity where a key is not seen.
+    // The scores of products s of the keys k0 .. (from .. of the step's) in base 2 (RAW: before the scale), minus infinity where a key is not seen.
     template <bool RAW>
-    __device__ __forceinline__ void scores(f32x16_t& s, const int* places, int k0, int from) const
+    __device__ __forceinline__ void scores(f32x16_t& s, const int* places, int from, int k0) const
     {
         if constexpr (BIAS)
             add_bias<T, 1>(s, scale2, reinterpret_cast<const float*>(places + kKeys), places + from, my_place, h, p.runs);

@@ -53,9 +53,10 @@ __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && D * 
         sum = 0.f;
         most = -INFINITY;
         bool first = pass == 0;
-        q.pass([&](const unsigned char* rows, const int* places, int k0, int from) {
-            f32x16_t s = q.products(rows, from, qf);
-            q.template scores<kFold>(s, places, k0, from);
+        q.pass([&](auto at, const int* places, int from, int k0) {
+            constexpr int kAt = decltype(at)::value;
+            f32x16_t s = q.products(kAt, qf);
+            q.template scores<kFold>(s, places, from, k0);
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i]);
             if (first) {
@@ -73,7 +74,7 @@ __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && D * 
                 const uint4 w = as_operand<T>(s, r);
 #pragma unroll
                 for (int c = 0; c < R::kColumns; ++c)
-                    o[c] = mma<T>(column_operand<T, D>(rows + q.kKeys * R::kBytes, from, r, c), w, o[c]);
+                    o[c] = mma<T>(q.reader.column(r, c, kAt + q.kValues), w, o[c]);
             }
         });
         if (pass == 1) break;

@@ -68,10 +68,11 @@ __global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBack
 
     // a lane's maximum, sum, and sum of dp: of its half of the keys
     float top = -INFINITY, sum = 0.f, dsum = 0.f;
-    q.pass([&](const unsigned char* rows, const int* places, int k0, int from) {
-        f32x16_t s = q.products(rows, from, qf);
-        const f32x16_t g = q.products(rows + q.kKeys * R::kBytes, from, gf);
-        q.template scores<false>(s, places, k0, from);
+    q.pass([&](auto at, const int* places, int from, int k0) {
+        constexpr int kAt = decltype(at)::value;
+        f32x16_t s = q.products(kAt, qf);
+        const f32x16_t g = q.products(kAt + q.kValues, gf);
+        q.template scores<false>(s, places, from, k0);
         float most = top;
 #pragma unroll
         for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i]);
@@ -113,10 +114,11 @@ __global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBack
     f32x16_t o[R::kColumns];
 #pragma unroll
     for (int c = 0; c < R::kColumns; ++c) o[c] = f32x16_t(0.f);
-    q.pass([&](const unsigned char* rows, const int* places, int k0, int from) {
-        f32x16_t s = q.products(rows, from, qf);
-        const f32x16_t g = q.products(rows + q.kKeys * R::kBytes, from, gf);
-        q.template scores<kFold>(s, places, k0, from);
+    q.pass([&](auto at, const int* places, int from, int k0) {
+        constexpr int kAt = decltype(at)::value;
+        f32x16_t s = q.products(kAt, qf);
+        const f32x16_t g = q.products(kAt + q.kValues, gf);
+        q.template scores<kFold>(s, places, from, k0);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             s[i] = __builtin_amdgcn_exp2f(kFold ? fmaf(s[i], scale2, -shift) : s[i] - shift) * (g[i] - mean);
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBack
         for (int r = 0; r < R::kRowSteps; ++r) {
             const uint4 w = as_operand<T>(s, r);
 #pragma unroll
-            for (int c = 0; c < R::kColumns; ++c) o[c] = mma<T>(column_operand<T, D>(rows, from, r, c), w, o[c]);
+            for (int c = 0; c < R::kColumns; ++c) o[c] = mma<T>(q.reader.column(r, c, kAt), w, o[c]);
         }
     });
     // the waves of the same queries: each joins a share of the channels
@@ -252,6 +254,10 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
         if constexpr (BIAS) bl.store(stats + 4 * kRows, q, kBlock);
         return st.y != 1.f;
     };
+    TileReader<T, D> reader;
+    reader.set(lds);
+    constexpr int kG = kRows * R::kBytes;
+    const lds_bytes first_base = reader.base;
     int t = seek(t0), at = 0;
     if (t < t1) {
         fetch(t, 0);
@@ -260,56 +266,60 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
     Stage::wait();
     apart = __syncthreads_or(apart);
     while (t < t1) {
+        reader.base = first_base + at * static_cast<int>(kKeyTile<T, D>);
         const int at0 = next_at;  // place of the tile's first query
         // 4 (place of the key, less the window's start)
         const int my_place = 4 * (key_place - (first_place - next_end));
-        const unsigned char* const q_tile = lds + at * kKeyTile<T, D>;
-        const unsigned char* const g_tile = q_tile + kRows * R::kBytes;
-        const float* const stats = s_stats + at * stats_floats;
+        const float* const stats = s_stats + at * stats_floats + tile_half<T>() * h;
+        const int t_now = t;
         t = seek(t + 1);
         if (t < t1) fetch(t, at ^ 1);
         // a query after which some key of the wave's comes, or a key that is not seen
         const bool masked = (p.causal && at0 < k_wave + 31) || k_wave + 32 > length;
-#pragma unroll 1
+#pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (p.causal && at0 + 32 * u + 31 < k_wave) continue;  // before the wave's keys
+            __builtin_amdgcn_sched_barrier(0);
+            reader.renew();
+            // nothing to add: queries before the wave's keys, or behind the slice's last
+            if ((p.causal && at0 + 32 * u + 31 < k_wave) || t_now % per_slice * kRows + 32 * u >= p.nq) continue;
             f32x16_t s(0.f), g(0.f);
 #pragma unroll
             for (int c = 0; c < R::kSteps; ++c) {
-                s = mma<T>(row_operand<T, D>(q_tile + 32 * u * R::kBytes, tile_row<T>(m), h, c), kf[c], s);
-                g = mma<T>(row_operand<T, D>(g_tile + 32 * u * R::kBytes, tile_row<T>(m), h, c), vf[c], g);
+                s = mma<T>(reader.row(c, 32 * u * R::kBytes), kf[c], s);
+                g = mma<T>(reader.row(c, kG + 32 * u * R::kBytes), vf[c], g);
             }
-            const int row0 = 32 * u + tile_half<T>() * h;
             f32x16_t w;
             if constexpr (BIAS) {
-                add_bias<T, -1>(s, p.scale2, stats + 4 * kRows, reinterpret_cast<const int*>(stats) + 3 * kRows + 32 * u, my_place, h, p.runs);
+                add_bias<T, -1>(s, p.scale2, s_stats + at * stats_floats + 4 * kRows,
+                                reinterpret_cast<const int*>(s_stats + at * stats_floats) + 3 * kRows + 32 * u, my_place, h, p.runs);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = s[i] - stats[row0 + tile_slot<T>(i)];
+                for (int i = 0; i < 16; ++i) w[i] = s[i] - stats[32 * u + tile_slot<T>(i)];
             } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = fmaf(s[i], p.scale2, -stats[row0 + tile_slot<T>(i)]);
+                for (int i = 0; i < 16; ++i) w[i] = fmaf(s[i], p.scale2, -stats[32 * u + tile_slot<T>(i)]);
             }
             if (masked) {
                 asm volatile("");  // (not for every tile, by selects)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = seen && (!p.causal || key <= at0 + row0 + tile_slot<T>(i)) ? w[i] : -INFINITY;
+                for (int i = 0; i < 16; ++i)
+                    w[i] = seen && (!p.causal || key <= at0 + 32 * u + tile_half<T>() * h + tile_slot<T>(i)) ? w[i] : -INFINITY;
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(w[i]);
             if (apart) {
                 asm volatile("");
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] *= stats[kRows + row0 + tile_slot<T>(i)];
+                for (int i = 0; i < 16; ++i) w[i] *= stats[kRows + 32 * u + tile_slot<T>(i)];
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = w[i] * (g[i] - stats[2 * kRows + row0 + tile_slot<T>(i)]);
+            for (int i = 0; i < 16; ++i) s[i] = w[i] * (g[i] - stats[2 * kRows + 32 * u + tile_slot<T>(i)]);
 #pragma unroll
             for (int r = 0; r < R::kRowSteps; ++r) {
                 const uint4 a = as_operand<T>(w, r), d = as_operand<T>(s, r);
 #pragma unroll
                 for (int c = 0; c < R::kColumns; ++c) {
-                    dv[c] = mma<T>(column_operand<T, D>(g_tile, 32 * u, r, c), a, dv[c]);
-                    dk[c] = mma<T>(column_operand<T, D>(q_tile, 32 * u, r, c), d, dk[c]);
+                    dv[c] = mma<T>(reader.column(r, c, kG + 32 * u * R::kBytes), a, dv[c]);
+                    dk[c] = mma<T>(reader.column(r, c, 32 * u * R::kBytes), d, dk[c]);
                 }
             }
         }
