@@ -463,7 +463,10 @@ struct QueryBlock {
     __device__ __forceinline__ void fetch_bias(int t)
     {
         if constexpr (BIAS) {
-            if (my_window < p.per_group) {
+            if (p.per_group == 1) {  // (numbers that are the same for all lanes)
+                const int begin = begin_of(group), k0 = t * kKeys;
+                bl.load(p, group % p.plane.rows, begin + q0, begin + q1, k0, min(k0 + kKeys, p.nk) - 1, threadIdx.x, kQueryThreads);
+            } else if (my_window < p.per_group) {
                 const int slice = group * p.per_group + my_window, begin = begin_of(slice), k0 = t * kKeys;
                 bl.load(p, slice % p.plane.rows, begin + q0, begin + q1, k0, min(k0 + kKeys, p.nk) - 1, my_thread, my_threads);
             }

@@ -25,7 +25,7 @@ struct DenseForward : DenseQueries {
 };
 
 template <typename T, int D, bool BIAS, int KW>
-__global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && D * sizeof(T) > 64) || KW == 8 ? 2 : 4) void dense_kernel(
+__global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW > 2) ? 2 : 4) void dense_kernel(
     DenseForward p)
 {
     using R = DenseRow<T, D>;

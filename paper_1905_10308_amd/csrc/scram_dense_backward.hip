@@ -52,7 +52,7 @@ __device__ __forceinline__ float4 row_stats(float top, float sum, float dsum)
 
 // The query side: two passes over the keys.
 template <typename T, int D, bool BIAS, int KW>
-__global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBackward p)
+__global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW > 2) ? 2 : 4) void dense_query_kernel(DenseBackward p)
 {
     using R = DenseRow<T, D>;
     constexpr bool kFold = sizeof(T) == 2 && !BIAS;  // as in the forward pass; the first pass keeps a certain key's weight at 1
@@ -71,8 +71,9 @@ __global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBack
     q.pass([&](auto at, const int* places, int from, int k0) {
         constexpr int kAt = decltype(at)::value;
         f32x16_t s = q.products(kAt, qf);
-        const f32x16_t g = q.products(kAt + q.kValues, gf);
         q.template scores<false>(s, places, from, k0);
+        if constexpr (BIAS) __builtin_amdgcn_sched_barrier(0);
+        const f32x16_t g = q.products(kAt + q.kValues, gf);
         float most = top;
 #pragma unroll
         for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i]);
@@ -117,8 +118,9 @@ __global__ __launch_bounds__(kQueryThreads, 2) void dense_query_kernel(DenseBack
     q.pass([&](auto at, const int* places, int from, int k0) {
         constexpr int kAt = decltype(at)::value;
         f32x16_t s = q.products(kAt, qf);
-        const f32x16_t g = q.products(kAt + q.kValues, gf);
         q.template scores<kFold>(s, places, from, k0);
+        if constexpr (BIAS) __builtin_amdgcn_sched_barrier(0);
+        const f32x16_t g = q.products(kAt + q.kValues, gf);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             s[i] = __builtin_amdgcn_exp2f(kFold ? fmaf(s[i], scale2, -shift) : s[i] - shift) * (g[i] - mean);
@@ -162,6 +164,22 @@ template <typename T, int D>
 size_t key_lds(const DenseBackward& p, bool biased)
 {
     return 2 * kKeyTile<T, D> + 2 * sizeof(float) * (3 * kStaged<T, D> + (biased ? kStaged<T, D> + p.key_window : 0)) + 64;
+}
+
+// A number of each of a tile's 32 rows, as registers of a result hold them.
+template <typename T>
+__device__ __forceinline__ f32x16_t row_numbers(const float* of, int h)
+{
+    f32x16_t x;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(of + tile_slot<T>(i) + tile_half<T>() * h);
+        x[i] = v.x;
+        x[i + 1] = v.y;
+        x[i + 2] = v.z;
+        x[i + 3] = v.w;
+    }
+    return x;
 }
 
 // The key side: a block's 128 keys against a run of the query tiles of the slices that read them.
@@ -270,7 +288,7 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
         const int at0 = next_at;  // place of the tile's first query
         // 4 (place of the key, less the window's start)
         const int my_place = 4 * (key_place - (first_place - next_end));
-        const float* const stats = s_stats + at * stats_floats + tile_half<T>() * h;
+        const float* const stats = s_stats + at * stats_floats;
         const int t_now = t;
         t = seek(t + 1);
         if (t < t1) fetch(t, at ^ 1);
@@ -278,7 +296,6 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
         const bool masked = (p.causal && at0 < k_wave + 31) || k_wave + 32 > length;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            __builtin_amdgcn_sched_barrier(0);
             reader.renew();
             // nothing to add: queries before the wave's keys, or behind the slice's last
             if ((p.causal && at0 + 32 * u + 31 < k_wave) || t_now % per_slice * kRows + 32 * u >= p.nq) continue;
@@ -290,13 +307,13 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
             }
             f32x16_t w;
             if constexpr (BIAS) {
-                add_bias<T, -1>(s, p.scale2, s_stats + at * stats_floats + 4 * kRows,
-                                reinterpret_cast<const int*>(s_stats + at * stats_floats) + 3 * kRows + 32 * u, my_place, h, p.runs);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = s[i] - stats[32 * u + tile_slot<T>(i)];
+                add_bias<T, -1>(s, p.scale2, stats + 4 * kRows, reinterpret_cast<const int*>(stats) + 3 * kRows + 32 * u, my_place, h,
+                                p.runs);
+                w = s - row_numbers<T>(stats + 32 * u, h);
             } else {
+                const f32x16_t x0 = row_numbers<T>(stats + 32 * u, h);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = fmaf(s[i], p.scale2, -stats[32 * u + tile_slot<T>(i)]);
+                for (int i = 0; i < 16; ++i) w[i] = fmaf(s[i], p.scale2, -x0[i]);
             }
             if (masked) {
                 asm volatile("");  // (not for every tile, by selects)
@@ -308,11 +325,9 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
             for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(w[i]);
             if (apart) {
                 asm volatile("");
-#pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] *= stats[kRows + 32 * u + tile_slot<T>(i)];
+                w *= row_numbers<T>(stats + kRows + 32 * u, h);
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = w[i] * (g[i] - stats[2 * kRows + 32 * u + tile_slot<T>(i)]);
+            s = w * (g - row_numbers<T>(stats + 2 * kRows + 32 * u, h));
 #pragma unroll
             for (int r = 0; r < R::kRowSteps; ++r) {
                 const uint4 a = as_operand<T>(w, r), d = as_operand<T>(s, r);
@@ -602,7 +617,7 @@ BackwardPlan backward_plan(const DenseCall& c, int elem_bytes)
     p.key_slices = c.key_slices;
     p.all_keys = int64_t(c.key_slices) * p.nk;
     p.key_tiles = (p.nk + kKeysBlock - 1) / kKeysBlock;
-    if (c.bias) p.key_window = int(bias_window(64, kKeysBlock, c.g.Hk, c.g.Wk));
+    if (c.bias) p.key_window = int(bias_window(64, kKeysBlock, c.g.Hk, c.g.Wk) + 3) & ~3;
     const int64_t tiles = int64_t(c.key_slices) * p.key_tiles;
     // splits of the queries: fewer than two blocks per CU leave CUs idle, and a part is worth a block from four tiles on
     const int64_t rows = int64_t(p.share) * ((p.nq + 63) / 64);
