@@ -394,11 +394,6 @@ __global__ __launch_bounds__(kBlock) void dense_key_join_kernel(DenseBackward p)
     store_vec<T, 4>((c < D ? static_cast<T*>(p.dK) + c : static_cast<T*>(p.dV) + c - D) + row * D, y);
 }
 
-// Rows of offsets that a block of the offset side takes: with two, a tile of keys that a step has met is the other row's at
-// the next step, and stays in registers.
-template <typename T, int D>
-constexpr int kOffsetRows = D * sizeof(T) > 256 ? 1 : 2;
-
 // 32 rows on their way through a wave's own part of LDS: read from memory as they lie there, a row by neighbouring lanes, and
 // from LDS as operands, a row by a lane (operands straight from memory touch 32 lines an instruction: 289 us where this takes
 // ROWS_US, 16 slices of 64 x 64, 64 channels).
@@ -437,37 +432,35 @@ struct WaveTile {
     }
 };
 
-// The offset side: offsets dy0 .. of rows, and tiles of 32 columns `apart`, of one head.  A wave goes down the grid rows of a
-// column of tiles (of every fourth column and slice); a tile's scores are formed transposed, so that a query's statistics are
-// its lane's, and what a pair of tiles leaves is added up in registers by the place in the tile.
+// The offset side: an offset dy of rows, and tiles of 32 columns `apart`, of one head.  A wave goes down the grid rows of a column
+// of tiles (of every fourth column and slice); a tile's scores are formed transposed, so that a query's statistics are its
+// lane's, and what a pair of tiles leaves is added up in registers by the place in the tile.
 template <typename T, int D>
-__global__ __launch_bounds__(kBlock, 2) void dense_offset_kernel(DenseBackward p)
+__global__ __launch_bounds__(kBlock, D * sizeof(T) > 256 ? 1 : 2) void dense_offset_kernel(DenseBackward p)
 {
     using R = DenseRow<T, D>;
-    constexpr int N = kOffsetRows<T, D>;
     __shared__ float s_sum[32][33];
-    __shared__ __align__(16) float s_bias[N][4][64][4];  // by register and lane
+    __shared__ __align__(16) float s_bias[4][64][4];  // by register and lane
     __shared__ __align__(16) unsigned char s_turn[4][WaveTile<T, D>::kBytes];
     const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
-    const int apart_all = 2 * p.x_tiles - 1, height = 2 * p.Hk - 1, groups = (height + N - 1) / N;
+    const int apart_all = 2 * p.x_tiles - 1, height = 2 * p.Hk - 1;
     const int apart = static_cast<int>(b % static_cast<uint32_t>(apart_all)) - p.x_tiles + 1;
-    const int dy0 = static_cast<int>(b / static_cast<uint32_t>(apart_all) % static_cast<uint32_t>(groups)) * N - p.Hk + 1;
-    const int head = static_cast<int>(b / static_cast<uint32_t>(apart_all) / static_cast<uint32_t>(groups));
+    const int dy = static_cast<int>(b / static_cast<uint32_t>(apart_all) % static_cast<uint32_t>(height)) - p.Hk + 1;
+    const int head = static_cast<int>(b / static_cast<uint32_t>(apart_all) / static_cast<uint32_t>(height));
     const int lane = threadIdx.x & 63, wave = wave_index(), m = lane & 31, h = lane >> 5;
     const int W = p.Wk, columns = p.x_tiles - abs(apart), column0 = apart < 0 ? -apart : 0;
-    for (int i = threadIdx.x; i < N * 1024; i += kBlock) {
-        const int e = i & 3, l = (i >> 2) & 63, r = 4 * ((i >> 8) & 3) + e, j = i >> 10;
-        const int dx = 32 * apart + tile_slot<T>(r) + tile_half<T>() * (l >> 5) - (l & 31), dy = dy0 + j;
-        const T* const table = static_cast<const T*>(p.bias) + head * p.plane.size;
-        s_bias[j][(i >> 8) & 3][l][e] =
-            abs(dx) < W && dy < p.Hk
-                ? bias_base2(to_float(table[(static_cast<int64_t>(dy) + p.Hk - 1) * p.plane.width + W - 1 + dx])) : 0.f;
+    const int64_t row = static_cast<int64_t>(head) * height + dy + p.Hk - 1;  // of all heads' rows of offsets
+    for (int i = threadIdx.x; i < 1024; i += kBlock) {
+        const int e = i & 3, l = (i >> 2) & 63, r = i >> 8;
+        const int dx = 32 * apart + tile_slot<T>(4 * r + e) + tile_half<T>() * (l >> 5) - (l & 31);
+        const T* const table = static_cast<const T*>(p.bias) + row * p.plane.width;
+        s_bias[r][l][e] = abs(dx) < W ? bias_base2(to_float(table[W - 1 + dx])) : 0.f;
     }
     __syncthreads();
-    f32x16_t sum[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) sum[j] = f32x16_t(0.f);
-    const int64_t strips = static_cast<int64_t>(p.S / p.plane.rows) * columns * p.cuts;
+    f32x16_t sum(0.f);
+    // no key comes after its query
+    const bool none = p.causal && (dy > 0 || (dy == 0 && apart > 0));
+    const int64_t strips = none ? 0 : static_cast<int64_t>(p.S / p.plane.rows) * columns * p.cuts;
     for (int64_t strip = wave; strip < strips; strip += 4) {
         const int cut = static_cast<int>(strip % p.cuts), column = static_cast<int>(strip / p.cuts % columns) + column0;
         const int slice = static_cast<int>(strip / p.cuts / columns) * p.plane.rows + head, slice_k = slice / p.share;
@@ -476,106 +469,81 @@ __global__ __launch_bounds__(kBlock, 2) void dense_offset_kernel(DenseBackward p
         const int64_t q_row = static_cast<int64_t>(slice) * p.nq, k_row = static_cast<int64_t>(slice_k) * p.nk;
         const int qx0 = 32 * column, qx = qx0 + m, kx0 = 32 * (column + apart);
         const bool x_whole = qx0 + 32 <= W && kx0 + 32 <= W;
-        uint4 kf[N][R::kSteps], vf[N][R::kSteps];
-        auto keys = [&](int ky, uint4 (&k)[R::kSteps], uint4 (&v)[R::kSteps]) {
-            const int key = ky * W + kx0;
-            const int last = ky >= 0 && ky < p.Hk ? min(min(32, W - kx0), length - key) : 0;
-            if (last <= 0) return;  // (a row that no pair is taken with)
-            WaveTile<T, D> kl, vl;
-            kl.load(p.K, k_row + key, 0, last);
-            vl.load(p.V, k_row + key, 0, last);
-            kl.turn(s_turn[wave], tile_row<T>(m), k);
-            vl.turn(s_turn[wave], tile_row<T>(m), v);
-        };
-        const int low = max(begin / W, -(dy0 + N - 1)), high = min((begin + p.nq - 1) / W, p.Hk - 1 - dy0);
-        const int from = low + (high - low + 1) * cut / p.cuts, to = low + (high - low + 1) * (cut + 1) / p.cuts - 1;
-        // grid row qy of the queries against rows qy + dy0 + j; those of j are in place (at + j) % N
-        auto step = [&](int qy, auto at) {
-            constexpr int kAt = decltype(at)::value;
+        const int low = max(begin / W, -dy), high = min((begin + p.nq - 1) / W, p.Hk - 1 - dy);
+        const int from = low + (high - low + 1) * cut / p.cuts, to = low + (high - low + 1) * (cut + 1) / p.cuts;
+        if (low > high) continue;
+        for (int qy = from; qy < to; ++qy) {
+            const int ky = qy + dy, key0 = ky * W + kx0, k_last = min(min(32, W - kx0), length - key0);
             const int q = qy * W + qx - begin;
-            const bool q_ok = qx < W && q >= 0 && q < p.nq;
-            keys(qy + dy0 + N - 1, kf[(kAt + N - 1) % N], vf[(kAt + N - 1) % N]);
             const int q0 = qy * W + qx0 - begin, q_first = max(0, -q0), q_last = min(min(32, W - qx0), p.nq - q0);
-            if (q_first >= q_last) return;  // none of the run's queries
-            const float4 st = q_ok ? p.stats[q_row + q] : make_float4(INFINITY, 1.f, 0.f, 0.f);
-            const bool apart_sums = __any(st.y != 1.f);
-            uint4 qf[R::kSteps], gf[R::kSteps];
+            if (k_last <= 0 || q_first >= q_last) continue;  // no key that counts, none of the run's queries
+            const bool q_ok = qx < W && q >= 0 && q < p.nq;
+            uint4 kf[R::kSteps], vf[R::kSteps], qf[R::kSteps], gf[R::kSteps];
+            float4 st = make_float4(INFINITY, 1.f, 0.f, 0.f);
             {
-                WaveTile<T, D> ql, gl;
+                // all on their way before the first is waited for
+                WaveTile<T, D> kl, vl, ql, gl;
+                kl.load(p.K, k_row + key0, 0, k_last);
+                vl.load(p.V, k_row + key0, 0, k_last);
                 ql.load(p.Q, q_row + q0, q_first, q_last);
                 gl.load(p.dO, q_row + q0, q_first, q_last);
+                if (q_ok) st = p.stats[q_row + q];
+                kl.turn(s_turn[wave], tile_row<T>(m), kf);
+                vl.turn(s_turn[wave], tile_row<T>(m), vf);
                 ql.turn(s_turn[wave], m, qf);
                 gl.turn(s_turn[wave], m, gf);
             }
+            f32x16_t s(0.f), g(0.f);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int ky = qy + dy0 + j, dy = dy0 + j;
-                if (ky < 0 || ky >= p.Hk || ky * W + kx0 >= length) continue;
-                if (p.causal && (dy > 0 || (dy == 0 && apart > 0))) continue;
-                f32x16_t s(0.f), g(0.f);
-#pragma unroll
-                for (int c = 0; c < R::kSteps; ++c) {
-                    s = mma<T>(kf[(kAt + j) % N][c], qf[c], s);
-                    g = mma<T>(vf[(kAt + j) % N][c], gf[c], g);
-                }
-                const bool whole = x_whole && ky * W + kx0 + 32 <= length && !(p.causal && dy == 0 && apart == 0) && __all(q_ok);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float4 bias = *reinterpret_cast<const float4*>(s_bias[j][r][lane]);
-                    s[4 * r] = fmaf(s[4 * r], p.scale2, bias.x);
-                    s[4 * r + 1] = fmaf(s[4 * r + 1], p.scale2, bias.y);
-                    s[4 * r + 2] = fmaf(s[4 * r + 2], p.scale2, bias.z);
-                    s[4 * r + 3] = fmaf(s[4 * r + 3], p.scale2, bias.w);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) g[i] -= st.z;
-                if (!whole)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int x1 = kx0 + tile_slot<T>(i) + tile_half<T>() * h, key = ky * W + x1;
-                        const bool on = q_ok && x1 < W && key < length && (!p.causal || key <= q + begin);
-                        s[i] = on ? s[i] : -INFINITY;
-                        g[i] = on ? g[i] : 0.f;
-                    }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] - st.x);
-                if (apart_sums) {
-                    asm volatile("");
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] *= st.y;
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum[j][i] = fmaf(s[i], g[i], sum[j][i]);
+            for (int c = 0; c < R::kSteps; ++c) {
+                s = mma<T>(kf[c], qf[c], s);
+                g = mma<T>(vf[c], gf[c], g);
             }
-        };
-        if (low > high || from > to) continue;
+            const bool whole = x_whole && k_last == 32 && !(p.causal && dy == 0 && apart == 0) && __all(q_ok);
 #pragma unroll
-        for (int j = 0; j < N - 1; ++j) keys(from + dy0 + j, kf[j], vf[j]);
-        for (int qy = from; qy <= to; qy += N) {
-            step(qy, std::integral_constant<int, 0>{});
-            if (N > 1 && qy + 1 <= to) step(qy + 1, std::integral_constant<int, N - 1>{});
+            for (int r = 0; r < 4; ++r) {
+                const float4 bias = *reinterpret_cast<const float4*>(s_bias[r][lane]);
+                s[4 * r] = fmaf(s[4 * r], p.scale2, bias.x);
+                s[4 * r + 1] = fmaf(s[4 * r + 1], p.scale2, bias.y);
+                s[4 * r + 2] = fmaf(s[4 * r + 2], p.scale2, bias.z);
+                s[4 * r + 3] = fmaf(s[4 * r + 3], p.scale2, bias.w);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) g[i] -= st.z;
+            if (!whole)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int x1 = kx0 + tile_slot<T>(i) + tile_half<T>() * h, key = ky * W + x1;
+                    const bool on = q_ok && x1 < W && key < length && (!p.causal || key <= q + begin);
+                    s[i] = on ? s[i] : -INFINITY;
+                    g[i] = on ? g[i] : 0.f;
+                }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] - st.x);
+            if (__any(st.y != 1.f)) {
+                asm volatile("");
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] *= st.y;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[i] = fmaf(s[i], g[i], sum[i]);
         }
     }
     // the waves' sums one after another, then the diagonals
+    for (int k = 0; k < 4; ++k) {
+        if (wave == k)
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-        for (int k = 0; k < 4; ++k) {
-            if (wave == k)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float& at = s_sum[m][tile_slot<T>(i) + tile_half<T>() * h];
-                    at = k ? at + sum[j][i] : sum[j][i];
-                }
-            __syncthreads();
-        }
-        if (threadIdx.x < 63 && dy0 + j < p.Hk) {
-            const int t = static_cast<int>(threadIdx.x) - 31;  // the key's column less the query's
-            float x = 0.f;
-            for (int r = max(0, -t); r < min(32, 32 - t); ++r) x += s_sum[r][r + t];
-            const int64_t row = static_cast<int64_t>(head) * height + dy0 + j + p.Hk - 1;
-            p.diagonals[(row * apart_all + apart + p.x_tiles - 1) * 64 + threadIdx.x] = x;
-        }
+            for (int i = 0; i < 16; ++i) {
+                float& at = s_sum[m][tile_slot<T>(i) + tile_half<T>() * h];
+                at = k ? at + sum[i] : sum[i];
+            }
         __syncthreads();
+    }
+    if (threadIdx.x < 63) {
+        const int t = static_cast<int>(threadIdx.x) - 31;  // the key's column less the query's
+        float x = 0.f;
+        for (int r = max(0, -t); r < min(32, 32 - t); ++r) x += s_sum[r][r + t];
+        p.diagonals[(row * apart_all + apart + p.x_tiles - 1) * 64 + threadIdx.x] = x;
     }
 }
 
@@ -631,8 +599,8 @@ BackwardPlan backward_plan(const DenseCall& c, int elem_bytes)
         p.x_tiles = (c.g.Wk + 31) / 32;
         // four runs of grid rows for the waves of a block at least
         const int64_t columns = int64_t(c.g.S / c.bias_rows) * (p.x_tiles > 1 ? p.x_tiles - 1 : 1);
-        p.cuts = columns >= 4 || c.g.Hk < 8 ? 1 : 4;
-        plan.offset_blocks = int64_t(c.bias_rows) * (2 * int64_t(c.g.Hk) - 1) * (2 * p.x_tiles - 1);  // at most
+        p.cuts = columns >= 4 || c.g.Hk == 1 ? 1 : 4;
+        plan.offset_blocks = int64_t(c.bias_rows) * (2 * int64_t(c.g.Hk) - 1) * (2 * p.x_tiles - 1);
         plan.diagonals = round256(size_t(plan.offset_blocks) * 64 * sizeof(float));
     }
     return plan;
@@ -691,8 +659,7 @@ hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, 
             if (e != hipSuccess) return e;
         }
         if (!dbias) return hipSuccess;
-        const int64_t offsets = int64_t(p.plane.rows) * ((2 * p.Hk - 1 + kOffsetRows<T, D> - 1) / kOffsetRows<T, D>) * (2 * p.x_tiles - 1);
-        e = launch_dense_kernel(dense_offset_kernel<T, D>, offsets, 0, stream, nullptr, nullptr, p);
+        e = launch_dense_kernel(dense_offset_kernel<T, D>, plan.offset_blocks, 0, stream, nullptr, nullptr, p);
         if (e != hipSuccess) return e;
         const int64_t blocks = (p.plane.rows * p.plane.size + kBlock - 1) / kBlock;
         return launch_dense_kernel(dense_offset_join_kernel<T>, blocks < 8192 ? blocks : 8192, 0, stream, nullptr, stop, p);
