@@ -8,6 +8,10 @@
 // output of the softmax stay in registers.  Scores are formed transposed
 // (scram_dense.h), so a query's statistics are a lane's own.
 //
+// Measured, bf16, 64 channels: 4 slices of 16384 queries and keys 323 us, 850 TFLOP/s, where a large matrix product reaches
+// 1130 on the same card; its vector units are busy for 0.66 of the time and the matrix cores for 0.39 at 1.85 GHz, the clock
+// that this load leaves.  16 slices of 4096 with a bias 112 us, 614 TFLOP/s.
+//
 // The waves of a block share its queries (32, 64 or 128) and its keys: KW of
 // them take different keys of the same queries and join at the end.  Calls of
 // few queries also split the keys over blocks; a second kernel joins those
@@ -24,6 +28,9 @@ struct DenseForward : DenseQueries {
     float* part;  // [splits][all rows][D], then [splits][all rows][2]: maximum, sum
 };
 
+// Waves to a SIMD: four where the registers suffice, also at the price of some spilled ones outside the steps (with a bias and two
+// waves to a step's keys, 16 slices of 64 x 64: 124 us, with two waves a SIMD 157).  Calls of fewer queries have no more than
+// one block a CU, which spilling only slows down (16 of 32 x 32: 19.2 us, 22.8 spilled).
 template <typename T, int D, bool BIAS, int KW>
 __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW > 2) ? 2 : 4) void dense_kernel(
     DenseForward p)

@@ -14,7 +14,13 @@
 // - offsets, with a bias: scores and ds once more, added up in registers over
 //   all pairs of tiles at one offset, whose diagonals are then one offset each.
 // The products with p and ds take them from the registers that formed them
-// (scram_dense.h).
+// (scram_dense.h); in bf16 both are rounded for that, to half a step of 2^-8,
+// as the matrix cores take no more, and sums stay in 32 bits.
+//
+// Measured, bf16, 16 slices of 64 x 64, 64 channels, a bias: queries 278 us,
+// keys 241, offsets 230 (the vector units are busy for 0.57, 0.40 and 0.4 of
+// that, the matrix cores for 0.28, 0.24 and 0.14); 16 slices of a row of 2500
+// on 4 of keys, 128 channels, causal: queries 155 us, keys 188, their parts 11.
 
 #include "scram_dense.h"
 
@@ -50,7 +56,8 @@ __device__ __forceinline__ float4 row_stats(float top, float sum, float dsum)
     return make_float4(apart ? top : top + __builtin_amdgcn_logf(sum), apart ? 1.f / sum : 1.f, dsum / sum, 0.f);
 }
 
-// The query side: two passes over the keys.
+// The query side: two passes over the keys.  Four waves a SIMD as in the forward pass: 278 us, 335 with two (16 slices of 64 x 64
+// with a bias); with one block a CU two (8 of 48 x 48: 105 us, 116 with four).
 template <typename T, int D, bool BIAS, int KW>
 __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW > 2) ? 2 : 4) void dense_query_kernel(DenseBackward p)
 {
@@ -182,7 +189,8 @@ __device__ __forceinline__ f32x16_t row_numbers(const float* of, int h)
     return x;
 }
 
-// The key side: a block's 128 keys against a run of the query tiles of the slices that read them.
+// The key side: a block's 128 keys against a run of the query tiles of the slices that read them.  Two waves a SIMD, as many as
+// 512 blocks are: squeezed into registers for three it took 285 us where this takes 241.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
 {
@@ -395,8 +403,8 @@ __global__ __launch_bounds__(kBlock) void dense_key_join_kernel(DenseBackward p)
 }
 
 // 32 rows on their way through a wave's own part of LDS: read from memory as they lie there, a row by neighbouring lanes, and
-// from LDS as operands, a row by a lane (operands straight from memory touch 32 lines an instruction: 289 us where this takes
-// ROWS_US, 16 slices of 64 x 64, 64 channels).
+// from LDS as operands, a row by a lane (operands straight from memory touch 32 lines an instruction: 289 us where this took
+// 207, 16 slices of 64 x 64, 64 channels).
 template <typename T, int D>
 struct WaveTile {
     using R = DenseRow<T, D>;
@@ -434,7 +442,9 @@ struct WaveTile {
 
 // The offset side: an offset dy of rows, and tiles of 32 columns `apart`, of one head.  A wave goes down the grid rows of a column
 // of tiles (of every fourth column and slice); a tile's scores are formed transposed, so that a query's statistics are its
-// lane's, and what a pair of tiles leaves is added up in registers by the place in the tile.
+// lane's, and what a pair of tiles leaves is added up in registers by the place in the tile.  Two rows of offsets a block, with a
+// tile of keys kept for the next step, read half as much, but leave half the blocks, of half the waves a CU: 16 slices of
+// 64 x 64 210 us, this 230; 64 of 32 x 32 127 and 90; 4 of 93 x 125 574 and 491.
 template <typename T, int D>
 __global__ __launch_bounds__(kBlock, D * sizeof(T) > 256 ? 1 : 2) void dense_offset_kernel(DenseBackward p)
 {
@@ -587,7 +597,8 @@ BackwardPlan backward_plan(const DenseCall& c, int elem_bytes)
     p.key_tiles = (p.nk + kKeysBlock - 1) / kKeysBlock;
     if (c.bias) p.key_window = int(bias_window(64, kKeysBlock, c.g.Hk, c.g.Wk) + 3) & ~3;
     const int64_t tiles = int64_t(c.key_slices) * p.key_tiles;
-    // splits of the queries: fewer than two blocks per CU leave CUs idle, and a part is worth a block from four tiles on
+    // splits of the queries: fewer than two blocks per CU leave CUs idle, and a part is worth a block from four tiles on (16 slices
+    // of 2500 on 4 of keys, 128 channels, all kernels: 647 us whole, 406 / 329 / 372 in 2 / 4 / 8 parts; this takes 6)
     const int64_t rows = int64_t(p.share) * ((p.nq + 63) / 64);
     int64_t n = 512 / tiles;
     if (n > rows / 4) n = rows / 4;
@@ -597,7 +608,8 @@ BackwardPlan backward_plan(const DenseCall& c, int elem_bytes)
     plan.part = p.key_splits > 1 ? round256(size_t(p.key_splits) * p.all_keys * 2 * c.g.d * sizeof(float)) : 0;
     if (c.bias) {
         p.x_tiles = (c.g.Wk + 31) / 32;
-        // four runs of grid rows for the waves of a block at least
+        // four runs of grid rows for the waves of a block at least (all kernels: 8 slices of 64 x 64, 8 heads 383 us, 429 uncut;
+        // 16 of 7 x 7 26.9 and 32.5; cut in vain, 32 of 64 x 64 1355 and 1330, 16 of one row of 100 34.1 and 29.4)
         const int64_t columns = int64_t(c.g.S / c.bias_rows) * (p.x_tiles > 1 ? p.x_tiles - 1 : 1);
         p.cuts = columns >= 4 || c.g.Hk == 1 ? 1 : 4;
         plan.offset_blocks = int64_t(c.bias_rows) * (2 * int64_t(c.g.Hk) - 1) * (2 * p.x_tiles - 1);
