@@ -529,7 +529,8 @@ struct QueryBlock {
         for (int c = 0; c < R::kSteps; ++c) s = mma<T>(reader.row(c, at), x[c], s);
         return s;
     }
-    // The scores of products s of the keys k0 .. (from .. of the step's) in base 2 (RAW: before the scale), minus infinity where a key is not seen.
+    // The scores of products s of the keys k0 .. (from .. of the step's) in base 2 (RAW: before the scale), minus infinity where
+    // a key is not seen.
     template <bool RAW>
     __device__ __forceinline__ void scores(f32x16_t& s, const int* places, int from, int k0) const
     {

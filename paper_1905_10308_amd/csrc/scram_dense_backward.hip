@@ -40,7 +40,8 @@ struct DenseBackward : DenseQueries {
     float* diagonals;  // [bias rows][2 Hk - 1][2 x_tiles - 1][64]
     int64_t all_keys;
     int key_tiles;     // of a slice's keys
-    int key_splits;    // runs of query tiles
+    int key_splits;    // runs of query tiles, at most
+    int key_each;      // causal, one place of all slices' queries: query tiles of a run
     int key_window;    // floats of LDS for the key side's bias
     int x_tiles, Hk, Wk, key_slices, S;
     int cuts;          // of a column's grid rows among waves
@@ -173,6 +174,21 @@ size_t key_lds(const DenseBackward& p, bool biased)
     return 2 * kKeyTile<T, D> + 2 * sizeof(float) * (3 * kStaged<T, D> + (biased ? kStaged<T, D> + p.key_window : 0)) + 64;
 }
 
+// The query tiles of a slice that see some key of the block at key k_first: `count` from `low` on; the runs that those of all
+// slices are dealt in.  (Where slices have places of their own, the tiles of none are told apart beforehand.)
+struct KeyRuns {
+    int low, count, all, runs;
+};
+__host__ __device__ inline KeyRuns key_runs(const DenseBackward& p, int rows, int k_first)
+{
+    const int tiles = (p.nq + rows - 1) / rows;
+    if (!p.causal || p.origin) return KeyRuns{0, tiles, tiles * p.share, p.key_splits};
+    const int behind = k_first - p.first;  // queries before these see none of the keys
+    const int low = behind >= p.nq ? tiles : behind > 0 ? behind / rows : 0, all = (tiles - low) * p.share;
+    const int runs = (all + p.key_each - 1) / p.key_each;
+    return KeyRuns{low, tiles - low, all, runs < 1 ? 1 : runs};
+}
+
 // A number of each of a tile's 32 rows, as registers of a result hold them.
 template <typename T>
 __device__ __forceinline__ f32x16_t row_numbers(const float* of, int h)
@@ -235,30 +251,32 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
         first_place = bias_place(p, k_first);
     }
 
-    const int per_slice = (p.nq + kRows - 1) / kRows, all = per_slice * p.share;
-    const int t0 = static_cast<int>(static_cast<int64_t>(all) * split / p.key_splits);
-    const int t1 = k_first < length ? static_cast<int>(static_cast<int64_t>(all) * (split + 1) / p.key_splits) : t0;
+    const KeyRuns of = key_runs(p, kRows, k_first);
+    if (split >= of.runs) return;
+    const int t0 = static_cast<int>(static_cast<int64_t>(of.all) * split / of.runs);
+    const int t1 = k_first < length ? static_cast<int>(static_cast<int64_t>(of.all) * (split + 1) / of.runs) : t0;
+    auto slice_of = [&](int t) { return slice_k * p.share + t / of.count; };
+    auto query_of = [&](int t) { return (of.low + t % of.count) * kRows; };
     // the next tile of which a query sees a key of the block, from t on
     auto seek = [&](int t) {
-        if (p.causal)
-            for (; t < t1; ++t) {
-                const int q0 = t % per_slice * kRows;
-                if (begin_of(slice_k * p.share + t / per_slice) + min(q0 + kRows, p.nq) > k_first) break;
-            }
+        if (p.causal && p.origin)
+            while (t < t1 && begin_of(slice_of(t)) + min(query_of(t) + kRows, p.nq) <= k_first) ++t;
         return t;
     };
     using Stage = DenseStage<T, D, kRows, kBlock>;
     BiasStage<T> bl;
     float4 st = make_float4(INFINITY, 1.f, 0.f, 0.f);
-    int next_at = 0, next_end = 0, next_place = 0;  // of the fetched tile: place of its first query; places on the bias' plane
+    // of the fetched tile: its first query and that one's place; places on the bias' plane
+    int next_q = 0, next_at = 0, next_end = 0, next_place = 0;
     auto fetch = [&](int t, int at) {
-        const int slice = slice_k * p.share + t / per_slice, q0 = t % per_slice * kRows, begin = begin_of(slice);
+        const int slice = slice_of(t), q0 = query_of(t), begin = begin_of(slice);
         const int64_t row = static_cast<int64_t>(slice) * p.nq + q0;
         Stage::load(p.Q, row, p.nq - q0, lds + at * kKeyTile<T, D>);
         Stage::load(p.dO, row, p.nq - q0, lds + at * kKeyTile<T, D> + kRows * R::kBytes);
         const int q = static_cast<int>(threadIdx.x);
         st = make_float4(INFINITY, 1.f, 0.f, 0.f);
         if (q < kRows && q0 + q < p.nq) st = p.stats[row + q];
+        next_q = q0;
         next_at = begin + q0;
         if constexpr (BIAS) {
             const int q1 = begin + min(q0 + kRows, p.nq) - 1;
@@ -297,7 +315,7 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
         // 4 (place of the key, less the window's start)
         const int my_place = 4 * (key_place - (first_place - next_end));
         const float* const stats = s_stats + at * stats_floats;
-        const int t_now = t;
+        const int q_now = next_q;
         t = seek(t + 1);
         if (t < t1) fetch(t, at ^ 1);
         // a query after which some key of the wave's comes, or a key that is not seen
@@ -306,7 +324,7 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
         for (int u = 0; u < U; ++u) {
             reader.renew();
             // nothing to add: queries before the wave's keys, or behind the slice's last
-            if ((p.causal && at0 + 32 * u + 31 < k_wave) || t_now % per_slice * kRows + 32 * u >= p.nq) continue;
+            if ((p.causal && at0 + 32 * u + 31 < k_wave) || q_now + 32 * u >= p.nq) continue;
             f32x16_t s(0.f), g(0.f);
 #pragma unroll
             for (int c = 0; c < R::kSteps; ++c) {
@@ -389,7 +407,8 @@ __global__ __launch_bounds__(kBlock) void dense_key_join_kernel(DenseBackward p)
     if (row >= p.all_keys) return;
     const int c = static_cast<int>(i % (D / 2)) * 4;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < p.key_splits; ++s) {
+    const int runs = key_runs(p, kStaged<T, D>, static_cast<int>(row % p.nk) / kKeysBlock * kKeysBlock).runs;
+    for (int s = 0; s < runs; ++s) {
         const float4 y = *reinterpret_cast<const float4*>(p.part + (static_cast<int64_t>(s) * p.all_keys + row) * (2 * D) + c);
         x[0] += y.x;
         x[1] += y.y;
@@ -598,11 +617,25 @@ BackwardPlan backward_plan(const DenseCall& c, int elem_bytes)
     if (c.bias) p.key_window = int(bias_window(64, kKeysBlock, c.g.Hk, c.g.Wk) + 3) & ~3;
     const int64_t tiles = int64_t(c.key_slices) * p.key_tiles;
     // splits of the queries: fewer than two blocks per CU leave CUs idle, and a part is worth a block from four tiles on (16 slices
-    // of 2500 on 4 of keys, 128 channels, all kernels: 647 us whole, 406 / 329 / 372 in 2 / 4 / 8 parts; this takes 6)
-    const int64_t rows = int64_t(p.share) * ((p.nq + 63) / 64);
-    int64_t n = 512 / tiles;
-    if (n > rows / 4) n = rows / 4;
-    p.key_splits = n < 1 ? 1 : int(n);
+    // of 2500 on 4 of keys, 128 channels, causal, all kernels: 647 us whole, 406 / 329 / 372 in 2 / 4 / 8 parts)
+    const int rows = c.g.d * elem_bytes > 256 ? 32 : 64;
+    if (c.causal && !c.origin && tiles <= 512) {
+        // a key's runs by how many queries see it: the first keys' are many, and all blocks are as long, one a CU (all kernels:
+        // 4 rows of 6000, 32 channels 172 us in equal numbers of runs, so 148; 16 of 2500 on 4 of keys, 128 channels 329 and
+        // 321, with blocks half as long 351)
+        p.key_each = 1;
+        int64_t all = 0;
+        for (int t = 0; t < p.key_tiles; ++t) all += c.key_slices * int64_t(key_runs(p, rows, t * kKeysBlock).all);
+        p.key_each = static_cast<int>((all + 255) / 256);
+        if (p.key_each < 4) p.key_each = 4;
+        p.key_splits = key_runs(p, rows, 0).runs;
+    } else {
+        const int64_t all = int64_t(p.share) * ((p.nq + rows - 1) / rows);
+        int64_t n = 512 / tiles;
+        if (n > all / 4) n = all / 4;
+        p.key_splits = n < 1 ? 1 : int(n);
+        p.key_each = 1 << 30;
+    }
     plan.key_blocks = tiles * p.key_splits;
     plan.stats = round256(size_t(c.g.S) * p.nq * sizeof(float4));
     plan.part = p.key_splits > 1 ? round256(size_t(p.key_splits) * p.all_keys * 2 * c.g.d * sizeof(float)) : 0;
@@ -622,10 +655,17 @@ int elem_bytes_of(int dtype) { return dtype == SCRAM_BF16 ? 2 : 4; }
 
 }  // namespace
 
+// Of a call with or without the causal mask, wherever its queries stand: the first keys' runs are most where they stand first.
 size_t dense_backward_workspace_bytes(int dtype, const DenseCall& c)
 {
-    const BackwardPlan plan = backward_plan(c, elem_bytes_of(dtype));
-    return plan.stats + plan.part + plan.diagonals;
+    DenseCall any = c;
+    any.origin = nullptr;
+    any.first = 0;
+    any.causal = false;
+    const BackwardPlan plan = backward_plan(any, elem_bytes_of(dtype));
+    any.causal = true;
+    const size_t part = backward_plan(any, elem_bytes_of(dtype)).part;
+    return plan.stats + (part > plan.part ? part : plan.part) + plan.diagonals;
 }
 
 uint64_t dense_backward_blocks(int dtype, const DenseCall& c)

@@ -91,6 +91,10 @@ FORMS = [
     dict(shape=(4, 1, 1, 8, 30, 31, 32), heads=2, first=[5, 922, 70, 800]),
     dict(shape=(2, 1, 40, 41, 2, 3, 64)),
     dict(shape=(2, 2, 2, 700, 2, 700, 64), heads=1),
+    # causal runs of the keys' side: many and few queries behind a place of their own, shared keys
+    dict(shape=(3, 1, 1, 900, 1, 1500, 32), causal=True, first=421),
+    dict(shape=(2, 2, 1, 129, 1, 1100, 128), causal=True, first=971),
+    dict(shape=(8, 1, 1, 640, 1, 641, 16), heads=2, causal=True, first=1),
 ]
 
 
