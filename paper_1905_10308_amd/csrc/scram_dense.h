@@ -558,10 +558,10 @@ constexpr int kMostSplits = 256;
 inline QueryPlan query_plan(const DenseCall& c, int elem_bytes, bool split, DenseQueries& p)
 {
     const int bytes = c.g.d * elem_bytes;
-    auto room = [&](int kw, int slices, int buffers) {
+    auto room = [&](int kw, int slices, int buffers, int blocks = 1) {
         const int64_t keys = kw * wave_keys(bytes, kw), rows = 256 / kw;
         const int64_t windows = c.bias ? slices * bias_window(int(rows), int(keys), c.g.Hk, c.g.Wk) + keys : 0;
-        return buffers * (2 * keys * bytes + 4 * windows) + 6144 <= 160 * 1024;
+        return blocks * (buffers * (2 * keys * bytes + 4 * windows) + 6144) <= 160 * 1024;
     };
     // A tile that holds the queries of all slices of a key slice, each with a window: the keys are read once (64 slices of two
     // queries on 4 of 64 x 64 keys 16.1 us, 16.4 with a tile a slice; 128 of one on 8 of 32 x 32 11.8 and 12.5).
@@ -579,8 +579,11 @@ inline QueryPlan query_plan(const DenseCall& c, int elem_bytes, bool split, Dens
     if (p.rows > 64 && blocks(2) >= 256) kw = 2;
     if (bytes > 256 && kw == 8) kw = 4;  // (a step of eight waves' rows of 512 bytes does not fit)
     if (!room(kw, together ? p.share : 1, 1)) kw = 2;
-    // the next step's rows are on their way while this one's are met: 2500 queries of 128 channels 95 us, with one buffer 106
+    // The next step's rows are on their way while this one's are met: 2500 queries of 128 channels 95 us, with one buffer 106.
+    // Two blocks a CU do as much for each other, and more where their registers let them (300 / 1024 slices of 48 queries
+    // on 1008 keys 20.7 / 50 us, 28.8 / 62 with two buffers; 256 of them, a block a CU, 19.5 and 18.3).
     p.buffers = room(kw, together ? p.share : 1, 2) ? 2 : 1;
+    if (!c.bias && bytes <= 128 && blocks(kw) > 256 && !room(kw, 1, 2, 2) && room(kw, 1, 1, 2)) p.buffers = 1;
     p.tiles = (p.rows + 256 / kw - 1) / (256 / kw);
     const int keys = kw * wave_keys(bytes, kw);
     if (c.bias) p.window = int(bias_window(256 / kw, keys, c.g.Hk, c.g.Wk));

@@ -91,6 +91,10 @@ FORMS = [
     dict(shape=(4, 1, 1, 8, 30, 31, 32), heads=2, first=[5, 922, 70, 800]),
     dict(shape=(2, 1, 40, 41, 2, 3, 64)),
     dict(shape=(2, 2, 2, 700, 2, 700, 64), heads=1),
+    # two blocks a CU that stage one step at a time
+    dict(shape=(300, 300, 1, 40, 1, 601, 64)),
+    dict(shape=(260, 130, 1, 5, 1, 790, 64), lengths=[790, 0, 700, 5, 64] * 26),
+    dict(shape=(264, 264, 1, 24, 1, 600, 32), causal=True, first=576),
     # causal runs of the keys' side: many and few queries behind a place of their own, shared keys
     dict(shape=(3, 1, 1, 900, 1, 1500, 32), causal=True, first=421),
     dict(shape=(2, 2, 1, 129, 1, 1100, 128), causal=True, first=971),
@@ -102,6 +106,20 @@ FORMS = [
 @pytest.mark.parametrize("c", FORMS, ids=lambda c: "x".join(map(str, c["shape"])))
 def test_forms(scram, c, dtype):
     check(scram, c, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,dv", [(20, 33), (64, 16), (8, 100)])
+def test_values_of_another_width(scram, d, dv, dtype):
+    Q, K, V, dO, kw = make(dict(shape=(4, 2, 5, 9, 5, 9, max(d, dv)), heads=2, causal=True), dtype)
+    Q, K, V, dO = (t[..., :n].contiguous() for t, n in ((Q, d), (K, d), (V, dv), (dO, dv)))
+    want, tol = ref.attend_all(Q, K, V, dO, **kw)
+    out = torch.full_like(dO, 7.0)
+    assert scram.dense_attend(Q, K, V, out=out, **kw) is out
+    got = [out, *scram.dense_attend_backward(Q, K, V, dO, **kw)]
+    for name, g, w, t in zip(("out", "dQ", "dK", "dV", "dbias"), got, want, tol):
+        assert g.shape == w.shape
+        near(g, w, t, name)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
