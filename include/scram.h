@@ -530,7 +530,7 @@ int scram_layer_norm_backward(const void* dY, int grad_dtype, const void* X, int
  *   lengths     nullable int32 [key_slices] on the device: the keys of a slice
  *               that count, in raster order; clamped into [0, Hk*Wk].  Those
  *               behind are not read
- *   key_slices  divides S
+ *   key_slices  divides S; S*Hq*Wq and Hk*Wk stay below 2^31 - 1024
  *   scale       softmax temperature, 1/sqrt(d) for Equation 1; finite
  *   flags       0 or SCRAM_CAUSAL
  *   first, origin

@@ -75,13 +75,22 @@ int check_differential(int dtype, const scram::Grid& g, int kappa, int dv, int w
     return SCRAM_OK;
 }
 
+// The kernels count rows in steps of up to 512: a step behind the last row is a number too.
+int check_dense_grid(int S, int key_slices, int Hq, int Wq, int Hk, int Wk)
+{
+    const int rc = check_grid(S, Hq, Wq, Hk, Wk);
+    if (rc) return rc;
+    const int64_t most = kMaxCount - 1024;
+    if (int64_t(S) * Hq * Wq >= most || int64_t(Hk) * Wk >= most) return SCRAM_ERR_SHAPE;
+    return key_slices < 1 || S % key_slices ? SCRAM_ERR_SHAPE : SCRAM_OK;
+}
+
 // Arguments that the dense attend and its gradients share, but for pointers.
 int check_dense(int dtype, const scram::DenseCall& c, int dv, uint32_t flags)
 {
     const scram::Grid& g = c.g;
-    int rc = check_grid(g.S, g.Hq, g.Wq, g.Hk, g.Wk);
+    int rc = check_dense_grid(g.S, c.key_slices, g.Hq, g.Wq, g.Hk, g.Wk);
     if (rc) return rc;
-    if (c.key_slices < 1 || g.S % c.key_slices) return SCRAM_ERR_SHAPE;
     if (!isfinite(c.scale)) return SCRAM_ERR_SHAPE;
     if ((rc = check_type(dtype, g.d))) return rc;
     if (dv != g.d) return SCRAM_ERR_UNSUPPORTED;
@@ -628,7 +637,7 @@ int scram_layer_norm_backward(const void* dY, int grad_dtype, const void* X, int
 
 size_t scram_dense_attend_workspace_bytes(int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dtype, int biased)
 {
-    if (check_grid(S, Hq, Wq, Hk, Wk) || key_slices < 1 || S % key_slices || check_type(dtype, d)) return 0;
+    if (check_dense_grid(S, key_slices, Hq, Wq, Hk, Wk) || check_type(dtype, d)) return 0;
     return scram::dense_workspace_bytes(dtype, dense_call(nullptr, nullptr, nullptr, biased ? "" : nullptr, 1, nullptr, S, key_slices, Hq, Wq,
                                                    Hk, Wk, d, 1.f, 0, 0, nullptr));
 }
@@ -667,7 +676,7 @@ int scram_dense_attend(const void* Q, const void* K, const void* V, int dtype, c
 size_t scram_dense_attend_backward_workspace_bytes(int S, int key_slices, int Hq, int Wq, int Hk, int Wk, int d, int dtype,
                                                    int bias_rows)
 {
-    if (check_grid(S, Hq, Wq, Hk, Wk) || key_slices < 1 || S % key_slices || check_type(dtype, d)) return 0;
+    if (check_dense_grid(S, key_slices, Hq, Wq, Hk, Wk) || check_type(dtype, d)) return 0;
     if (bias_rows < 0 || (bias_rows && S % bias_rows)) return 0;
     return scram::dense_backward_workspace_bytes(dtype, dense_call(nullptr, nullptr, nullptr, bias_rows ? "" : nullptr, bias_rows, nullptr, S,
                                                             key_slices, Hq, Wq, Hk, Wk, d, 1.f, 0, 0, nullptr));

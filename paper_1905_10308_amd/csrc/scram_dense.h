@@ -249,10 +249,9 @@ __device__ __forceinline__ int bias_place(const DenseParams& p, int at)
     return static_cast<int>(y) * p.plane.width + static_cast<int>(x);
 }
 
-
-// A window of the bias' plane on its way to LDS, by a block's threads or a share of them: queries q0 .. q1 against keys k0 .. k1.  Places
-// rise with the raster index, so that they lie between those of the runs' ends: the window's start is place(k0) - place(q1),
-// and a pair's index its place less that.
+// A window of the bias' plane on its way to LDS, by a block's threads or a share of them: queries q0 .. q1 against keys k0 .. k1.
+// Places rise with the raster index, so that they lie between those of the runs' ends: the window's start is
+// place(k0) - place(q1), and a pair's index its place less that.
 template <typename T>
 struct BiasStage {
     float x[2];

@@ -50,6 +50,8 @@ SHARED = [
     # a bias whose heads do not divide the slices, planes of 2^31 places, windows that no block holds
     (dict(bias=A[9], heads=0), ESHAPE), (dict(bias=A[9], heads=3), ESHAPE), (dict(B, S=2, Hq=1, Wq=1, Hk=1 << 15, Wk=1 << 14), ESHAPE),
     (dict(B, Hq=1, Wq=1, Hk=2, Wk=7000), ESHAPE),
+    # so many rows that a step behind the last is no number
+    (dict(S=2, Sk=2, Hq=1, Wq=1, Hk=2, Wk=(1 << 30) - 1), ESHAPE), (dict(S=2, Sk=1, Hq=1, Wq=(1 << 30) - 1), ESHAPE),
     (dict(Q=A[0] + 8), EALIGN), (dict(V=A[2] + 2), EALIGN), (dict(B, bias=A[9] + 1), EALIGN), (dict(lengths=A[10] + 2), EALIGN),
     (dict(flags=CAUSAL, Hq=1, Wq=1, origin=A[10] + 2), EALIGN),
 ]
