@@ -306,7 +306,7 @@ struct DenseQueries : DenseParams {
     int window;         // floats of LDS for the bias, of each slice in a tile
     int window_shift;   // log2 of the shares of a block's threads that stage them
     int buffers;        // steps whose rows fit in LDS: with two, the next one's are stored while this one's are read
-    int runs;           // whether the keys of a lane's vectors (tile_half of them) lie in one grid row
+    int runs;           // whether grid rows are whole vectors of tile_half rows: those of keys, which begin at a multiple, lie in one
 };
 
 // Keys of a wave in a block's step: 64, which halves the barriers, 32 where two steps' rows would not fit in LDS.
@@ -334,7 +334,7 @@ template <typename T, int SIGN>
 __device__ __forceinline__ void add_bias(f32x16_t& s, float scale2, const float* window, const int* places, int mine, int h, bool runs)
 {
     constexpr int N = tile_half<T>();
-    if (runs) {  // a vector's rows lie side by side
+    if (runs) {  // a vector's rows lie side by side on the grid
 #pragma unroll
         for (int g = 0; g < 16; g += N) {
             const int at = SIGN * (places[tile_slot<T>(g) + N * h] - mine);
