@@ -526,7 +526,7 @@ int scram_layer_norm_backward(const void* dY, int grad_dtype, const void* X, int
  *               key; the type's lowest value hides it behind any other.
  *               bias_rows >= 1 divides S (slice = image * heads + head: the
  *               images share the heads' tables).  Not for Hk > 1 with Wk above
- *               5000 or so (SCRAM_ERR_SHAPE), nor 2^31 offsets
+ *               4993 (SCRAM_ERR_SHAPE), nor 2^31 offsets
  *   lengths     nullable int32 [key_slices] on the device: the keys of a slice
  *               that count, in raster order; clamped into [0, Hk*Wk].  Those
  *               behind are not read

@@ -116,6 +116,8 @@ scram::DenseCall dense_call(const void* Q, const void* K, const void* V, const v
                             (flags & SCRAM_CAUSAL) != 0, first, origin};
 }
 
+bool fits(const scram::DenseNeeds& n) { return n.blocks <= kMaxBlocks && n.lds <= scram::kLdsMost; }
+
 size_t bias_bytes(const scram::DenseCall& c, size_t eb)
 {
     return c.bias ? size_t(c.bias_rows) * (2 * size_t(c.g.Hk) - 1) * (2 * size_t(c.g.Wk) - 1) * eb : 0;
@@ -652,7 +654,7 @@ int scram_dense_attend(const void* Q, const void* K, const void* V, int dtype, c
         dense_call(Q, K, V, bias, bias_rows, lengths, S, key_slices, Hq, Wq, Hk, Wk, d, scale, flags, first, origin);
     int rc = check_dense(dtype, call, dv, flags);
     if (rc) return rc;
-    if (scram::dense_blocks(dtype, call) > kMaxBlocks) return SCRAM_ERR_SHAPE;
+    if (!fits(scram::dense_needs(dtype, call))) return SCRAM_ERR_SHAPE;
     const size_t eb = elem_bytes(dtype), need = scram::dense_workspace_bytes(dtype, call);
     if (need && !workspace) return SCRAM_ERR_WORKSPACE;
     if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(bias, eb) || !aligned(lengths, 4) ||
@@ -694,7 +696,7 @@ int scram_dense_attend_backward(const void* Q, const void* K, const void* V, int
         dense_call(Q, K, V, bias, bias_rows, lengths, S, key_slices, Hq, Wq, Hk, Wk, d, scale, flags, first, origin);
     int rc = check_dense(dtype, call, dv, flags);
     if (rc) return rc;
-    if (scram::dense_backward_blocks(dtype, call) > kMaxBlocks) return SCRAM_ERR_SHAPE;
+    if (!fits(scram::dense_backward_needs(dtype, call))) return SCRAM_ERR_SHAPE;
     if (!workspace) return SCRAM_ERR_WORKSPACE;
     const size_t eb = elem_bytes(dtype), need = scram::dense_backward_workspace_bytes(dtype, call);
     if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(dO, 16) || !aligned(bias, eb) || !aligned(lengths, 4) ||

@@ -318,14 +318,18 @@ constexpr int kWaveKeys = wave_keys(D * sizeof(T), KW);
 template <typename T, int D, int KW>
 constexpr size_t kTileBytes = 2 * (KW * kWaveKeys<T, D, KW> * DenseRow<T, D>::kBytes);
 
-// Bytes of LDS before the bias': the staged rows, and after them what the waves of the same queries join.
-template <typename T, int D, int KW>
-__host__ __device__ constexpr size_t query_lds(int buffers)
+// What a block of queries may take of LDS in arrays of its own (3104 bytes in the gradients' kernel: maxima, sums and means of its
+// waves' rows, their last keys; 288 in the forward's: those last, and the vote on another pass).
+constexpr size_t kQueryStatic = 6144 - 64;
+
+// The rest: staged rows, with a bias the places of their keys and its windows (floats of a step; behind the last a vector's), and in
+// the place of all these at the end what the waves of the same queries join.
+constexpr size_t query_lds(int d, int elem_bytes, int kw, int buffers, int64_t bias_floats)
 {
-    using R = DenseRow<T, D>;
-    const size_t tiles = buffers * kTileBytes<T, D, KW>;
-    constexpr size_t join = 8 * 64 * sizeof(float) * (16 * R::kColumns + 2);
-    return tiles > join ? tiles : join;
+    const size_t row = size_t(d) * elem_bytes, rows = 2 * size_t(kw) * wave_keys(int(row), kw) * row;
+    const size_t steps = buffers * (rows + bias_floats * sizeof(float)) + (bias_floats ? 64 : 0);
+    const size_t join = 8 * 64 * sizeof(float) * (16 * (d < 32 ? 1 : d / 32) + 2);
+    return steps > join ? steps : join;
 }
 
 // s scale2 + bias for a 32 x 32 tile: places are those of the rows of the tile (4 a place), mine the lane's, so that a row's
@@ -377,7 +381,7 @@ struct QueryBlock {
 
     __device__ __forceinline__ QueryBlock(const DenseQueries& params, unsigned char* memory) : p(params), lds(memory)
     {
-        s_places = reinterpret_cast<int*>(lds + query_lds<T, D, KW>(p.buffers));
+        s_places = reinterpret_cast<int*>(lds + p.buffers * kTileBytes<T, D, KW>);
         bias_floats = kKeys + p.per_group * p.window;
         const uint32_t b = xcd_remap(blockIdx.x, gridDim.x);
         split = static_cast<int>(b % static_cast<uint32_t>(p.splits));
@@ -560,7 +564,7 @@ inline QueryPlan query_plan(const DenseCall& c, int elem_bytes, bool split, Dens
     auto room = [&](int kw, int slices, int buffers, int blocks = 1) {
         const int64_t keys = kw * wave_keys(bytes, kw), rows = 256 / kw;
         const int64_t windows = c.bias ? slices * bias_window(int(rows), int(keys), c.g.Hk, c.g.Wk) + keys : 0;
-        return blocks * (buffers * (2 * keys * bytes + 4 * windows) + 6144) <= 160 * 1024;
+        return blocks * (query_lds(c.g.d, elem_bytes, kw, buffers, windows) + kQueryStatic) <= kLdsMost;
     };
     // A tile that holds the queries of all slices of a key slice, each with a window: the keys are read once (64 slices of two
     // queries on 4 of 64 x 64 keys 16.1 us, 16.4 with a tile a slice; 128 of one on 8 of 32 x 32 11.8 and 12.5).
@@ -577,7 +581,7 @@ inline QueryPlan query_plan(const DenseCall& c, int elem_bytes, bool split, Dens
     if (p.rows > 32 && blocks(4) >= 256) kw = 4;
     if (p.rows > 64 && blocks(2) >= 256) kw = 2;
     if (bytes > 256 && kw == 8) kw = 4;  // (a step of eight waves' rows of 512 bytes does not fit)
-    if (!room(kw, together ? p.share : 1, 1)) kw = 2;
+    if (!room(kw, together ? p.share : 1, 1)) kw = 2;  // (which any window fits beside that a call may have: kBiasWindowMost)
     // The next step's rows are on their way while this one's are met: 2500 queries of 128 channels 95 us, with one buffer 106.
     // Two blocks a CU do as much for each other, and more where their registers let them (300 / 1024 slices of 48 queries
     // on 1008 keys 20.7 / 50 us, 28.8 / 62 with two buffers; 256 of them, a block a CU, 19.5 and 18.3).
@@ -605,7 +609,14 @@ template <typename T, int D, bool BIAS, int KW>
 size_t query_block_lds(const DenseQueries& p)
 {
     constexpr int keys = KW * kWaveKeys<T, D, KW>;
-    return query_lds<T, D, KW>(p.buffers) + (BIAS ? p.buffers * (keys + size_t(p.per_group) * p.window) * sizeof(float) + 64 : 0);
+    return query_lds(D, sizeof(T), KW, p.buffers, BIAS ? keys + int64_t(p.per_group) * p.window : 0);
+}
+
+// All bytes of a plan's block.
+inline size_t query_plan_lds(const DenseQueries& p, const DenseCall& c, int elem_bytes, int kw)
+{
+    const int64_t keys = kw * wave_keys(c.g.d * elem_bytes, kw);
+    return query_lds(c.g.d, elem_bytes, kw, p.buffers, c.bias ? keys + int64_t(p.per_group) * p.window : 0) + kQueryStatic;
 }
 
 // f(BIAS, KW) of a plan

@@ -222,7 +222,12 @@ size_t dense_workspace_bytes(int dtype, const DenseCall& c)
     return plan.p.splits == 1 ? 0 : size_t(plan.p.splits) * plan.p.all_rows * (c.g.d + 2) * sizeof(float);
 }
 
-uint64_t dense_blocks(int dtype, const DenseCall& c) { return 2 * uint64_t(forward_plan(c, elem_bytes_of(dtype)).queries.blocks); }
+DenseNeeds dense_needs(int dtype, const DenseCall& c)
+{
+    const int eb = elem_bytes_of(dtype);
+    const ForwardPlan plan = forward_plan(c, eb);
+    return DenseNeeds{2 * uint64_t(plan.queries.blocks), query_plan_lds(plan.p, c, eb, plan.queries.key_waves)};
+}
 
 hipError_t launch_dense(int dtype, const DenseCall& c, void* out, void* workspace, hipStream_t stream, hipEvent_t start,
                         hipEvent_t stop)

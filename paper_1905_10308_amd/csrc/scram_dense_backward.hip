@@ -162,16 +162,19 @@ __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW >
     }
 }
 
-// Rows of queries that a block of the key side stages at a time, and whether two such steps fit in LDS.
+// Rows of queries that a block of the key side stages at a time; two such steps are in LDS.
+constexpr int staged_rows(int row_bytes) { return row_bytes > 256 ? 32 : 64; }
 template <typename T, int D>
-constexpr int kStaged = D * sizeof(T) > 256 ? 32 : 64;
+constexpr int kStaged = staged_rows(D * sizeof(T));
 template <typename T, int D>
 constexpr size_t kKeyTile = 2 * (kStaged<T, D> * DenseRow<T, D>::kBytes);
 
-template <typename T, int D>
-size_t key_lds(const DenseBackward& p, bool biased)
+constexpr size_t kKeyStatic = 64 * sizeof(float);  // the vote on a step's factors
+
+inline size_t key_lds(int d, int elem_bytes, const DenseBackward& p, bool biased)
 {
-    return 2 * kKeyTile<T, D> + 2 * sizeof(float) * (3 * kStaged<T, D> + (biased ? kStaged<T, D> + p.key_window : 0)) + 64;
+    const size_t row = size_t(d) * elem_bytes, staged = staged_rows(int(row));
+    return 2 * (2 * staged * row) + 2 * sizeof(float) * (3 * staged + (biased ? staged + p.key_window : 0)) + 64;
 }
 
 // The query tiles of a slice that see some key of the block at key k_first: `count` from `low` on; the runs that those of all
@@ -621,7 +624,7 @@ BackwardPlan backward_plan(const DenseCall& c, int elem_bytes)
     const int64_t tiles = int64_t(c.key_slices) * p.key_tiles;
     // splits of the queries: fewer than two blocks per CU leave CUs idle, and a part is worth a block from four tiles on (16 slices
     // of 2500 on 4 of keys, 128 channels, causal, all kernels: 647 us whole, 406 / 329 / 372 in 2 / 4 / 8 parts)
-    const int rows = c.g.d * elem_bytes > 256 ? 32 : 64;
+    const int rows = staged_rows(c.g.d * elem_bytes);
     if (c.causal && !c.origin && tiles <= 512) {
         // a key's runs by how many queries see it: the first keys' are many, and all blocks are as long, one a CU (all kernels:
         // 4 rows of 6000, 32 channels 172 us in equal numbers of runs, so 148; 16 of 2500 on 4 of keys, 128 channels 329 and
@@ -671,12 +674,16 @@ size_t dense_backward_workspace_bytes(int dtype, const DenseCall& c)
     return plan.stats + (part > plan.part ? part : plan.part) + plan.diagonals;
 }
 
-uint64_t dense_backward_blocks(int dtype, const DenseCall& c)
+DenseNeeds dense_backward_needs(int dtype, const DenseCall& c)
 {
-    const BackwardPlan plan = backward_plan(c, elem_bytes_of(dtype));
-    uint64_t most = 2 * uint64_t(plan.queries.blocks);
-    if (uint64_t(plan.key_blocks) > most) most = plan.key_blocks;
-    return uint64_t(plan.offset_blocks) > most ? plan.offset_blocks : most;
+    const int eb = elem_bytes_of(dtype);
+    const BackwardPlan plan = backward_plan(c, eb);
+    uint64_t blocks = 2 * uint64_t(plan.queries.blocks);
+    if (uint64_t(plan.key_blocks) > blocks) blocks = plan.key_blocks;
+    if (uint64_t(plan.offset_blocks) > blocks) blocks = plan.offset_blocks;
+    const size_t query = query_plan_lds(plan.p, c, eb, plan.queries.key_waves);
+    const size_t key = key_lds(c.g.d, eb, plan.p, c.bias) + kKeyStatic;
+    return DenseNeeds{blocks, query > key ? query : key};
 }
 
 hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, void* dQ, void* dK, void* dV, void* dbias,
@@ -704,7 +711,7 @@ hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, 
         });
         if (e != hipSuccess) return e;
         const hipEvent_t end = p.key_splits == 1 && !dbias ? stop : nullptr;
-        const size_t lds = key_lds<T, D>(p, c.bias);
+        const size_t lds = key_lds(D, sizeof(T), p, c.bias);
         e = c.bias ? launch_dense_kernel(dense_key_kernel<T, D, true>, plan.key_blocks, lds, stream, nullptr, end, p)
                    : launch_dense_kernel(dense_key_kernel<T, D, false>, plan.key_blocks, lds, stream, nullptr, end, p);
         if (e != hipSuccess) return e;

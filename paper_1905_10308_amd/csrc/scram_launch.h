@@ -101,11 +101,17 @@ struct DenseCall {
 constexpr int kBiasWindowMost = 10240;  // most places of a bias' plane that a block holds at once
 int64_t dense_bias_window(int Hk, int Wk);
 size_t dense_workspace_bytes(int dtype, const DenseCall& c);
-uint64_t dense_blocks(int dtype, const DenseCall& c);
+// Of a call's launches the most blocks (of 256 threads) and the most bytes of shared memory of a block; of a CU.
+struct DenseNeeds {
+    uint64_t blocks;
+    size_t lds;
+};
+constexpr size_t kLdsMost = 160 * 1024;
+DenseNeeds dense_needs(int dtype, const DenseCall& c);
 hipError_t launch_dense(int dtype, const DenseCall& c, void* out, void* workspace, hipStream_t stream, hipEvent_t start,
                         hipEvent_t stop);
 size_t dense_backward_workspace_bytes(int dtype, const DenseCall& c);
-uint64_t dense_backward_blocks(int dtype, const DenseCall& c);
+DenseNeeds dense_backward_needs(int dtype, const DenseCall& c);
 hipError_t launch_dense_backward(int dtype, const DenseCall& c, const void* dO, void* dQ, void* dK, void* dV, void* dbias,
                                  void* workspace, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
 

@@ -40,3 +40,25 @@ def test_queries_at_any_place(scram, c, dtype):
 @pytest.mark.parametrize("H,W", [(8, 8), (16, 24), (64, 64)])
 def test_runs_of_queries_that_cross_rows(scram, H, W, first, dtype):
     check(scram, dict(shape=(2, 2, 1, min(3 * W, H * W - first), H, W, 64), heads=2, first=first), dtype, seed=first)
+
+
+# wide grids, whose part of the bias' plane fills what the staged rows leave of a block's shared memory: around the choice of one
+# or two steps in flight, of how many queries a block holds, and the widest; heads of one slice of keys with a window each
+WIDE = [
+    dict(shape=(1, 1, 2, 1404, 2, 1404, 128), heads=1),
+    dict(shape=(1, 1, 2, 1450, 2, 1450, 128), heads=1, causal=True),
+    dict(shape=(300, 300, 1, 256, 2, 1450, 128), heads=2, first=1301),
+    dict(shape=(1, 1, 2, 2950, 2, 2950, 128), heads=1),
+    dict(shape=(2, 2, 1, 700, 2, 3400, 128), heads=1, first=[3000, 5]),
+    dict(shape=(2, 2, 1, 1, 2, 3600, 128), heads=2, causal=True, first=[7199, 3600]),
+    dict(shape=(1, 1, 1, 900, 2, 4993, 128), heads=1, causal=True, first=8001),
+    dict(shape=(1, 1, 1, 900, 2, 4993, 16), heads=1, first=4500),
+    dict(shape=(10, 1, 1, 1, 70, 70, 128), heads=10, causal=True, first=[4899, 0, 70, 69, 1, 2500, 2501, 3333, 4001, 8]),
+    dict(shape=(20, 2, 1, 3, 70, 70, 128), heads=5, first=[4897, 0, 70, 69, 1, 2500, 2501, 3333, 4001, 8] * 2),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", WIDE, ids=lambda c: "x".join(map(str, c["shape"])))
+def test_wide_grids(scram, c, dtype):
+    check(scram, c, dtype)
