@@ -195,7 +195,7 @@ struct TileReader {
 // lanes' 16 bytes one after another from the place in m0 on, so the order of a row's chunks is that in which lanes fetch them.
 // The rows from `live` (> 0) on are row live - 1 again, whose products count nowhere.  Issued in assembly, since for the
 // builtin the compiler would wait for the rows on their way before it reads any others; wait() waits for them, and for the
-// other waves' a barrier.  (m0 has no other use in these kernels.)
+// other waves' a barrier.  (The compiler writes m0, as an operand; a scalar write of it and the load keep an instruction between.)
 template <typename T, int D, int N, int THREADS>
 struct DenseStage {
     using R = DenseRow<T, D>;
@@ -217,9 +217,9 @@ struct DenseStage {
         for (int j = 0; j < kEach; ++j) {
             const int load = j * kWaves + wave;
             if (kTotal % kWaves == 0 || load < kTotal)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                              :
-                             : "s"(to + 1024u * load), "v"(offset(load, live)), "s"(from)
+                             : "{m0}"(to + 1024u * load), "v"(offset(load, live)), "s"(from)
                              : "memory");
         }
     }
