@@ -448,7 +448,9 @@ struct QueryBlock {
 #pragma unroll
             for (int c = 0; c < R::kSteps; ++c) qf[c] = make_uint4(qf[c].x ^ kSign, qf[c].y ^ kSign, qf[c].z ^ kSign, qf[c].w ^ kSign);
         }
-        if (scale2 == 0.f) scale2 = 1e-37f;  // (a key that is not seen has a score of minus infinity, and a weight of 0 by it)
+        // (a key that is not seen has a score of minus infinity, and a weight of 0 by it; the others' weights, whose products stay
+        // under 2^128, differ by less than 2^-21)
+        if (scale2 == 0.f) scale2 = 0x1p-149f;
     }
 
     // The rows of step t, on their way to their buffer.
