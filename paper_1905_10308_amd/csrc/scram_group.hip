@@ -85,6 +85,9 @@ __device__ __forceinline__ float channel_value(const void* w, int f32, int c, fl
     return f32 ? static_cast<const float*>(w)[c] : to_float(static_cast<const uint16_t*>(w)[c]);
 }
 
+// What a difference of sums of squares leaves of them; not a number stays that (a maximum would hide it).
+__device__ __forceinline__ float not_negative(float x) { return x < 0.f ? 0.f : x; }
+
 // Sums of two values a thread over a block, on all its threads.
 __device__ __forceinline__ float2 block_sum(float2 x, float2 (&lds)[kBlock / 64])
 {
@@ -240,7 +243,7 @@ __global__ __launch_bounds__(kBlock) void group_stats_kernel(GroupParams p)
                        // what the weighted sum's rounding left out of the mean
                        const float d = to[3 * place] > 0.f ? x.y / to[3 * place] : 0.f;
                        to[3 * place + 1] = s_all[place] + d;
-                       to[3 * place + 2] = fmaxf(fmaf(-x.y, d, x.x), 0.f);
+                       to[3 * place + 2] = not_negative(fmaf(-x.y, d, x.x));
                    });
     }
 }
@@ -278,7 +281,7 @@ __global__ __launch_bounds__(kBlock) void group_join_kernel(GroupParams p)
             // what the weighted sum's rounding left out of the mean
             const float d = q.y / x.x;
             p.mean[u] = mean + d;
-            p.rstd[u] = 1.f / sqrtf(fmaxf(q.x / x.x - d * d, 0.f) + p.eps);
+            p.rstd[u] = 1.f / sqrtf(not_negative(q.x / x.x - d * d) + p.eps);
         }
     }
 }
@@ -589,7 +592,7 @@ __global__ __launch_bounds__(kBlock) void group_small_kernel(GroupParams p)
         }
         sum = block_sum(sum, s_part);
         const float d = sum.x / n, mean = near + d;  // (what the first sum's rounding left out)
-        const float rstd = 1.f / sqrtf(fmaxf(sum.y / n - d * d, 0.f) + p.eps);
+        const float rstd = 1.f / sqrtf(not_negative(sum.y / n - d * d) + p.eps);
         if (threadIdx.x == 0 && p.mean) {
             p.mean[u] = mean;
             p.rstd[u] = rstd;
