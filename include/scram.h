@@ -512,8 +512,8 @@ int scram_layer_norm_backward(const void* dY, int grad_dtype, const void* X, int
  * over the keys j < lengths[its slice of keys], and with SCRAM_CAUSAL at or
  * before the query's place.  A query without a key, or with scores of minus
  * infinity alone, gets a zero row.  The softmax is fp32 and online; in bf16 its
- * weights are rounded to bf16 (half a step each, 2^-8) for their product with
- * the values, which adds up in fp32 and is rounded once.
+ * weights keep 16 bits (two parts of bf16) in their product with the values,
+ * which adds up in fp32 and is rounded once.
  *
  * Arguments:
  *   Q, K, V     [S, Hq, Wq, d], [key_slices, Hk, Wk, d], [key_slices, Hk, Wk, dv]
@@ -559,8 +559,8 @@ int scram_dense_attend(const void* Q, const void* K, const void* V, int dtype, c
  * (dK_j, dV_j over the queries of all slices that read the key's).  The
  * weights are recomputed; D is formed of fp32 weights and not of the rounded
  * output, so that what a nearly certain weight leaves is not lost.  fp32
- * throughout, but that in bf16 p and ds are rounded to bf16 (half a step each,
- * 2^-8) for the products that give dQ, dK and dV; every result is rounded once
+ * throughout, but that in bf16 p and ds keep 16 bits (two parts of bf16) in the
+ * products that give dQ, dK and dV; every result is rounded once
  * to `dtype`.  Each has one writer and a fixed order of its sums: equal calls
  * give equal bits.  Keys behind `lengths`, and offsets that no pair has, get
  * zeros.

@@ -37,7 +37,7 @@ __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW >
 {
     using R = DenseRow<T, D>;
     // in bf16 without a bias the scale and the shift enter the exponential's argument in one step (a certain key's weight is
-    // then off 1 by a rounding, which its rounding to bf16 takes back)
+    // then off 1 by the shift's rounding, as their sum is, which divides it)
     constexpr bool kFold = sizeof(T) == 2 && !BIAS;
     extern __shared__ __align__(16) unsigned char lds[];
     QueryBlock<T, D, BIAS, KW> q(p, lds);
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW >
             }
 #pragma unroll
             for (int r = 0; r < R::kRowSteps; ++r) {
-                const uint4 w = as_operand<T>(s, r);
+                const RightOperand<T> w = as_operand<T>(s, r);
 #pragma unroll
                 for (int c = 0; c < R::kColumns; ++c)
                     o[c] = mma<T>(q.reader.column(r, c, kAt + q.kValues), w, o[c]);

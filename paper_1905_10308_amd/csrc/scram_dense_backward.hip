@@ -14,8 +14,8 @@
 // - offsets, with a bias: scores and ds once more, added up in registers over
 //   all pairs of tiles at one offset, whose diagonals are then one offset each.
 // The products with p and ds take them from the registers that formed them
-// (scram_dense.h); in bf16 both are rounded for that, to half a step of 2^-8,
-// as the matrix cores take no more, and sums stay in 32 bits.
+// (scram_dense.h); in bf16 both go in two parts, which add up to them to 2^-16,
+// as the matrix cores take 8 bits a number, and sums stay in 32 bits.
 //
 // Measured, bf16, 16 slices of 64 x 64, 64 channels, a bias: queries 278 us,
 // keys 241, offsets 230 (the vector units are busy for 0.57, 0.40 and 0.4 of
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW >
             s[i] = __builtin_amdgcn_exp2f(kFold ? fmaf(s[i], scale2, -shift) : s[i] - shift) * (g[i] - mean);
 #pragma unroll
         for (int r = 0; r < R::kRowSteps; ++r) {
-            const uint4 w = as_operand<T>(s, r);
+            const RightOperand<T> w = as_operand<T>(s, r);
 #pragma unroll
             for (int c = 0; c < R::kColumns; ++c) o[c] = mma<T>(q.reader.column(r, c, kAt), w, o[c]);
         }
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
             s = w * (g - row_numbers<T>(stats + 2 * kRows + 32 * u, h));
 #pragma unroll
             for (int r = 0; r < R::kRowSteps; ++r) {
-                const uint4 a = as_operand<T>(w, r), d = as_operand<T>(s, r);
+                const RightOperand<T> a = as_operand<T>(w, r), d = as_operand<T>(s, r);
 #pragma unroll
                 for (int c = 0; c < R::kColumns; ++c) {
                     dv[c] = mma<T>(reader.column(r, c, kG + 32 * u * R::kBytes), a, dv[c]);
