@@ -667,8 +667,9 @@ hipError_t launch_dense_kernel(void (*kernel)(P), uint64_t blocks, size_t lds, h
 {
     if (blocks == 0 || blocks > 0xFFFFFFFFull / THREADS) return hipErrorInvalidConfiguration;
     if (lds > 64 * 1024) {
+        // (the most that any call takes: a number for all threads of the program, which another may set before the launch)
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 static_cast<int>(lds));
+                                                 static_cast<int>(kLdsMost - kQueryStatic));
         if (e != hipSuccess) return e;
     }
     if (start || stop)

@@ -6,7 +6,7 @@ grid row, where the place on the bias' plane jumps.
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_gpu_dense import check  # noqa: E402
+from test_gpu_dense import check, make  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +62,35 @@ WIDE = [
 @pytest.mark.parametrize("c", WIDE, ids=lambda c: "x".join(map(str, c["shape"])))
 def test_wide_grids(scram, c, dtype):
     check(scram, c, dtype)
+
+
+def test_two_threads(scram):
+    """Calls of one kernel with different needs of shared memory, issued by two threads at once on streams of their own."""
+    import threading
+
+    torch.cuda.synchronize()
+    jobs = []
+    for Wk in (1500, 4993):
+        Q, K, V, dO, kw = make(dict(shape=(2, 2, 1, 300, 2, Wk, 128), heads=1, first=1000), "bf16")
+        jobs.append(lambda Q=Q, K=K, V=V, dO=dO, kw=kw: [scram.dense_attend(Q, K, V, **kw), *scram.dense_attend_backward(Q, K, V, dO, **kw)])
+    want = [job() for job in jobs]
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(50):
+                    got = jobs[i]()
+            stream.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want[i]))
+        except BaseException as e:  # noqa: BLE001 (told by the test below)
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
