@@ -595,7 +595,7 @@ inline QueryPlan query_plan(const DenseCall& c, int elem_bytes, bool split, Dens
         return blocks * (query_lds(c.g.d, elem_bytes, kw, buffers, windows) + kQueryStatic) <= kLdsMost;
     };
     // A tile that holds the queries of all slices of a key slice, each with a window: the keys are read once (64 slices of two
-    // queries on 4 of 64 x 64 keys 16.1 us, 16.4 with a tile a slice; 128 of one on 8 of 32 x 32 11.8 and 12.5).
+    // queries on 4 of 64 x 64 keys 16.4 us, 17.4 with a tile a slice; 128 of one on 8 of 32 x 32 12.3 and 13.0).
     const bool together = c.bias && p.share > 1 && int64_t(p.share) * p.nq <= 32 && p.share <= 16 && bytes <= 256 && room(8, p.share, 1);
     if (!c.bias || together) {
         p.per_group = p.share;
@@ -604,25 +604,26 @@ inline QueryPlan query_plan(const DenseCall& c, int elem_bytes, bool split, Dens
     }
     auto blocks = [&](int kw) { return int64_t(p.groups) * ((p.rows + 256 / kw - 1) / (256 / kw)); };
     // The more queries a block holds the fewer times keys are staged, but every CU needs a block.  Slices of 32 x 32, with
-    // 8 / 4 / 2 waves to a step's keys: 8 of them 11.1 / 15.2 / 17.1 us, 16 19.8 / 12.7 / 19.5, 32 36.6 / 23.6 / 17.2.
+    // 8 / 4 / 2 waves to a step's keys: 8 of them 12.1 / 16.3 / 18.0 us, 16 17.3 / 15.4 / 21.5, 32 29.7 / 22.7 / 20.0.
     int kw = 8;
     if (p.rows > 32 && blocks(4) >= 256) kw = 4;
     if (p.rows > 64 && blocks(2) >= 256) kw = 2;
     if (bytes > 256 && kw == 8) kw = 4;  // (a step of eight waves' rows of 512 bytes does not fit)
     if (!room(kw, together ? p.share : 1, 1)) kw = 2;  // (which any window fits beside that a call may have: kBiasWindowMost)
-    // The next step's rows are on their way while this one's are met: 2500 queries of 128 channels 95 us, with one buffer 106.
+    // The next step's rows are on their way while this one's are met: 2500 queries of 128 channels 120 us, with one buffer 131.
     // Two blocks a CU do as much for each other, and more where their registers let them (300 / 1024 slices of 48 queries
-    // on 1008 keys 20.7 / 50 us, 28.8 / 62 with two buffers; 256 of them, a block a CU, 19.5 and 18.3).
+    // on 1008 keys 23.1 / 55 us, 32.4 / 69 with two buffers; 256 of them, a block a CU, 21.1 and 19.5).
     p.buffers = room(kw, together ? p.share : 1, 2) ? 2 : 1;
     if (!c.bias && bytes <= 128 && blocks(kw) > 256 && !room(kw, 1, 2, 2) && room(kw, 1, 1, 2)) p.buffers = 1;
     p.tiles = (p.rows + 256 / kw - 1) / (256 / kw);
     const int keys = kw * wave_keys(bytes, kw);
     if (c.bias) p.window = int(bias_window(256 / kw, keys, c.g.Hk, c.g.Wk));
     while ((1 << p.window_shift) < p.per_group && c.bias) ++p.window_shift;
-    // one place then serves a vector's keys: 16 slices of 64 x 64 111 us, with a place a key 122
+    // one place then serves a vector's keys: 16 slices of 64 x 64 141 us, with a place a key 150
     p.runs = c.g.Wk % (elem_bytes == 2 ? 8 : 4) == 0;
-    // fewer blocks than CUs leave CUs idle: 8 slices of 4 queries on 64 x 64 keys in 8 parts 12.2 us with their join, 13.1 in
-    // 4, 20.8 whole; where the blocks fill the CUs the join only costs (16 slices of 16 x 16: 7.1 us, 10.6 in two parts)
+    // fewer blocks than CUs leave CUs idle: 8 slices of 4 queries on 64 x 64 keys 14.5 us in the 16 parts of one step each with
+    // their join, 12.7 in 8, 23.7 whole; 4 slices of 16 x 16 queries on as many 14.9 in 4 and 24.0.  Where the blocks fill the
+    // CUs the join only costs (32 slices of 32 x 32: 22.4 us, 35.3 in two parts)
     const int64_t steps = (p.nk + keys - 1) / keys;
     int64_t n = split ? 256 / blocks(kw) : 1;
     if (n > steps) n = steps;

@@ -8,9 +8,10 @@
 // output of the softmax stay in registers.  Scores are formed transposed
 // (scram_dense.h), so a query's statistics are a lane's own.
 //
-// Measured, bf16, 64 channels: 4 slices of 16384 queries and keys 323 us, 850 TFLOP/s, where a large matrix product reaches
-// 1130 on the same card; its vector units are busy for 0.66 of the time and the matrix cores for 0.39 at 1.85 GHz, the clock
-// that this load leaves.  16 slices of 4096 with a bias 112 us, 614 TFLOP/s.
+// Measured, bf16, 64 channels: 4 slices of 16384 queries and keys 428 us, 640 TFLOP/s (960 with the second part of the weights'
+// product, without which it took 314 us), where a large matrix product reaches 1130 on the same card; its vector units are busy
+// for 0.74 of the time and the matrix cores for 0.47 at 1.74 GHz, the clock that this load leaves.  16 slices of 4096 with a bias
+// 141 us, 490 TFLOP/s.
 //
 // The waves of a block share its queries (32, 64 or 128) and its keys: KW of
 // them take different keys of the same queries and join at the end.  Calls of
@@ -29,8 +30,9 @@ struct DenseForward : DenseQueries {
 };
 
 // Waves to a SIMD: four where the registers suffice, also at the price of some spilled ones outside the steps (with a bias and two
-// waves to a step's keys, 16 slices of 64 x 64: 124 us, with two waves a SIMD 157).  Calls of fewer queries have no more than
-// one block a CU, which spilling only slows down (16 of 32 x 32: 19.2 us, 22.8 spilled).
+// waves to a step's keys, 16 slices of 64 x 64: 147 us, with two waves a SIMD 161).  Calls of fewer queries have no more than
+// one block a CU, which spilling only slows down (16 of 32 x 32: 16.8 us, 19.1 spilled).  fp32 rows of 128 channels with a bias
+// spill with two waves too (96 bytes a lane).
 template <typename T, int D, bool BIAS, int KW>
 __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW > 2) ? 2 : 4) void dense_kernel(
     DenseForward p)

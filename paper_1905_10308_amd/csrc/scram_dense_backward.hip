@@ -17,10 +17,10 @@
 // (scram_dense.h); in bf16 both go in two parts, which add up to them to 2^-16,
 // as the matrix cores take 8 bits a number, and sums stay in 32 bits.
 //
-// Measured, bf16, 16 slices of 64 x 64, 64 channels, a bias: queries 278 us,
-// keys 241, offsets 230 (the vector units are busy for 0.57, 0.40 and 0.4 of
-// that, the matrix cores for 0.28, 0.24 and 0.14); 16 slices of a row of 2500
-// on 4 of keys, 128 channels, causal: queries 156 us, keys 182, their parts 8.
+// Measured, bf16, 16 slices of 64 x 64, 64 channels, a bias: queries 276 us,
+// keys 261, offsets 204 (the vector units are busy for 0.60, 0.48 and 0.45 of
+// that, the matrix cores for 0.31, 0.31 and 0.14); 16 slices of a row of 2500
+// on 4 of keys, 128 channels, causal: queries 166 us, keys 202, their parts 8.
 
 #include "scram_dense.h"
 
@@ -57,8 +57,9 @@ __device__ __forceinline__ float4 row_stats(float top, float sum, float dsum)
     return make_float4(apart ? top : top + __builtin_amdgcn_logf(sum), apart ? 1.f / sum : 1.f, dsum / sum, 0.f);
 }
 
-// The query side: two passes over the keys.  Four waves a SIMD as in the forward pass: 278 us, 335 with two (16 slices of 64 x 64
-// with a bias); with one block a CU two (8 of 48 x 48: 105 us, 116 with four).
+// The query side: two passes over the keys.  Four waves a SIMD as in the forward pass: 745 us, 779 with two (all kernels, 16
+// slices of 64 x 64 with a bias); with one block a CU two (8 of 48 x 48: 244 us, 253 with four).  fp32 rows of 128 channels spill
+// 232 to 328 bytes a lane with two.
 template <typename T, int D, bool BIAS, int KW>
 __global__ __launch_bounds__(kQueryThreads, D * sizeof(T) > 128 || (BIAS && KW > 2) ? 2 : 4) void dense_query_kernel(DenseBackward p)
 {
@@ -209,7 +210,7 @@ __device__ __forceinline__ f32x16_t row_numbers(const float* of, int h)
 }
 
 // The key side: a block's 128 keys against a run of the query tiles of the slices that read them.  Two waves a SIMD, as many as
-// 512 blocks are: squeezed into registers for three it took 285 us where this takes 241.
+// 512 blocks are: squeezed into registers for three 16 slices of 64 x 64 with a bias took 773 us where all kernels take 745.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
 {
@@ -324,7 +325,8 @@ __global__ __launch_bounds__(kBlock) void dense_key_kernel(DenseBackward p)
         // a query after which some key of the wave's comes, or a key that is not seen
         const bool masked = (p.causal && at0 < k_wave + 31) || k_wave + 32 > length;
         // a vector's rows are queries here, which lie side by side where it does not cross a grid row: grid rows of whole vectors
-        // and a tile that begins at one (16 slices of a run of 4080 on 64 x 64, all kernels: from place 8 on 664 us, from 5 on 675)
+        // and a tile that begins at one (16 slices of a run of 4080 on 64 x 64, all kernels: from place 8 on 746 us, from 5 on 757;
+        // rows behind the last query may meet what lies before the window, a number, with an infinite logarithm: a weight of 0)
         const bool runs = p.runs && (p.Hk == 1 || at0 % tile_half<T>() == 0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -623,12 +625,13 @@ BackwardPlan backward_plan(const DenseCall& c, int elem_bytes)
     if (c.bias) p.key_window = int(bias_window(64, kKeysBlock, c.g.Hk, c.g.Wk) + 3) & ~3;
     const int64_t tiles = int64_t(c.key_slices) * p.key_tiles;
     // splits of the queries: fewer than two blocks per CU leave CUs idle, and a part is worth a block from four tiles on (16 slices
-    // of 2500 on 4 of keys, 128 channels, causal, all kernels: 647 us whole, 406 / 329 / 372 in 2 / 4 / 8 parts)
+    // of 2500 on 4 of keys, 128 channels, all kernels: 840 us whole, 541 / 544 / 448 / 482 in 2 / 4 / 6 / 8 parts, of which this
+    // takes 6)
     const int rows = staged_rows(c.g.d * elem_bytes);
     if (c.causal && !c.origin && tiles <= 512) {
         // a key's runs by how many queries see it: the first keys' are many, and all blocks are as long, one a CU (all kernels:
-        // 4 rows of 6000, 32 channels 172 us in equal numbers of runs, so 148; 16 of 2500 on 4 of keys, 128 channels 329 and
-        // 321, with blocks half as long 351)
+        // 4 rows of 6000, 32 channels 212 us in equal numbers of runs, so 179, with blocks half as long 172; 16 of 2500 on
+        // 4 of keys, 128 channels 381, 368 and 394)
         p.key_each = 1;
         int64_t all = 0;
         for (int t = 0; t < p.key_tiles; ++t) all += c.key_slices * int64_t(key_runs(p, rows, t * kKeysBlock).all);
@@ -647,8 +650,8 @@ BackwardPlan backward_plan(const DenseCall& c, int elem_bytes)
     plan.part = p.key_splits > 1 ? round256(size_t(p.key_splits) * p.all_keys * 2 * c.g.d * sizeof(float)) : 0;
     if (c.bias) {
         p.x_tiles = (c.g.Wk + 31) / 32;
-        // four runs of grid rows for the waves of a block at least (all kernels: 8 slices of 64 x 64, 8 heads 383 us, 429 uncut;
-        // 16 of 7 x 7 26.9 and 32.5; cut in vain, 32 of 64 x 64 1355 and 1330, 16 of one row of 100 34.1 and 29.4)
+        // four runs of grid rows for the waves of a block at least (all kernels: 8 slices of 64 x 64, 8 heads 423 us, 466 uncut;
+        // 16 of 7 x 7 27.6 and 33.2; cut in vain, 32 of 64 x 64 1524 and 1493, 16 of one row of 100 35.1 and 30.5)
         const int64_t columns = int64_t(c.g.S / c.bias_rows) * (p.x_tiles > 1 ? p.x_tiles - 1 : 1);
         p.cuts = columns >= 4 || c.g.Hk == 1 ? 1 : 4;
         plan.offset_blocks = int64_t(c.bias_rows) * (2 * int64_t(c.g.Hk) - 1) * (2 * p.x_tiles - 1);

@@ -18,9 +18,10 @@
 //
 // Small groups are held in a block's registers and read once, in one launch.
 //
-// Measured, bf16: 4 images of 256 x 256, 128 channels 44.8 us, 67 MB each read
-// and written (3.0 TB/s; a copy of them takes 19.9, 6.7 TB/s, half of it from
-// the caches as here); the gradients of 4 of 128 x 128, 256 channels 41.6 us.
+// Measured, bf16, replayed from a graph: 4 images of 256 x 256, 128 channels
+// 44.9 us, 67 MB each read and written (3.0 TB/s; a copy of them takes 20.0, 6.7
+// TB/s, half of it from the caches as here); the gradients of 4 of 128 x 128,
+// 256 channels 41.4 us.  Alone in a trace the kernels take 47.2 and 46.2 us.
 
 #include "scram_rows.h"
 
